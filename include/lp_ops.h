@@ -1,7 +1,8 @@
 /* lp_ops.h -- single-kernel entry points of the serving step, for parity
- * checks and kernel timing.  They launch exactly the kernels the engine runs,
- * on caller-provided device buffers, asynchronously on `hip_stream` (a
- * hipStream_t, NULL for the null stream).  All pointers are device pointers
+ * checks and kernel timing.  They launch exactly the kernels the engine runs
+ * (those of the last section, a batch that shares a prefix, are for callers
+ * that plan their own steps), on caller-provided device buffers,
+ * asynchronously on `hip_stream` (a hipStream_t, NULL for the null stream).  All pointers are device pointers
  * unless stated otherwise; the caller owns every buffer.  Each returns LP_OK or
  * LP_EINVAL (bad sizes; checked before any launch) or LP_EHIP (launch error);
  * lp_last_error(NULL) then holds a message.  A call with no rows (M, rows or
@@ -163,6 +164,113 @@ typedef struct {
  * whose cumulative weight interval holds r.  V <= 2^21 (LP_EINVAL beyond). */
 int lp_op_sample(const float *logits, int64_t ld, int32_t M, int32_t V, const lp_sample_params *params,
                  int32_t *tokens, void *hip_stream);
+
+/* ---- a batch whose sequences begin with the same prefix ----
+ *
+ * Requests of one service often start with the same tokens (an instruction, a
+ * document they ask about).  The K and V of those P = prefix_len positions are
+ * kept once, in the cache blocks prefix_blocks[0 .. ceil(P / 64)); a
+ * sequence's own positions, P and up, are in the blocks of its row of the
+ * block table, position p in entry p / 64 at place p % 64, as everywhere in
+ * this header.  The entries below floor(P / 64) of a table row name the
+ * prefix's whole blocks; with P a multiple of 64 the table is therefore one
+ * that lp_op_decode_attention and lp_op_prefill_attention read too.  A prefix
+ * that ends inside a block leaves the first P % 64 places of a sequence's
+ * first own block unused.  P = 0 is no prefix (prefix_blocks may be null).
+ *
+ * The four calls below make a step: tables and cache entries from lengths,
+ * the projection's K and V into the cache, attention over it.  They share
+ * these rules.  Positions, slots, entries and block ids are data on the
+ * device, which no call can check before it launches; what does not fit is
+ * left out, never read or written through: a slot outside 0 .. n_slots - 1, a
+ * block id outside 0 .. n_blocks - 1 (-1 marks one that is missing), a
+ * negative position.  q, out, the caches and ws start on 16 bytes (LP_EINVAL
+ * otherwise).  A call keeps nothing from one call to the next, in ws neither,
+ * so ws needs no clearing; calls that overlap in time need one each. */
+
+/* Block tables, packed row offsets and cache entries of one step, from
+ * lengths that are on the device.  Sequence j (slot seq_slot[j], no slot
+ * twice) holds cached[j] positions before the step and lengths[j] after it:
+ * its n_j = max(0, lengths[j] - max(0, cached[j])) new positions are packed
+ * rows.
+ *   seq_start[0 .. n_seq]   exclusive sums of n_j (at most 2^31 - 1)
+ *   free_start[0 .. n_seq]  *free_head plus exclusive sums of the blocks each
+ *                           sequence takes: its new ones are
+ *                           free_blocks[free_start[j] ..].  free_start[n_seq]
+ *                           is the next free_head; past n_free, blocks are
+ *                           lacking.  free_head may point at it.
+ *   block_table             [n_slots][max_blocks], updated: entries below
+ *                           floor(P / 64) that the length reaches become the
+ *                           prefix's blocks; where lengths[j] > P, entries
+ *                           from have_j up to ceil(lengths[j] / 64) the
+ *                           blocks taken, -1 if they are lacking; have_j =
+ *                           ceil(cached[j] / 64) if cached[j] > P, else
+ *                           floor(P / 64).  Others stay.
+ *   row_slot, row_pos,      [max_rows]: slot, position and cache entry (64 *
+ *   row_entry               block + place) of each row; the entry is -1 where
+ *                           there is no block: past the table's width, or
+ *                           lacking.  Rows from seq_start[n_seq] on get -1 in
+ *                           all three, rows from max_rows on are left out.
+ * Rows at positions below P (a request that computes the prefix itself) have
+ * their entry in prefix_blocks.  All pointers but prefix_blocks (P < 1) and
+ * free_blocks (n_free = 0) are required when n_seq > 0; with n_seq = 0 nothing
+ * is written. */
+int lp_op_block_tables(const int32_t *seq_slot, const int32_t *cached, const int32_t *lengths, int32_t n_seq,
+                       const int32_t *prefix_blocks, int32_t prefix_len, const int32_t *free_blocks, int32_t n_free,
+                       const int32_t *free_head, int32_t *block_table, int32_t n_slots, int32_t max_blocks,
+                       int32_t *seq_start, int32_t *free_start, int32_t *row_slot, int32_t *row_pos,
+                       int64_t *row_entry, int32_t max_rows, void *hip_stream);
+
+/* The QKV projection of `rows` rows as lp_op_gemm writes it (fp32, row stride
+ * ld >= (Hq + 2 Hkv) hd elements: query heads, key heads, value heads), made
+ * ready for attention: q and k heads get the rotary embedding of their row's
+ * position (dimensions i and i + hd / 2 form a pair, rotated by the angle
+ * whose cosine and sine are rope_cos[pos][i], rope_sin[pos][i], tables of
+ * n_pos positions), q goes to q [rows][Hq][hd] and k, v to the cache at
+ * row_entry, all rounded to dtype once.  K and V of a row with an entry
+ * outside 0 .. 64 n_blocks - 1 are left out; of a row with a position outside
+ * 0 .. n_pos - 1, everything.  No two rows may have the same entry.  qkv and
+ * the tables start on 8 bytes, ld is even; head_dim 64 or 128. */
+int lp_op_qkv_append(int32_t dtype, const float *qkv, int64_t ld, const float *rope_cos, const float *rope_sin,
+                     int32_t n_pos, const int32_t *row_pos, const int64_t *row_entry, int32_t rows, void *q,
+                     void *k_cache, void *v_cache, int64_t n_blocks, int32_t n_heads, int32_t n_kv_heads,
+                     int32_t head_dim, void *hip_stream);
+
+/* Decode attention with a shared prefix: row m of q, out [M][Hq][hd] reads
+ * positions 0 .. row_pos[m] of slot row_slot[m], those below P from the
+ * prefix's blocks, which are read once for the whole batch.  Contexts longer
+ * than max_ctx are clamped to it (max_ctx, prefix_len and M Hq at most 2^30).
+ * A row that reads nothing (position -1, no
+ * such slot, all its blocks missing) gets zeros.  Any group Hq / Hkv; head_dim
+ * 64 or 128 in every dtype; 64 * max_blocks >= max_ctx where max_ctx > P.
+ * ws: at least lp_op_prefix_decode_attention_ws_bytes of the same sizes (0
+ * for sizes that are refused). */
+size_t lp_op_prefix_decode_attention_ws_bytes(int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                              int32_t prefix_len, int32_t max_ctx);
+int lp_op_prefix_decode_attention(int32_t dtype, const void *q, void *out, const void *k_cache, const void *v_cache,
+                                  int64_t n_blocks, const int32_t *prefix_blocks, int32_t prefix_len,
+                                  const int32_t *block_table, int32_t n_slots, int32_t max_blocks,
+                                  const int32_t *row_slot, const int32_t *row_pos, int32_t M, int32_t n_heads,
+                                  int32_t n_kv_heads, int32_t head_dim, int32_t max_ctx, void *ws, size_t ws_bytes,
+                                  void *hip_stream);
+
+/* Causal attention of packed new tokens with a shared prefix: sequence j owns
+ * rows [seq_start[j], seq_start[j + 1]) of q, out [rows][Hq][hd], at positions
+ * seq_pos[j], seq_pos[j] + 1, ... of slot seq_slot[j]; each row reads
+ * positions 0 up to its own.  K and V of the new positions are in the cache
+ * already, as are those before them (a sequence may go on from any context:
+ * the prefix, one longer than it, or none of it).  Contexts and rows that read
+ * nothing as for decode.  max_new bounds the rows of every sequence (rows of a
+ * longer one from max_new on hold no result); rows of no sequence stay as they
+ * are.  seq_start ascends; what of it lies outside 0 .. rows is left out. */
+size_t lp_op_prefix_prefill_attention_ws_bytes(int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                               int32_t prefix_len, int32_t max_ctx);
+int lp_op_prefix_prefill_attention(int32_t dtype, const void *q, void *out, const void *k_cache, const void *v_cache,
+                                   int64_t n_blocks, const int32_t *prefix_blocks, int32_t prefix_len,
+                                   const int32_t *block_table, int32_t n_slots, int32_t max_blocks,
+                                   const int32_t *seq_start, const int32_t *seq_slot, const int32_t *seq_pos,
+                                   int32_t n_seq, int32_t rows, int32_t max_new, int32_t n_heads, int32_t n_kv_heads,
+                                   int32_t head_dim, int32_t max_ctx, void *ws, size_t ws_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

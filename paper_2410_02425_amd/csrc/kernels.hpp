@@ -153,6 +153,47 @@ void launch_prefill_attention(const T *q, T *out, const int32_t *seq_start, cons
                               int n_seq, int max_len, const KVCache &kv, int layer, int n_heads,
                               hipStream_t s);
 
+// A batch whose sequences begin with the same prefix_len positions, which are
+// cached once, in prefix_blocks; a sequence's other positions are in the
+// blocks of its row of kv.block_table.  Sequence j has rows [seq_start[j],
+// seq_start[j + 1]) at positions seq_pos[j] .. of slot seq_slot[j]; with
+// seq_start null it is row j alone (decode).
+struct PrefixBatch {
+  KVCache kv;
+  const int32_t *prefix_blocks;
+  int32_t prefix_len, n_slots;
+  const int32_t *seq_start, *seq_slot, *seq_pos;
+  int32_t n_seq, rows, max_new, max_ctx, n_heads;
+};
+size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_heads, int head_dim, int prefix_len,
+                                 int max_ctx);
+template <typename T>
+void launch_prefix_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s);
+
+// Block tables, row offsets and cache entries of a step (see lp_op_block_tables).
+struct TableStep {
+  const int32_t *seq_slot, *cached, *lengths;
+  const int32_t *prefix_blocks, *free_blocks, *free_head;
+  int32_t *block_table, *seq_start, *free_start, *row_slot, *row_pos;
+  int64_t *row_entry;
+  int32_t n_seq, prefix_len, n_free, n_slots, max_blocks, max_rows;
+};
+void launch_block_tables(const TableStep &t, hipStream_t s);
+
+// Rotary embedding of the fp32 QKV projection, q rounded to q, k and v to
+// their cache entries (see lp_op_qkv_append).
+struct QkvAppend {
+  const float *qkv;
+  int64_t ld;
+  const float *rope_cos, *rope_sin;
+  const int32_t *row_pos;
+  const int64_t *row_entry;
+  int64_t n_blocks;
+  int32_t n_pos, rows, n_heads, n_kv_heads, head_dim;
+};
+template <typename T>
+void launch_qkv_append(const QkvAppend &a, T *q, T *k, T *v, hipStream_t s);
+
 // Greedy token per row (lowest index on ties): tok -> slot_tok[out_slot[m]]
 // and tok_log[m].
 void launch_argmax(const float *logits, int64_t ld, int M, int V, const int32_t *out_slot,

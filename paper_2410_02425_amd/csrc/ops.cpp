@@ -205,3 +205,126 @@ extern "C" int lp_op_init_weight(int32_t dtype, void *dst, uint64_t seed, int32_
     OPCHK(false, "init_weight: dtype");
   return op_status();
 }
+
+// ------------------------------------------------------------------ a batch that shares a prefix
+
+constexpr int32_t PREFIX_MAX_POS = 1 << 30;  // prefix and context lengths, (row, head) pairs
+
+static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+extern "C" int lp_op_block_tables(const int32_t *seq_slot, const int32_t *cached, const int32_t *lengths,
+                                  int32_t n_seq, const int32_t *prefix_blocks, int32_t prefix_len,
+                                  const int32_t *free_blocks, int32_t n_free, const int32_t *free_head,
+                                  int32_t *block_table, int32_t n_slots, int32_t max_blocks, int32_t *seq_start,
+                                  int32_t *free_start, int32_t *row_slot, int32_t *row_pos, int64_t *row_entry,
+                                  int32_t max_rows, void *stream) {
+  OPCHK(n_seq >= 0 && prefix_len >= 0 && prefix_len <= PREFIX_MAX_POS && n_free >= 0 && n_slots > 0 && max_blocks > 0 && max_rows >= 0,
+        "block tables: sizes");
+  if (n_seq == 0) return LP_OK;  // no sequences: nothing is read or written
+  OPCHK(seq_slot && cached && lengths && free_head && block_table && seq_start && free_start,
+        "block tables: pointers");
+  OPCHK((prefix_len == 0 || prefix_blocks) && (n_free == 0 || free_blocks), "block tables: block lists");
+  OPCHK(max_rows == 0 || (row_slot && row_pos && row_entry), "block tables: row arrays");
+  TableStep t{seq_slot, cached, lengths, prefix_blocks, free_blocks, free_head, block_table, seq_start, free_start,
+              row_slot, row_pos, row_entry, n_seq, prefix_len, n_free, n_slots, max_blocks, max_rows};
+  launch_block_tables(t, (hipStream_t)stream);
+  return op_status();
+}
+
+extern "C" int lp_op_qkv_append(int32_t dtype, const float *qkv, int64_t ld, const float *rope_cos,
+                                const float *rope_sin, int32_t n_pos, const int32_t *row_pos,
+                                const int64_t *row_entry, int32_t rows, void *q, void *k_cache, void *v_cache,
+                                int64_t n_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                void *stream) {
+  OPCHK(n_heads > 0 && n_kv_heads > 0 && n_heads % n_kv_heads == 0, "qkv append: heads");
+  OPCHK(head_dim == 64 || head_dim == 128, "qkv append: head_dim must be 64 or 128");
+  OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "qkv append: dtype");
+  OPCHK(rows >= 0 && n_pos > 0 && n_blocks > 0 && ld % 2 == 0 &&
+            ld >= ((int64_t)n_heads + 2 * (int64_t)n_kv_heads) * head_dim,
+        "qkv append: sizes");
+  if (rows == 0) return LP_OK;  // no rows: nothing is read or written
+  OPCHK(qkv && rope_cos && rope_sin && row_pos && row_entry && q && k_cache && v_cache, "qkv append: pointers");
+  OPCHK((((uintptr_t)qkv | (uintptr_t)rope_cos | (uintptr_t)rope_sin) & 7) == 0,
+        "qkv append: qkv and the rotary tables start on 8 bytes");
+  OPCHK(aligned16(q) && aligned16(k_cache) && aligned16(v_cache), "qkv append: q and the caches start on 16 bytes");
+  QkvAppend a{qkv, ld, rope_cos, rope_sin, row_pos, row_entry, n_blocks, n_pos, rows, n_heads, n_kv_heads, head_dim};
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == LP_BF16)
+    launch_qkv_append<bf16_t>(a, (bf16_t *)q, (bf16_t *)k_cache, (bf16_t *)v_cache, s);
+  else if (dtype == LP_F16)
+    launch_qkv_append<f16_t>(a, (f16_t *)q, (f16_t *)k_cache, (f16_t *)v_cache, s);
+  else
+    launch_qkv_append<float>(a, (float *)q, (float *)k_cache, (float *)v_cache, s);
+  return op_status();
+}
+
+static bool prefix_sizes(int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t prefix_len,
+                         int32_t max_ctx) {
+  return rows >= 0 && n_heads > 0 && n_kv_heads > 0 && n_heads % n_kv_heads == 0 &&
+         (head_dim == 64 || head_dim == 128) && prefix_len >= 0 && prefix_len <= PREFIX_MAX_POS && max_ctx > 0 &&
+         max_ctx <= PREFIX_MAX_POS && (int64_t)rows * n_heads <= PREFIX_MAX_POS;
+}
+
+extern "C" size_t lp_op_prefix_decode_attention_ws_bytes(int32_t M, int32_t n_heads, int32_t n_kv_heads,
+                                                         int32_t head_dim, int32_t prefix_len, int32_t max_ctx) {
+  if (!prefix_sizes(M, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx)) return 0;
+  return prefix_attention_ws_bytes(true, M, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx);
+}
+
+extern "C" size_t lp_op_prefix_prefill_attention_ws_bytes(int32_t rows, int32_t n_heads, int32_t n_kv_heads,
+                                                          int32_t head_dim, int32_t prefix_len, int32_t max_ctx) {
+  if (!prefix_sizes(rows, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx)) return 0;
+  return prefix_attention_ws_bytes(false, rows, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx);
+}
+
+// The checks that both phases share; `b` is complete but for them.
+static int prefix_attention(int32_t dtype, const void *q, void *out, const PrefixBatch &b, bool decode, void *ws,
+                            size_t ws_bytes, void *stream) {
+  OPCHK(prefix_sizes(b.rows, b.n_heads, b.kv.n_kv_heads, b.kv.head_dim, b.prefix_len, b.max_ctx),
+        "prefix attention: sizes (rows, heads, head_dim 64 or 128, prefix_len, max_ctx)");
+  OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "prefix attention: dtype");
+  OPCHK(b.n_seq >= 0 && b.kv.n_blocks > 0 && b.n_slots > 0 && b.max_new > 0, "prefix attention: sizes");
+  OPCHK(b.kv.max_blocks > 0 && (b.max_ctx <= b.prefix_len || (int64_t)b.kv.max_blocks * KV_BLOCK >= b.max_ctx),
+        "prefix attention: max_blocks too small for max_ctx");
+  if (b.rows == 0 || b.n_seq == 0) return LP_OK;  // no rows: nothing is read or written
+  OPCHK(q && out && b.kv.k && b.kv.v && b.kv.block_table && b.seq_slot && b.seq_pos && (decode || b.seq_start) &&
+            (b.prefix_len == 0 || b.prefix_blocks),
+        "prefix attention: pointers");
+  OPCHK(aligned16(q) && aligned16(out) && aligned16(b.kv.k) && aligned16(b.kv.v) && aligned16(ws),
+        "prefix attention: q, out, the caches and ws start on 16 bytes");
+  const size_t need = prefix_attention_ws_bytes(decode, b.rows, b.n_heads, b.kv.n_kv_heads, b.kv.head_dim,
+                                                b.prefix_len, b.max_ctx);
+  OPCHK(need == 0 || (ws && ws_bytes >= need), "prefix attention: ws");
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == LP_BF16)
+    launch_prefix_attention<bf16_t>((const bf16_t *)q, (bf16_t *)out, b, (float *)ws, s);
+  else if (dtype == LP_F16)
+    launch_prefix_attention<f16_t>((const f16_t *)q, (f16_t *)out, b, (float *)ws, s);
+  else
+    launch_prefix_attention<float>((const float *)q, (float *)out, b, (float *)ws, s);
+  return op_status();
+}
+
+extern "C" int lp_op_prefix_decode_attention(int32_t dtype, const void *q, void *out, const void *k_cache,
+                                             const void *v_cache, int64_t n_blocks, const int32_t *prefix_blocks,
+                                             int32_t prefix_len, const int32_t *block_table, int32_t n_slots,
+                                             int32_t max_blocks, const int32_t *row_slot, const int32_t *row_pos,
+                                             int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                             int32_t max_ctx, void *ws, size_t ws_bytes, void *stream) {
+  PrefixBatch b{{(void *)k_cache, (void *)v_cache, block_table, max_blocks, n_blocks, n_kv_heads, head_dim},
+                prefix_blocks, prefix_len, n_slots, nullptr, row_slot, row_pos, M, M, 1, max_ctx, n_heads};
+  return prefix_attention(dtype, q, out, b, true, ws, ws_bytes, stream);
+}
+
+extern "C" int lp_op_prefix_prefill_attention(int32_t dtype, const void *q, void *out, const void *k_cache,
+                                              const void *v_cache, int64_t n_blocks, const int32_t *prefix_blocks,
+                                              int32_t prefix_len, const int32_t *block_table, int32_t n_slots,
+                                              int32_t max_blocks, const int32_t *seq_start, const int32_t *seq_slot,
+                                              const int32_t *seq_pos, int32_t n_seq, int32_t rows, int32_t max_new,
+                                              int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_ctx,
+                                              void *ws, size_t ws_bytes, void *stream) {
+  PrefixBatch b{{(void *)k_cache, (void *)v_cache, block_table, max_blocks, n_blocks, n_kv_heads, head_dim},
+                prefix_blocks, prefix_len, n_slots, seq_start, seq_slot, seq_pos, n_seq, rows, max_new, max_ctx,
+                n_heads};
+  return prefix_attention(dtype, q, out, b, false, ws, ws_bytes, stream);
+}

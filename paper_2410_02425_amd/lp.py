@@ -27,6 +27,8 @@ EXPORTED = [
     "lp_op_gemm", "lp_op_gemm_plan", "lp_op_packed_weight_bytes", "lp_op_pack_weight", "lp_op_rmsnorm", "lp_op_decode_attention_ws_bytes", "lp_op_decode_attention",
     "lp_op_decode_attention_noalloc",
     "lp_op_prefill_attention", "lp_op_argmax", "lp_op_init_weight", "lp_op_sample",
+    "lp_op_block_tables", "lp_op_qkv_append", "lp_op_prefix_decode_attention_ws_bytes",
+    "lp_op_prefix_decode_attention", "lp_op_prefix_prefill_attention_ws_bytes", "lp_op_prefix_prefill_attention",
 ]
 
 
@@ -127,6 +129,12 @@ def lib():
             "lp_op_argmax": [vp, i64, i32, i32, vp, vp],
             "lp_op_init_weight": [i32, vp, C.c_uint64, i32, i64, i64, f32, vp],
             "lp_op_sample": [vp, i64, i32, i32, vp, vp, vp],
+            "lp_op_block_tables": [vp, vp, vp, i32, vp, i32, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, i32, vp],
+            "lp_op_qkv_append": [i32, vp, i64, vp, vp, i32, vp, vp, i32, vp, vp, vp, i64, i32, i32, i32, vp],
+            "lp_op_prefix_decode_attention": [i32, vp, vp, vp, vp, i64, vp, i32, vp, i32, i32, vp, vp, i32, i32, i32,
+                                              i32, i32, vp, sz, vp],
+            "lp_op_prefix_prefill_attention": [i32, vp, vp, vp, vp, i64, vp, i32, vp, i32, i32, vp, vp, vp, i32, i32,
+                                               i32, i32, i32, i32, i32, vp, sz, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -136,6 +144,9 @@ def lib():
         L.lp_last_error.restype = C.c_char_p
         L.lp_op_decode_attention_ws_bytes.argtypes = [i32, i32, i32, i32]
         L.lp_op_decode_attention_ws_bytes.restype = sz
+        for name in ("lp_op_prefix_decode_attention_ws_bytes", "lp_op_prefix_prefill_attention_ws_bytes"):
+            getattr(L, name).argtypes = [i32] * 6
+            getattr(L, name).restype = sz
         L.lp_op_packed_weight_bytes.argtypes = [i32, i32, i32]
         L.lp_op_packed_weight_bytes.restype = sz
         L.lp_engine_destroy.restype = None
@@ -512,3 +523,149 @@ def sample_params_array(rows) -> np.ndarray:
 def op_init_weight(dst, seed, tensor_id, std):
     rows, cols = dst.shape
     _check(lib().lp_op_init_weight(_dt(dst), _ptr(dst), seed, tensor_id, rows, cols, std, _stream()))
+
+
+# ------------------------------------------------------------------ a batch that shares a prefix
+
+def _call(fn, device, args):
+    """fn(*args, stream) on the current stream of `device`, which is made current for the call."""
+    import torch
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, stream))
+
+
+def _tensors(device, dtype, **named):
+    """Data pointers of contiguous tensors of one dtype on `device`, in order (None: a null pointer)."""
+    _need(device.type == "cuda", f"tensors on a GPU, got {device}")
+    ptrs = []
+    for name, t in named.items():
+        if t is None:
+            ptrs.append(None)
+            continue
+        if t.dtype != dtype or t.device != device or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {dtype} tensor on {device}, got {t.dtype} on {t.device}"
+                             f"{'' if t.is_contiguous() else ', not contiguous'}")
+        ptrs.append(t.data_ptr())
+    return ptrs
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _dt3(t):
+    import torch
+    d = {torch.float32: LP_F32, torch.bfloat16: LP_BF16, torch.float16: LP_F16}.get(t.dtype)
+    _need(d is not None, f"float32, bfloat16 or float16 tensors, got {t.dtype}")
+    return d
+
+
+def op_block_tables(seq_slot, cached, lengths, prefix_blocks, prefix_len, free_blocks, free_head, block_table,
+                    seq_start, free_start, row_slot, row_pos, row_entry):
+    """A step's block tables, packed row offsets and cache entries from device
+    lengths (lp_op_block_tables).  int32 tensors: seq_slot, cached, lengths [n],
+    prefix_blocks [at least ceil(prefix_len / 64)] (or None), free_blocks,
+    free_head [1], block_table [n_slots, max_blocks], seq_start and free_start
+    [n + 1], row_slot and row_pos [max_rows]; row_entry int64 [max_rows]."""
+    import torch
+    dev, n = seq_slot.device, seq_slot.numel()
+    i32 = _tensors(dev, torch.int32, seq_slot=seq_slot, cached=cached, lengths=lengths, prefix_blocks=prefix_blocks,
+                   free_blocks=free_blocks, free_head=free_head, block_table=block_table, seq_start=seq_start,
+                   free_start=free_start, row_slot=row_slot, row_pos=row_pos)
+    entry, = _tensors(dev, torch.int64, row_entry=row_entry)
+    max_rows = row_entry.numel()
+    _need(cached.numel() == n and lengths.numel() == n and seq_start.numel() == n + 1 and free_start.numel() == n + 1
+          and free_head.numel() >= 1, "seq_slot, cached, lengths [n]; seq_start, free_start [n + 1]; free_head [1]")
+    _need(row_slot.numel() == max_rows and row_pos.numel() == max_rows, "row_slot, row_pos and row_entry: one length")
+    _need(prefix_blocks is None or prefix_blocks.numel() * 64 >= prefix_len, "prefix_blocks: ceil(prefix_len / 64)")
+    _call(lib().lp_op_block_tables, dev,
+          (i32[0], i32[1], i32[2], n, i32[3], prefix_len, i32[4], free_blocks.numel(), i32[5], i32[6],
+           block_table.shape[0], block_table.shape[1], i32[7], i32[8], i32[9], i32[10], entry, max_rows))
+
+
+def op_qkv_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, kc, vc):
+    """Rotates q and k of the fp32 projection qkv [rows, (Hq + 2 Hkv) hd] (rows
+    may be strided), rounds q to q [rows, Hq, hd] and stores k and v in the
+    cache at row_entry (lp_op_qkv_append)."""
+    import torch
+    dev, dt = q.device, _dt3(q)
+    rows, hq, hd = q.shape
+    n_blocks, hkv = kc.shape[:2]
+    acts = _tensors(dev, q.dtype, q=q, kc=kc, vc=vc)
+    cos, sin = _tensors(dev, torch.float32, rope_cos=rope_cos, rope_sin=rope_sin)
+    pos, = _tensors(dev, torch.int32, row_pos=row_pos)
+    entry, = _tensors(dev, torch.int64, row_entry=row_entry)
+    _need(qkv.dtype == torch.float32 and qkv.device == dev and qkv.dim() == 2 and (rows == 0 or qkv.stride(1) == 1),
+          "qkv: float32 rows of contiguous columns")
+    _need(tuple(kc.shape) == (n_blocks, hkv, 64, hd) and tuple(vc.shape) == (n_blocks, hkv, hd, 64),
+          "kc [n_blocks, Hkv, 64, hd], vc [n_blocks, Hkv, hd, 64]")
+    _need(tuple(qkv.shape) == (rows, (hq + 2 * hkv) * hd) and row_pos.numel() == rows and row_entry.numel() == rows,
+          "qkv [rows, (Hq + 2 Hkv) hd], row_pos and row_entry [rows]")
+    _need(rope_cos.shape == rope_sin.shape and rope_cos.dim() == 2 and rope_cos.shape[1] == hd // 2,
+          "rope_cos, rope_sin [positions, hd / 2]")
+    ld = qkv.stride(0) if rows > 1 else qkv.shape[1]
+    _call(lib().lp_op_qkv_append, dev,
+          (dt, qkv.data_ptr(), ld, cos, sin, rope_cos.shape[0], pos, entry, rows, acts[0], acts[1], acts[2], n_blocks,
+           hq, hkv, hd))
+
+
+def prefix_decode_attention_ws_bytes(M, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx):
+    return lib().lp_op_prefix_decode_attention_ws_bytes(M, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx)
+
+
+def prefix_prefill_attention_ws_bytes(rows, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx):
+    return lib().lp_op_prefix_prefill_attention_ws_bytes(rows, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx)
+
+
+def _prefix_args(q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws, **index):
+    """What both phases hand over alike: dtype and cache arguments, the index
+    tensors' pointers, and the workspace's pointer and bytes."""
+    import torch
+    dev, dt = q.device, _dt3(q)
+    hd = q.shape[2]
+    n_blocks, hkv = kc.shape[:2]
+    acts = _tensors(dev, q.dtype, q=q, out=out, kc=kc, vc=vc)
+    idx = _tensors(dev, torch.int32, prefix_blocks=prefix_blocks, block_table=block_table, **index)
+    _need(out.shape == q.shape, "out: shape of q")
+    _need(tuple(kc.shape) == (n_blocks, hkv, 64, hd) and tuple(vc.shape) == (n_blocks, hkv, hd, 64),
+          "kc [n_blocks, Hkv, 64, hd], vc [n_blocks, Hkv, hd, 64]")
+    _need(prefix_blocks is None or prefix_blocks.numel() * 64 >= prefix_len, "prefix_blocks: ceil(prefix_len / 64)")
+    _need(ws is None or (ws.device == dev and ws.is_contiguous()), "ws: contiguous, on the device of q")
+    cache = (dt, *acts, n_blocks, idx[0], prefix_len, idx[1], block_table.shape[0], block_table.shape[1])
+    space = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+    return cache, idx[2:], space
+
+
+def op_prefix_decode_attention(q, out, kc, vc, prefix_blocks, prefix_len, block_table, row_slot, row_pos, max_ctx, ws):
+    """One token a row over the shared prefix and the row's own blocks
+    (lp_op_prefix_decode_attention): q, out [M, Hq, hd], kc [n_blocks, Hkv, 64,
+    hd], vc [n_blocks, Hkv, hd, 64]; int32 prefix_blocks (None without a
+    prefix), block_table [n_slots, max_blocks], row_slot and row_pos [M]; ws of
+    prefix_decode_attention_ws_bytes."""
+    M, hq, hd = q.shape
+    cache, idx, space = _prefix_args(q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws, row_slot=row_slot,
+                                     row_pos=row_pos)
+    _need(row_slot.numel() == M and row_pos.numel() == M, "row_slot, row_pos [M]")
+    _call(lib().lp_op_prefix_decode_attention, q.device,
+          (*cache, *idx, M, hq, kc.shape[1], hd, max_ctx, *space))
+
+
+def op_prefix_prefill_attention(q, out, kc, vc, prefix_blocks, prefix_len, block_table, seq_start, seq_slot, seq_pos,
+                                max_new, max_ctx, ws):
+    """Packed new tokens, causal, over the shared prefix and their sequences'
+    own blocks (lp_op_prefix_prefill_attention): q, out [rows, Hq, hd]; int32
+    seq_start [n + 1], seq_slot and seq_pos [n] (position of each sequence's
+    first row); the others as for decode, ws of
+    prefix_prefill_attention_ws_bytes."""
+    rows, hq, hd = q.shape
+    n = seq_slot.numel()
+    cache, idx, space = _prefix_args(q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws, seq_start=seq_start,
+                                     seq_slot=seq_slot, seq_pos=seq_pos)
+    _need(seq_start.numel() == n + 1 and seq_pos.numel() == n, "seq_start [n + 1], seq_slot and seq_pos [n]")
+    _call(lib().lp_op_prefix_prefill_attention, q.device,
+          (*cache, *idx, n, rows, max_new, hq, kc.shape[1], hd, max_ctx, *space))
