@@ -11,6 +11,7 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef float floatx4_t __attribute__((ext_vector_type(4)));
 typedef float floatx16_t __attribute__((ext_vector_type(16)));
+typedef unsigned int u32x4_tt __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float bf16_to_f32(bf16_t b) { return __uint_as_float((uint32_t)b << 16); }
 
@@ -184,6 +185,70 @@ __device__ __forceinline__ void dma16s(const void *base, uint32_t off, uint32_t 
 __device__ __forceinline__ uint32_t lds_addr(const void *p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)p;
 }
+
+// Maximum / sum with the other half of the wave (lane ^ 32).
+__device__ __forceinline__ float half_swap_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_swap_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <typename T>
+__device__ __forceinline__ typename Mfma<T>::v8 pack8(const float *p) {
+  typedef __typeof__((typename Mfma<T>::v8){}[0]) elem_t;
+  typename Mfma<T>::v8 v;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = (elem_t)p[j];
+  return v;
+}
+
+// Stores a 32-dim tile of O^T times inv: a lane holds one row's dims 8 (r / 4) +
+// 4 hh + r % 4.  The halves of the wave trade every other four dims, so that a
+// lane stores eight consecutive dims at once (dst: the row's tile), from a base
+// that is aligned for them; all lanes call, `valid` ones store.
+template <typename T>
+__device__ __forceinline__ void store_o32(T *dst, const floatx16_t &o, float inv, int hh, bool valid) {
+  typedef uint32_t u4_t __attribute__((ext_vector_type(4), aligned(4)));
+  const bool al4 = ((uintptr_t)dst & 3) == 0;
+#pragma unroll
+  for (int r8 = 0; r8 < 2; ++r8) {
+    uint32_t w[2][2];  // dims 16 r8 + 8 i + 4 hh + {0, 1}, {2, 3}
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const T lo = Act<T>::st(o[r8 * 8 + i * 4 + e * 2] * inv), hi = Act<T>::st(o[r8 * 8 + i * 4 + e * 2 + 1] * inv);
+        w[i][e] = (uint32_t)__builtin_bit_cast(uint16_t, lo) | (uint32_t)__builtin_bit_cast(uint16_t, hi) << 16;
+      }
+    u4_t v;  // dims 16 r8 + 8 hh ..
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const auto t = __builtin_amdgcn_permlane32_swap(w[0][e], w[1][e], false, false);
+      v[e] = t[0];
+      v[e + 2] = t[1];
+    }
+    T *d = dst + r8 * 16 + hh * 8;
+    if (valid) {
+      if (al4) {
+        *(u4_t *)d = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          d[2 * e] = __builtin_bit_cast(T, (uint16_t)v[e]);
+          d[2 * e + 1] = __builtin_bit_cast(T, (uint16_t)(v[e] >> 16));
+        }
+      }
+    }
+  }
+}
+
+// Base-2 score past which the maximum is taken off before the scale: up to here
+// a rounded mc is within 2^-13, which moves a weight of 1 by 8.5e-5, less than
+// its rounding to 16 bits (2.4e-4 in f16).
+constexpr float PFA_LARGE = 4096.f;
+
 
 // Rotary embedding of one pair (x0, x1) = (dimension i, dimension i + hd/2)
 // at angle theta, cs = cos theta, sn = sin theta.  Every kernel that rotates
