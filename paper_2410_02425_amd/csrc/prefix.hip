@@ -13,6 +13,7 @@
 // e of the prefix, entry nP + i is own block F + i of the sequence, F =
 // floor(P / 64) being the first that is not all prefix.
 #include <algorithm>
+#include <type_traits>
 
 #include "device.hpp"
 
@@ -107,7 +108,7 @@ __device__ __forceinline__ bool own_tile(const PrefixArgs &a, int u, int &j, int
     if (u < total) {
       const int k = __popcll(__ballot(incl <= u));  // sequences wholly before the tile
       j = base + k;
-      r0 = (u - __shfl(incl - tiles, k, 64)) * RT;
+      r0 = (__shfl(incl, k, 64) - 1 - u) * RT;  // from the last, whose rows see most
       return true;
     }
     u -= total;
@@ -240,8 +241,8 @@ __global__ __launch_bounds__(256) void prefix_attn_kernel(const T *__restrict__ 
 // infinite or NaN there.  A tile whose result is not finite is therefore
 // computed again with every row's own V (`careful`), once.
 template <typename T, int HD, int QW>
-__global__ __launch_bounds__(QW * 64, 2) void prefix_tile_kernel(const T *__restrict__ q, T *__restrict__ out,
-                                                                 PrefixArgs a) {
+__global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) void prefix_tile_kernel(
+    const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
   typedef typename Mfma<T>::v8 v8;
   constexpr int RT = QW * 32;
   constexpr int KS = HD / 16;         // contraction steps of S over head_dim
@@ -340,7 +341,10 @@ __global__ __launch_bounds__(QW * 64, 2) void prefix_tile_kernel(const T *__rest
 
   floatx16_t o[NT];
   float mref, lsum;
-  for (bool careful = false;; careful = true) {
+  // the entries' walk; returns whether a block was seen whole by some rows of
+  // the wave only
+  auto walk = [&](auto careful_) __attribute__((always_inline)) {
+    constexpr bool careful = decltype(careful_)::value;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -456,11 +460,11 @@ __global__ __launch_bounds__(QW * 64, 2) void prefix_tile_kernel(const T *__rest
         }
       if (careful && partly) {
         // row by row, each with V of its own keys alone
-#pragma unroll 1
-        for (int i = 0; i < 32; ++i) {
-          const int lim = __builtin_amdgcn_readlane(end, i);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll 1
+          for (int i = 0; i < 32; ++i) {
+            const int lim = __builtin_amdgcn_readlane(end, i);
             floatx16_t acc = o[t];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -486,14 +490,15 @@ __global__ __launch_bounds__(QW * 64, 2) void prefix_tile_kernel(const T *__rest
           }
       }
     }
-    if (careful) break;
-    float z = 0.f;
+    return masked;
+  };
+  const bool masked = walk(std::false_type());
+  float z = 0.f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z = fmaf(o[t][r], 0.f, z);
-    if (!__syncthreads_or(masked && w.live && !(z == 0.f))) break;
-  }
+    for (int r = 0; r < 16; ++r) z = fmaf(o[t][r], 0.f, z);
+  if (__syncthreads_or(masked && w.live && !(z == 0.f))) walk(std::true_type());
   // o[t][r]: dim 32 t + 8 (r / 4) + 4 hh + r % 4 of this lane's row
   const float sum = half_swap_sum(lsum);
   const int64_t row = (int64_t)w.token * Hq + w.head;
@@ -519,7 +524,7 @@ __global__ __launch_bounds__(QW * 64, 2) void prefix_tile_kernel(const T *__rest
 // the waves' (m, l, o) meet in LDS.  Own items: the query heads of one row.
 // Shared items (a batch of few rows): packed rows.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void prefix_chunk_kernel(const T *__restrict__ q, PrefixArgs a) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void prefix_chunk_kernel(const T *__restrict__ q, PrefixArgs a) {
   typedef typename Mfma<T>::v8 v8;
   constexpr int KS = HD / 32, NT = HD / 16;
   constexpr float c2 = SCORE_C2<HD>;
@@ -758,7 +763,7 @@ static PrefixPlan prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, i
   a.G = n_heads / n_kv_heads;
   a.nP = ceil_div(std::min(prefix_len, max_ctx), KV_BLOCK);
   a.F = prefix_len / KV_BLOCK;
-  const int own = max_ctx > prefix_len ? ceil_div(max_ctx, KV_BLOCK) - a.F : 0;
+  int own = max_ctx > prefix_len ? ceil_div(max_ctx, KV_BLOCK) - a.F : 0;
   const int64_t packed = (int64_t)rows * a.G;
   PrefixPlan p{PK_SIMPLE, PK_SIMPLE, 64};
   if (half) {
@@ -778,6 +783,12 @@ static PrefixPlan prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, i
     a.splits = ceil_div(a.nP, a.sblk);
   }
   a.oblk = std::max(1, decode ? std::min(own, 4) : own);
+  if (p.own == PK_TILE && a.tiles * n_kv_heads >= 512) {
+    a.splits = 0;
+    a.tiles = 0;
+    own += a.nP;
+    a.oblk = own;
+  }
   a.osplits = ceil_div(own, a.oblk);
   a.parts = a.splits + a.osplits;
   a.direct = a.parts == 1 && (a.splits ? p.shared : p.own) == PK_TILE;
