@@ -24,6 +24,7 @@ struct PrefixArgs {
   int G;                      // query heads of a KV head
   int nP, F;                  // prefix entries, first own block
   int tiles, splits, sblk;    // shared items: row tiles, splits of the prefix, entries of a split
+  int shared_rows;            // 16-row tiles of the shared items that take rows_item (tiles is 0 then)
   int otiles, osplits, oblk;  // own items: row tiles, splits of the own entries, entries of a split
   int parts;                  // splits + osplits
   int direct;                 // one part, written to out by the tile kernel itself
@@ -241,8 +242,8 @@ __global__ __launch_bounds__(256) void prefix_attn_kernel(const T *__restrict__ 
 // infinite or NaN there.  A tile whose result is not finite is therefore
 // computed again with every row's own V (`careful`), once.
 template <typename T, int HD, int QW>
-__global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) void prefix_tile_kernel(
-    const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
+__device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict__ out, const PrefixArgs &a, int idx,
+                                          int g, char *lds) {
   typedef typename Mfma<T>::v8 v8;
   constexpr int RT = QW * 32;
   constexpr int KS = HD / 16;         // contraction steps of S over head_dim
@@ -252,12 +253,8 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   constexpr int STAGE = 2 * PB;
   constexpr int ND = PB / 1024 / QW;  // 1 KB copies per wave and block, K and V each
   constexpr float c2 = SCORE_C2<HD>;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
   const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads, P = a.b.prefix_len;
-  // KV head fastest: with 8 of them each XCD's L2 holds one head's blocks
-  int idx = blockIdx.x, j = -1, r0, e0, e1, part, most = INT_MAX, slot = -1;
-  const int g = idx % Hkv;
-  idx /= Hkv;
+  int j = -1, r0, e0, e1, part, most = INT_MAX, slot = -1;
   if (idx < a.tiles * a.splits) {
     part = idx % a.splits;
     r0 = idx / a.splits * RT;
@@ -278,11 +275,11 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l32 = lane & 31, hh = lane >> 5;
   const PrefixRow w = packed_row(a, j, r0 + wave * 32 + l32, g);
-  // rows that do not exist see everything (no mask on their account)
-  const int ctx = w.live ? w.ctx : INT_MAX;
+  // rows that do not exist or see nothing (zeros at the end, whatever is summed
+  // for them) ask for no mask
+  const int ctx = w.ctx ? w.ctx : INT_MAX;
   const int ctx_lo = (int)wave_min_u32((uint32_t)ctx);
-  const int ctx_hi = w.live ? w.ctx : 0;
-  const int ctx_top = (int)~wave_min_u32(~(uint32_t)ctx_hi);
+  const int ctx_top = (int)~wave_min_u32(~(uint32_t)w.ctx);
 
   v8 qb[KS];  // Q^T as the B operand: this lane's row, dims 16 k + 8 hh ..
   {
@@ -498,7 +495,15 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) z = fmaf(o[t][r], 0.f, z);
-  if (__syncthreads_or(masked && w.live && !(z == 0.f))) walk(std::true_type());
+  if (__syncthreads_or(masked && w.ctx && !(z == 0.f))) walk(std::true_type());
+  if (!w.ctx) {
+    mref = -INFINITY;
+    lsum = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  }
   // o[t][r]: dim 32 t + 8 (r / 4) + 4 hh + r % 4 of this lane's row
   const float sum = half_swap_sum(lsum);
   const int64_t row = (int64_t)w.token * Hq + w.head;
@@ -518,177 +523,278 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   }
 }
 
-// Few rows over four entries, on 16x16x32 MFMAs: up to 16 packed rows of a KV
-// head, a wave per entry, which requests its K fragments at once from the cache
-// and then its V fragments.  P goes through LDS into the A operand's layout;
-// the waves' (m, l, o) meet in LDS.  Own items: the query heads of one row.
-// Shared items (a batch of few rows): packed rows.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void prefix_chunk_kernel(const T *__restrict__ q, PrefixArgs a) {
+constexpr int TILE_LDS = 4 * 64 * HD * 2;  // two stages of K and V
+
+template <typename T, int HD, int QW>
+__global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) void prefix_tile_kernel(
+    const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[TILE_LDS<T, HD>];
+  // KV head fastest: with 8 of them each XCD's L2 holds one head's blocks
+  const int Hkv = a.b.kv.n_kv_heads;
+  tile_item<T, HD, QW>(q, out, a, blockIdx.x / Hkv, blockIdx.x % Hkv, lds);
+}
+
+// Few rows over a range of entries, on 16x16x32 MFMAs: up to 16 packed rows of a
+// KV head; wave w takes every fourth entry from the w-th on, its K and V
+// fragments straight from the cache in registers, the next entry's K requested
+// as soon as this one's is used, V likewise.  Online softmax per wave; P goes
+// through LDS into the A operand's layout; the waves' (m, l, o) meet in LDS at
+// the end.  Own items: the query heads of one row.  Shared items (batches of few
+// rows): packed rows.
+template <typename T, int HD>
+__device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixArgs &a, int idx, int g, char *lds) {
   typedef typename Mfma<T>::v8 v8;
-  constexpr int KS = HD / 32, NT = HD / 16;
+  constexpr int KS = HD / 32, NT = HD / 16, LP = 32 + 8;
   constexpr float c2 = SCORE_C2<HD>;
-  __shared__ T pls[4][16][64 + 8];
-  __shared__ float wm[4][16], wl[4][16];
-  __shared__ float wo[4][16][HD];
+  float(*wo)[16][HD] = (float(*)[16][HD])lds;                  // [4][16][HD]
+  float *wm = (float *)(lds + 4 * 16 * HD * 4), *wl = wm + 64;  // [4][16] each
+  T(*pls)[LP] = (T(*)[LP])(lds + 4 * 16 * HD * 4 + 512);       // [4 * 16][LP]
   const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads, P = a.b.prefix_len;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int r16 = lane & 15, quad = lane >> 4, kq = quad * 8;
-  int idx = blockIdx.x, j = -1, r0, e, part, slot = -1;
-  const int g = idx % Hkv;
-  idx /= Hkv;
-  if (idx < a.tiles * a.splits) {
-    part = idx % a.splits;
-    r0 = idx / a.splits * 16;
-    e = part * a.sblk + wave;
+  pls += wave * 16;
+  int j = -1, r0, e0, e1, part, slot = -1;
+  const int shared = a.shared_rows * a.splits;
+  if (idx < shared) {
+    r0 = idx % a.shared_rows * 16;
+    part = idx / a.shared_rows;
+    e0 = part * a.sblk;
+    e1 = min(a.nP, e0 + a.sblk);
   } else {
-    idx -= a.tiles * a.splits;
-    const int s = idx / a.otiles;  // all rows' first chunks, then their second ones: the grid ends with what few have
+    idx -= shared;
+    const int s = idx / a.otiles;  // all rows' first splits, then their second ones: the grid ends with what few have
     own_tile<16>(a, idx % a.otiles, j, r0);
     part = a.splits + s;
     slot = a.b.seq_slot[j];
-    e = a.nP + s * a.oblk + wave;
     const int ctx = row_ctx(a.b, j, 0);
-    if (ctx <= P || (a.F + s * a.oblk) * KV_BLOCK >= ctx) return;
+    e0 = a.nP + s * a.oblk;
+    e1 = min(e0 + a.oblk, ctx > P ? a.nP + (ctx + KV_BLOCK - 1) / KV_BLOCK - a.F : 0);
+    if (e0 >= e1) return;  // the join reads no such part
   }
-  const PrefixRow w = packed_row(a, j, r0 + r16, g);
   const bool own = j >= 0;
-  const bool live = w.live && (!own || r0 + r16 < a.G);
-  const int ctx_top = (int)~wave_min_u32(~(uint32_t)(live ? w.ctx : 0));
-  const int base = own ? (a.F + e - a.nP) * KV_BLOCK : e * KV_BLOCK;
-  const int lo = own ? max(0, P - base) : 0;
-  const int hi = min(KV_BLOCK, min(own ? INT_MAX : P, ctx_top) - base);
-  const PrefixEntry x = lo < hi ? prefix_entry(a, slot, e) : PrefixEntry{-1, 0, 0, 0};
-  const bool there = x.id >= 0;
-  const int64_t off = there ? ((int64_t)x.id * Hkv + g) * KV_BLOCK * HD : 0;
-  v8 qa[KS], kf[4][KS], vf[NT][2];
+  // Byte offsets of the entries' blocks (head included), -1 for none: lane i
+  // holds that of entry e0 + i (an item has at most 64).
+  int64_t off = -1;
+  if (e0 + lane < e1) {
+    const int id = prefix_entry(a, slot, e0 + lane).id;
+    if (id >= 0) off = ((int64_t)id * Hkv + g) * (KV_BLOCK * HD * 2);
+  }
+  const int off_lo = (int)off, off_hi = (int)(off >> 32);
+  const PrefixRow w = packed_row(a, j, r0 + r16, g);
+  const int ctx = w.live ? w.ctx : 0;
+  const int ctx_top = (int)~wave_min_u32(~(uint32_t)ctx);
+  // rows that see nothing get zeros at the end, whatever is summed for them
+  const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
+  // the wave's entries that have a block some row sees, and those of them that
+  // not every row sees whole (rows inside the prefix), which come after the rest
+  const int first = e0 + lane < a.nP ? (e0 + lane) * KV_BLOCK : (a.F + e0 + lane - a.nP) * KV_BLOCK;
+  const int last = own ? INT_MAX : P;
+  const uint64_t mine = 0x1111111111111111ull << wave;
+  const uint64_t seen = __ballot(off >= 0 && first < ctx_top) & mine;
+  const uint64_t mixed = own ? 0 : seen & __ballot(min(first + KV_BLOCK, last) > ctx_lo);
+  // K and V of 32 keys: keys 16 nt + r16 of the half, dims 32 k + kq .. of K;
+  // dim 16 nt + r16, keys kq .. of V
+  v8 kf[2][KS], vf[NT];
+  const uint32_t klane = (r16 * HD + kq) * 2, vlane = (r16 * KV_BLOCK + kq) * 2;
+  int64_t at;
+  auto place = [&](int i, int h) __attribute__((always_inline)) {  // half h of entry e0 + i
+    at = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, i) << 32) |
+                   (uint32_t)__builtin_amdgcn_readlane(off_lo, i));
+    return __builtin_amdgcn_readlane(first, i) + h * 32;
+  };
+  auto load_k = [&](int h) __attribute__((always_inline)) {
+    const char *kb = (const char *)a.b.kv.k + at + h * 32 * HD * 2;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[nt][k] = load8<T>((const T *)(kb + (nt * 16 * HD + k * 32) * 2 + klane));
+  };
+  auto load_v = [&](int h) __attribute__((always_inline)) {
+    const char *vb = (const char *)a.b.kv.v + at + h * 32 * 2;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) vf[nt] = load8<T>((const T *)(vb + nt * 16 * KV_BLOCK * 2 + vlane));
+  };
+  v8 qa[KS];
   const T *qrow = q + ((int64_t)w.token * Hq + w.head) * HD;
 #pragma unroll
-  for (int k = 0; k < KS; ++k) qa[k] = live ? load8<T>(qrow + k * 32 + kq) : zero8<T>();
-  floatx4_t sacc[4], oacc[NT];
+  for (int k = 0; k < KS; ++k) qa[k] = load8<T>(qrow + k * 32 + kq);
+  // row 4 quad + i: running maximum (raw scores) and this lane's share of the
+  // sum; o[nt][i]: its dim nt * 16 + r16
   float mx[4], sm[4];
+  int rctx[4];
+  floatx4_t o[NT], s[2];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) oacc[nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  for (int nt = 0; nt < NT; ++nt) o[nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) mx[i] = -INFINITY, sm[i] = 0.f;
-  if (there) {
-    const T *kb = (const T *)a.b.kv.k + off, *vb = (const T *)a.b.kv.v + off;
+  for (int i = 0; i < 4; ++i) mx[i] = -INFINITY, sm[i] = 0.f, rctx[i] = __shfl(ctx, 4 * quad + i, 64);
+  auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt)
+    for (int nt = 0; nt < 2; ++nt) s[nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) kf[nt][k] = load8<T>(kb + (nt * 16 + r16) * HD + k * 32 + kq);
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
-    for (int nt = 0; nt < 4; ++nt) {
-      sacc[nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < KS; ++k) sacc[nt] = Mfma<T>::m16(qa[k], kf[nt][k], sacc[nt]);
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) vf[nt][k] = load8<T>(vb + (nt * 16 + r16) * KV_BLOCK + k * 32 + kq);
-    // sacc[nt][i]: row 4 quad + i, key nt * 16 + r16
+      for (int nt = 0; nt < 2; ++nt) s[nt] = Mfma<T>::m16(qa[k], kf[nt][k], s[nt]);
+  };
+  // keys [lo, hi) of the 32 at `base` are there
+  auto bounds = [&](int base, int &lo, int &hi) __attribute__((always_inline)) {
+    lo = own ? max(0, P - base) : 0;
+    hi = min(32, min(last, ctx_top) - base);
+  };
+  // s[nt][i]: row 4 quad + i, key nt * 16 + r16, to weights in LDS
+  auto weights = [&](int base, int lo, int hi) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int end = min(hi, __shfl(live ? w.ctx : 0, 4 * quad + i, 64) - base);
-      float v = -INFINITY;
+      const int end = min(hi, rctx[i] - base);
 #pragma unroll
-      for (int nt = 0; nt < 4; ++nt) {
+      for (int nt = 0; nt < 2; ++nt) {
         const int key = nt * 16 + r16;
-        sacc[nt][i] = key >= lo && key < end ? sacc[nt][i] : -INFINITY;
-        v = fmaxf(v, sacc[nt][i]);
+        s[nt][i] = key >= lo && key < end ? s[nt][i] : -INFINITY;
       }
-      v = row16_max(v);
-      mx[i] = v;
+      const float v = fmaxf(mx[i], row16_max(fmaxf(s[0][i], s[1][i])));
       const float m0 = v == -INFINITY ? 0.f : v;
-      float t = 0.f;
+      const float corr = mx[i] == v ? 1.f : __builtin_amdgcn_exp2f((mx[i] - v) * c2);
+      mx[i] = v;
+      sm[i] *= corr;
 #pragma unroll
-      for (int nt = 0; nt < 4; ++nt) {
-        const float p = __builtin_amdgcn_exp2f((sacc[nt][i] - m0) * c2);
-        t += p;
-        pls[wave][4 * quad + i][nt * 16 + r16] = Act<T>::st(p);
+      for (int nt = 0; nt < 2; ++nt) {
+        const float p = __builtin_amdgcn_exp2f((s[nt][i] - m0) * c2);
+        sm[i] += p;
+        pls[4 * quad + i][nt * 16 + r16] = Act<T>::st(p);
       }
-      sm[i] = row16_sum(t);
-    }
-  }
-  __syncthreads();
-  if (there) {
-    v8 pa[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) pa[k] = load8<T>(&pls[wave][r16][k * 32 + kq]);
-    // keys [from, to) of the V fragments, others 0 (stale entries hold anything)
-    auto keep = [&](v8 f, int k, int from, int to) __attribute__((always_inline)) {
-      u32x4_tt m = __builtin_bit_cast(u32x4_tt, f);
+      for (int nt = 0; nt < NT; ++nt) o[nt][i] *= corr;
+    }
+  };
+  uint64_t left = seen & ~mixed;
+  if (left) {
+    int i = __builtin_ctzll(left), h = 0, base = place(i, 0);
+    load_k(0);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(0);
+    __builtin_amdgcn_sched_barrier(0);
+    // One half; with `more`, the next one's K and V are requested as soon as
+    // their registers are free.  The last half has code of its own: where loads
+    // may or may not have been issued, the compiler waits for all of them.
+    auto step = [&](auto more_) __attribute__((always_inline)) {
+      constexpr bool more = decltype(more_)::value;
+      int lo, hi, nbase = 0;
+      bounds(base, lo, hi);
+      scores();
+      if constexpr (more) {
+        h ^= 1;
+        if (!h) {
+          left &= left - 1;
+          i = __builtin_ctzll(left);
+        }
+        nbase = place(i, h);
+        __builtin_amdgcn_sched_barrier(0);
+        load_k(h);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      weights(base, lo, hi);
+      // V outside [lo, hi) is stale and may hold anything, and 0 * NaN is not 0
+      u32x4_tt keep;
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        const int key = k * 32 + kq + 2 * y;
-        m[y] &= (key >= from && key < to ? 0xFFFFu : 0u) | (key + 1 >= from && key + 1 < to ? 0xFFFF0000u : 0u);
+        const int key = kq + 2 * y;
+        keep[y] = (key >= lo && key < hi ? 0xFFFFu : 0u) | (key + 1 >= lo && key + 1 < hi ? 0xFFFF0000u : 0u);
       }
-      return __builtin_bit_cast(v8, m);
-    };
-    if (lo > 0 || hi < KV_BLOCK) {
+      const v8 pa = load8<T>(&pls[r16][kq]);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int k = 0; k < 2; ++k) vf[nt][k] = keep(vf[nt][k], k, lo, hi);
-    }
-    float z = 0.f;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) oacc[nt] = Mfma<T>::m16(pa[k], vf[nt][k], oacc[nt]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z = fmaf(oacc[nt][i], 0.f, z);
-    }
-    if (!own && __any(!(z == 0.f))) {
-      // V is not finite at a key that perhaps not every row sees: row by row
+        o[nt] = Mfma<T>::m16(pa, __builtin_bit_cast(v8, __builtin_bit_cast(u32x4_tt, vf[nt]) & keep), o[nt]);
+      if constexpr (more) {
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(h);
+        __builtin_amdgcn_sched_barrier(0);
+        base = nbase;
+      }
+    };
+    while (h == 0 || (left & (left - 1))) step(std::true_type());
+    step(std::false_type());
+  }
+  // a key at a time, each added to the rows that see it (a weight of 0 does not
+  // cancel V that is infinite or NaN)
+  for (left = mixed; left; left &= left - 1)
 #pragma unroll 1
-      for (int rr = 0; rr < 16; ++rr) {
-        const int end = min(hi, __builtin_amdgcn_readlane(live ? w.ctx : 0, rr) - base);
+    for (int h = 0; h < 2; ++h) {
+      int lo, hi;
+      const int base = place(__builtin_ctzll(left), h);
+      bounds(base, lo, hi);
+      load_k(h);
+      scores();
+      weights(base, lo, hi);
+      const T *vb = (const T *)((const char *)a.b.kv.v + at) + r16 * KV_BLOCK + h * 32;
+#pragma unroll 1
+      for (int key = 0; key < hi; ++key) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          floatx4_t acc = floatx4_t{0.f, 0.f, 0.f, 0.f};
+          const float v = Act<T>::ld(vb[nt * 16 * KV_BLOCK + key]);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) acc = Mfma<T>::m16(pa[k], keep(vf[nt][k], k, 0, end), acc);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) oacc[nt][i] = 4 * quad + i == rr ? acc[i] : oacc[nt][i];
+          for (int y = 0; y < 4; ++y)
+            if (base + key < rctx[y]) o[nt][y] = fmaf(Act<T>::ld(pls[4 * quad + y][key]), v, o[nt][y]);
         }
       }
     }
-  }
-  if (r16 == 0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      wm[wave][4 * quad + i] = mx[i];
-      wl[wave][4 * quad + i] = sm[i];
-    }
-  }
   const int nrows = own ? min(16, a.G - r0) : 16;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (4 * quad + i < nrows) {
+    const int r = 4 * quad + i;
+    const float t = row16_sum(sm[i]);
+    if (r16 == 0) wm[wave * 16 + r] = mx[i], wl[wave * 16 + r] = t;
+    if (r < nrows) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) wo[wave][4 * quad + i][nt * 16 + r16] = oacc[nt][i];
+      for (int nt = 0; nt < NT; ++nt) wo[wave][r][nt * 16 + r16] = o[nt][i];
     }
   }
   __syncthreads();
   // a wave a row: its lanes over the dims
   for (int r = wave; r < nrows; r += 4) {
     const int token = __builtin_amdgcn_readlane(w.token, r), h = __builtin_amdgcn_readlane(w.head, r);
-    if (!__builtin_amdgcn_readlane((int)live, r)) continue;
+    if (!__builtin_amdgcn_readlane((int)w.live, r)) continue;
     float M = -INFINITY, f[4], L = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) M = fmaxf(M, wm[k][r]);
+    for (int k = 0; k < 4; ++k) M = fmaxf(M, wm[k * 16 + r]);
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      f[k] = wm[k][r] == M ? 1.f : __builtin_amdgcn_exp2f((wm[k][r] - M) * c2);
-      L += f[k] * wl[k][r];
+      f[k] = wm[k * 16 + r] == M ? 1.f : __builtin_amdgcn_exp2f((wm[k * 16 + r] - M) * c2);
+      L += f[k] * wl[k * 16 + r];
     }
     const int64_t rec = ((int64_t)token * Hq + h) * a.parts + part;
+    const bool none = __builtin_amdgcn_readlane(ctx, r) == 0;
     for (int d = lane; d < HD; d += 64)
-      a.po[rec * HD + d] = (f[0] * wo[0][r][d] + f[1] * wo[1][r][d]) + (f[2] * wo[2][r][d] + f[3] * wo[3][r][d]);
-    if (lane == 0) *(float2 *)(a.pml + rec * 2) = make_float2(M, L);
+      a.po[rec * HD + d] =
+          none ? 0.f : (f[0] * wo[0][r][d] + f[1] * wo[1][r][d]) + (f[2] * wo[2][r][d] + f[3] * wo[3][r][d]);
+    if (lane == 0) *(float2 *)(a.pml + rec * 2) = none ? make_float2(-INFINITY, 0.f) : make_float2(M, L);
   }
+}
+
+template <typename T, int HD>
+constexpr int ROWS_LDS = 4 * 16 * HD * 4 + 512 + 4 * 16 * 40 * 2;
+
+// Decode: shared items of 128 rows, which the matrix cores bound, and items of
+// few rows (the rows' own, and the shared ones of small batches), which memory
+// bounds, dealt out in turn so that a CU has some of each.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_decode_kernel(
+    const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[std::max(TILE_LDS<T, HD>, ROWS_LDS<T, HD>)];
+  const int Hkv = a.b.kv.n_kv_heads, g = blockIdx.x % Hkv;
+  int i = blockIdx.x / Hkv;
+  const int tiles = a.tiles * a.splits, rows = a.shared_rows * a.splits + a.otiles * a.osplits;
+  const int both = min(tiles, rows);
+  bool tile = tiles > rows;
+  if (i < 2 * both) {
+    tile = i % 2 == 0;
+    i /= 2;
+  } else {
+    i -= both;
+  }
+  if (tile)
+    tile_item<T, HD, 4>(q, out, a, i, g, lds);
+  else
+    rows_item<T, HD>(q, a, i, g, lds);
 }
 
 // Joins the parts of a (token, head), a wave each: its lanes hold the parts'
@@ -748,51 +854,39 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
 
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-enum PrefixKernel : int { PK_SIMPLE, PK_CHUNK, PK_TILE };
-
-// The shared items' row tile and kernel, the splits of both parts.  16-bit
-// types: batches of at most 16 packed rows take the chunk kernel (the rows of a
-// KV head are one tile of it), larger ones the tile kernel; a decode batch's own
-// parts take the chunk kernel.
-struct PrefixPlan {
-  int shared, own;  // kernels
-  int rt;           // rows of a shared tile
-};
-static PrefixPlan prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_heads, int n_kv_heads,
-                              int prefix_len, int max_ctx) {
+// Row tiles and splits.
+static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_heads, int n_kv_heads, int prefix_len,
+                        int max_ctx) {
   a.G = n_heads / n_kv_heads;
   a.nP = ceil_div(std::min(prefix_len, max_ctx), KV_BLOCK);
   a.F = prefix_len / KV_BLOCK;
   int own = max_ctx > prefix_len ? ceil_div(max_ctx, KV_BLOCK) - a.F : 0;
   const int64_t packed = (int64_t)rows * a.G;
-  PrefixPlan p{PK_SIMPLE, PK_SIMPLE, 64};
-  if (half) {
-    p.shared = decode && packed <= 16 ? PK_CHUNK : PK_TILE;
-    p.own = decode ? PK_CHUNK : PK_TILE;
-    p.rt = p.shared == PK_CHUNK ? 16 : !decode || packed > 64 ? 128 : packed > 32 ? 64 : 32;
-  }
-  a.tiles = a.nP ? ceil_div(packed, p.rt) : 0;
-  a.splits = a.sblk = 0;
+  const bool few = half && decode && packed <= 64;
+  const int rt = half ? few ? 16 : 128 : 64;
+  const int tiles = a.nP ? ceil_div(packed, rt) : 0;
+  a.tiles = few ? 0 : tiles;
+  a.shared_rows = few ? tiles : 0;
   if (a.nP) {
-    if (p.shared == PK_CHUNK) {
-      a.sblk = 4;
-    } else {
-      const int want = std::max(1, 512 / std::max(1, a.tiles * n_kv_heads));
-      a.sblk = ceil_div(a.nP, std::min(want, ceil_div(a.nP, 4)));
-    }
+    const int want = std::max(1, 512 / std::max(1, tiles * n_kv_heads));
+    a.sblk = ceil_div(a.nP, std::min(want, ceil_div(a.nP, 4)));
+    if (few) a.sblk = std::min(a.sblk, 64);
     a.splits = ceil_div(a.nP, a.sblk);
   }
-  a.oblk = std::max(1, decode ? std::min(own, 4) : own);
-  if (p.own == PK_TILE && a.tiles * n_kv_heads >= 512) {
-    a.splits = 0;
-    a.tiles = 0;
+  a.oblk = std::max(1, own);
+  if (decode) {
+    const int want = std::max(1, 512 / (int)std::min((int64_t)rows * n_kv_heads, (int64_t)512));
+    a.oblk = std::max(1, ceil_div(own, std::min(want, std::max(1, ceil_div(own, 4)))));
+    if (half) a.oblk = std::min(a.oblk, 64);
+  }
+  if (half && !decode && (int64_t)tiles * n_kv_heads >= 512) {
+    a.splits = a.tiles = 0;
     own += a.nP;
     a.oblk = own;
   }
   a.osplits = ceil_div(own, a.oblk);
   a.parts = a.splits + a.osplits;
-  a.direct = a.parts == 1 && (a.splits ? p.shared : p.own) == PK_TILE;
-  return p;
+  a.direct = a.parts == 1 && half && !few && (!decode || a.splits);
 }
 
 size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_heads, int head_dim, int prefix_len,
@@ -811,39 +905,24 @@ static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   PrefixArgs a{};
   a.b = b;
   const int Hkv = b.kv.n_kv_heads;
+  constexpr bool half = sizeof(T) == 2;
   const bool decode = !b.seq_start;
-  const PrefixPlan p =
-      prefix_plan(a, decode, sizeof(T) == 2, b.rows, b.n_heads, Hkv, b.prefix_len, b.max_ctx);
+  prefix_plan(a, decode, half, b.rows, b.n_heads, Hkv, b.prefix_len, b.max_ctx);
   a.po = ws;
   a.pml = ws + (size_t)b.rows * b.n_heads * a.parts * HD;
-  const int rto = p.own == PK_CHUNK ? 16 : p.own == PK_TILE ? 128 : 64;
+  const int rto = !half ? 64 : decode ? 16 : 128;
   a.otiles = decode ? b.rows * ceil_div(a.G, rto)
                     : (int)std::min((int64_t)b.n_seq * ceil_div((int64_t)std::min(b.max_new, b.rows) * a.G, rto),
                                     (int64_t)b.rows * a.G / rto + b.n_seq);
-  const int64_t shared = (int64_t)a.tiles * a.splits * Hkv, own = (int64_t)a.otiles * a.osplits * Hkv;
+  const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.otiles * a.osplits) * Hkv;
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
-  if constexpr (sizeof(T) == 2) {
-    const auto tile = [&](int64_t n, const PrefixArgs &x) {
-      if (p.rt == 32)
-        prefix_tile_kernel<T, HD, 1><<<grid(n), 64, 0, s>>>(q, out, x);
-      else if (p.rt == 64)
-        prefix_tile_kernel<T, HD, 2><<<grid(n), 128, 0, s>>>(q, out, x);
-      else
-        prefix_tile_kernel<T, HD, 4><<<grid(n), 256, 0, s>>>(q, out, x);
-    };
-    if (p.shared == p.own) {
-      if (p.own == PK_TILE)
-        tile(shared + own, a);
-      else
-        prefix_chunk_kernel<T, HD><<<grid(shared + own), 256, 0, s>>>(q, a);
-    } else {
-      if (shared) tile(shared, a);
-      PrefixArgs x = a;
-      x.tiles = 0;  // own items alone
-      if (own) prefix_chunk_kernel<T, HD><<<grid(own), 256, 0, s>>>(q, x);
-    }
+  if constexpr (half) {
+    if (decode)
+      prefix_decode_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
+    else
+      prefix_tile_kernel<T, HD, 4><<<grid(items), 256, 0, s>>>(q, out, a);
   } else {
-    prefix_attn_kernel<T, HD><<<grid(shared + own), 256, 0, s>>>(q, a);
+    prefix_attn_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, a);
   }
   if (!a.direct)
     prefix_join_kernel<T, HD><<<grid(ceil_div((int64_t)b.rows * b.n_heads, 4)), 256, 0, s>>>(out, a);
