@@ -19,6 +19,20 @@
 
 namespace lp {
 
+// n / d for n >= 0 with m = floor(2^32 / d) (all ones for d = 1): n m / 2^32 is
+// at most one short, which the remainder shows.
+struct Divisor {
+  uint32_t d, m;
+};
+__device__ __forceinline__ int div_by(int n, Divisor x) {
+  const uint32_t k = __umulhi((uint32_t)n, x.m);
+  return (int)(k + ((uint32_t)n - k * x.d >= x.d ? 1 : 0));
+}
+static Divisor divisor(int d) {
+  const uint32_t u = (uint32_t)std::max(d, 1);
+  return {u, u > 1 ? (uint32_t)((1ull << 32) / u) : 0xFFFFFFFFu};
+}
+
 struct PrefixArgs {
   PrefixBatch b;
   int G;                      // query heads of a KV head
@@ -28,6 +42,7 @@ struct PrefixArgs {
   int otiles, osplits, oblk;  // own items: row tiles, splits of the own entries, entries of a split
   int parts;                  // splits + osplits
   int direct;                 // one part, written to out by the tile kernel itself
+  Divisor by_g, by_hkv, by_splits, by_osplits, by_otiles, by_shared, by_per;
   float *po, *pml;            // partial o [rows][n_heads][parts][hd], (m, l) [rows][n_heads][parts][2]
 };
 // A part's m is the largest score before the scale 1/sqrt(hd), its weights are
@@ -36,9 +51,15 @@ template <int HD>
 constexpr float SCORE_C2 = (HD == 64 ? 0.125f : 0.08838834764831845f) * 1.44269504088896341f;
 
 struct PrefixRow {
-  int token, head, ctx;  // ctx: keys the row sees, 0 for a row that does not exist or sees none
-  bool live;             // the row exists: its result (or partial) is written
+  int token, head, t;  // t: the token's place in its sequence, or in the batch
 };
+
+// Row l of the packed rows from r0 (uniform) on: of all tokens, or of a sequence
+// whose first token is `start`.
+__device__ __forceinline__ PrefixRow packed_row(const PrefixArgs &a, int start, int r0, int l, int g) {
+  const int t0 = div_by(r0, a.by_g), x = r0 - t0 * a.G + l, dt = div_by(x, a.by_g);
+  return PrefixRow{start + t0 + dt, g * a.G + x - dt * a.G, t0 + dt};
+}
 
 // Sequence j's first row and row count, inside the batch's rows.
 __device__ __forceinline__ void seq_rows(const PrefixBatch &b, int j, int &start, int &n) {
@@ -59,33 +80,29 @@ __device__ __forceinline__ int row_ctx(const PrefixBatch &b, int j, int i) {
   return p0 < 0 ? 0 : (int)min(ctx, (int64_t)b.max_ctx);
 }
 
-// Packed row r of all tokens (j < 0), or of sequence j alone.
-__device__ __forceinline__ PrefixRow packed_row(const PrefixArgs &a, int j, int r, int g) {
-  PrefixRow w{0, g * a.G + r % a.G, 0, false};
-  int t = r / a.G, start, n;
-  if (j < 0) {
-    if (t >= a.b.rows) return w;
-    if (!a.b.seq_start) {
-      j = t;
-    } else {  // the last sequence that starts at or before the token
-      int lo = 0, hi = a.b.n_seq - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.b.seq_start[mid] <= t) lo = mid;
-        else hi = mid - 1;
-      }
-      j = lo;
-    }
-    seq_rows(a.b, j, start, n);
-    t -= start;
-  } else {
-    seq_rows(a.b, j, start, n);
+// Keys that a packed row sees, -1 if the row does not exist: token t of sequence
+// j (which has n rows), or with j < 0 token t of the batch.
+__device__ __forceinline__ int packed_ctx(const PrefixArgs &a, int j, int t, int n) {
+  if (j >= 0) return t < n && t < a.b.max_new ? row_ctx(a.b, j, t) : -1;
+  if (!a.b.seq_start) return t < a.b.rows ? row_ctx(a.b, t, 0) : -1;
+  // the last sequence that starts at or before the token, 64 sequences at a time
+  const int lane = threadIdx.x & 63;
+  int at = -1;
+  for (int base = 0; base < a.b.n_seq; base += 64) {
+    const int s = base + lane < a.b.n_seq ? a.b.seq_start[base + lane] : INT_MAX;
+    if (!__any(__builtin_amdgcn_readlane(s, 0) <= t)) break;
+    int k = -1;
+#pragma unroll
+    for (int step = 32; step; step >>= 1)
+      if (__shfl(s, k + step, 64) <= t) k += step;
+    if (k == 62 && __shfl(s, 63, 64) <= t) k = 63;
+    if (k >= 0) at = base + k;
   }
-  if (t < 0 || t >= n || t >= a.b.max_new) return w;
-  w.token = start + t;
-  w.ctx = row_ctx(a.b, j, t);
-  w.live = true;
-  return w;
+  if (at < 0 || t >= a.b.rows) return -1;
+  int start;
+  seq_rows(a.b, at, start, n);
+  t -= start;
+  return t >= 0 && t < n && t < a.b.max_new ? row_ctx(a.b, at, t) : -1;
 }
 
 // Own tile u of RT packed rows: sequence by sequence, each with as many tiles as
@@ -95,9 +112,8 @@ template <int RT>
 __device__ __forceinline__ bool own_tile(const PrefixArgs &a, int u, int &j, int &r0) {
   const int lane = threadIdx.x & 63;
   if (!a.b.seq_start) {  // one row a sequence
-    const int per = (a.G + RT - 1) / RT;
-    j = u / per;
-    r0 = u % per * RT;
+    j = div_by(u, a.by_per);
+    r0 = (u - j * (int)a.by_per.d) * RT;
     return j < a.b.n_seq;
   }
   for (int base = 0; base < a.b.n_seq; base += 64) {
@@ -149,7 +165,7 @@ __global__ __launch_bounds__(256) void prefix_attn_kernel(const T *__restrict__ 
   __shared__ T ks[64][HD + 2];
   __shared__ T vs[64][HD + 2];
   const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads;
-  int idx = blockIdx.x, j = -1, r0, e0, e1, part;
+  int idx = blockIdx.x, j = -1, r0, e0, e1, part, start = 0, n = 0;
   const int g = idx % Hkv;
   idx /= Hkv;
   if (idx < a.tiles * a.splits) {
@@ -161,24 +177,27 @@ __global__ __launch_bounds__(256) void prefix_attn_kernel(const T *__restrict__ 
     idx -= a.tiles * a.splits;
     const int s = idx % a.osplits;
     if (!own_tile<64>(a, idx / a.osplits, j, r0)) return;
+    seq_rows(a.b, j, start, n);
     part = a.splits + s;
     e0 = a.nP + s * a.oblk;
     e1 = e0 + a.oblk;
   }
   const int slot = j < 0 ? -1 : a.b.seq_slot[j];
   const int qi = threadIdx.x >> 2, qq = threadIdx.x & 3;
-  const PrefixRow w = packed_row(a, j, r0 + qi, g);
+  const PrefixRow w = packed_row(a, start, r0, qi, g);
+  const int seen = packed_ctx(a, j, w.t, n), ctx = max(seen, 0);
+  const bool live = seen >= 0;
   __shared__ int top;  // the largest context of the tile
   if (threadIdx.x == 0) top = 0;
   __syncthreads();
-  atomicMax(&top, w.ctx);
+  atomicMax(&top, ctx);
   __syncthreads();
   const int most = top;
   float qv[Q4], o[Q4];
   const T *qr = q + ((int64_t)w.token * Hq + w.head) * HD + qq * Q4;
 #pragma unroll
   for (int t = 0; t < Q4; ++t) {
-    qv[t] = w.live ? Act<T>::ld(qr[t]) : 0.f;
+    qv[t] = live ? Act<T>::ld(qr[t]) : 0.f;
     o[t] = 0.f;
   }
   float mx = -INFINITY, l = 0.f;
@@ -203,7 +222,7 @@ __global__ __launch_bounds__(256) void prefix_attn_kernel(const T *__restrict__ 
       for (int t = 0; t < Q4; ++t) sc += qv[t] * Act<T>::ld(ks[p][qq * Q4 + t]);
       sc += __shfl_xor(sc, 1, 64);
       sc += __shfl_xor(sc, 2, 64);
-      if (x.base + p >= w.ctx) continue;  // uniform across the 4 threads of a row
+      if (x.base + p >= ctx) continue;  // uniform across the 4 threads of a row
       const float mn = fmaxf(mx, sc);
       const float corr = mx == mn ? 1.f : __builtin_amdgcn_exp2f((mx - mn) * c2);
       const float pe = mn == -INFINITY && sc == sc ? 0.f : __builtin_amdgcn_exp2f((sc - mn) * c2);
@@ -213,7 +232,7 @@ __global__ __launch_bounds__(256) void prefix_attn_kernel(const T *__restrict__ 
       mx = mn;
     }
   }
-  if (w.live) {
+  if (live) {
     const int64_t rec = ((int64_t)w.token * Hq + w.head) * a.parts + part;
     float *dst = a.po + rec * HD + qq * Q4;
 #pragma unroll
@@ -254,36 +273,32 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
   constexpr int ND = PB / 1024 / QW;  // 1 KB copies per wave and block, K and V each
   constexpr float c2 = SCORE_C2<HD>;
   const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads, P = a.b.prefix_len;
-  int j = -1, r0, e0, e1, part, most = INT_MAX, slot = -1;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int l32 = lane & 31, hh = lane >> 5;
+  int j = -1, r0, e0, e1, part, most = INT_MAX, slot = -1, start = 0, n = a.b.rows;
   if (idx < a.tiles * a.splits) {
-    part = idx % a.splits;
-    r0 = idx / a.splits * RT;
+    const int tile = div_by(idx, a.by_splits);
+    part = idx - tile * a.splits;
+    r0 = tile * RT;
     e0 = part * a.sblk;
     e1 = min(a.nP, e0 + a.sblk);
   } else {
     idx -= a.tiles * a.splits;
-    const int s = idx % a.osplits;
-    if (!own_tile<RT>(a, idx / a.osplits, j, r0)) return;
+    const int u = div_by(idx, a.by_osplits), s = idx - u * a.osplits;
+    if (!own_tile<RT>(a, u, j, r0)) return;
     part = a.splits + s;
     slot = a.b.seq_slot[j];
-    int start, n;
     seq_rows(a.b, j, start, n);
-    most = row_ctx(a.b, j, min((r0 + RT - 1) / a.G, n - 1));  // the last row sees most
+    most = row_ctx(a.b, j, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
     e0 = (a.splits ? a.nP : 0) + s * a.oblk;
     e1 = min(e0 + a.oblk, most > P ? a.nP + (most + KV_BLOCK - 1) / KV_BLOCK - a.F : (most + KV_BLOCK - 1) / KV_BLOCK);
   }
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int l32 = lane & 31, hh = lane >> 5;
-  const PrefixRow w = packed_row(a, j, r0 + wave * 32 + l32, g);
-  // rows that do not exist or see nothing (zeros at the end, whatever is summed
-  // for them) ask for no mask
-  const int ctx = w.ctx ? w.ctx : INT_MAX;
-  const int ctx_lo = (int)wave_min_u32((uint32_t)ctx);
-  const int ctx_top = (int)~wave_min_u32(~(uint32_t)w.ctx);
-
+  // What the first copies wait for is requested first, with the rows' q: a
+  // walk of few blocks is one memory round trip after the other.
+  const PrefixRow w = packed_row(a, start, r0, wave * 32 + l32, g);
   v8 qb[KS];  // Q^T as the B operand: this lane's row, dims 16 k + 8 hh ..
   {
-    const T *qr = q + ((int64_t)w.token * Hq + w.head) * HD + hh * 8;
+    const T *qr = q + ((int64_t)(w.t < n ? w.token : 0) * Hq + w.head) * HD + hh * 8;
 #pragma unroll
     for (int k = 0; k < KS; ++k) qb[k] = load8<T>(qr + k * 16);
   }
@@ -310,7 +325,7 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
   uint32_t ko[ND], vo[ND];  // byte offsets of this lane's pieces inside a block
 #pragma unroll
   for (int c = 0; c < ND; ++c) {
-    const int n = wave * ND + c, kr = n * KR + lane / CK, vr = n * 8 + (lane >> 3);
+    const int m = wave * ND + c, kr = m * KR + lane / CK, vr = m * 8 + (lane >> 3);
     ko[c] = kr * HD * 2 + ((lane % CK) ^ swz(kr)) * 16;
     vo[c] = vr * KV_BLOCK * 2 + ((lane & 7) ^ ((vr >> 1) & 7)) * 16;
   }
@@ -332,6 +347,22 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
       dma16s((const char *)a.b.kv.v + off, vo[c], st + PB + c * 1024);
     }
   };
+  auto begin = [&]() __attribute__((always_inline)) {  // the first two blocks
+    win = e0;
+    if (e0 < e1) {
+      window();
+      issue(e0);
+      if (e0 + 1 < e1) issue(e0 + 1);
+    }
+  };
+  begin();
+  const int seen = packed_ctx(a, j, w.t, n), wctx = max(seen, 0);
+  const bool live = seen >= 0;
+  // rows that do not exist or see nothing (zeros at the end, whatever is summed
+  // for them) ask for no mask
+  const int ctx = wctx ? wctx : INT_MAX;
+  const int ctx_lo = (int)wave_min_u32((uint32_t)ctx);
+  const int ctx_top = (int)~wave_min_u32(~(uint32_t)wctx);
   const int krow = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
   const int kfb = krow * HD * 2, kfx = (hh ^ swz(krow)) << 4;
   const int vfb = l32 * KV_BLOCK * 2, vfx = (hh ^ ((l32 >> 1) & 7)) << 4;
@@ -352,11 +383,7 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
     lsum = 0.f;
     bool large = false;   // wave-uniform: a row's |mc| is past PFA_LARGE
     bool masked = false;  // wave-uniform: a block that only some rows see whole
-    if (e0 < e1) {
-      win = e0;
-      window();
-      issue(e0);
-    }
+    if constexpr (careful) begin();
     for (int e = e0; e < e1; ++e) {
       const bool mine = e < a.nP;
       const int base = mine ? e * KV_BLOCK : (a.F + e - a.nP) * KV_BLOCK;
@@ -387,7 +414,7 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
         }
         __syncthreads();
       }
-      if (e + 1 < e1) issue(e + 1);
+      if (e > e0 && e + 1 < e1) issue(e + 1);
       if (!there || base + lo >= ctx_top) continue;  // no block, or wholly past this wave's rows
       floatx16_t s[2];
 #pragma unroll
@@ -403,8 +430,8 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
       // s[t][r]: key 32 t + 16 (r / 8) + 8 hh + r % 8 of the block
       const bool partly = lo > 0 || base + hi > ctx_lo || hi < KV_BLOCK;
       const int end = min(hi, max(ctx - base, 0));  // the row's keys: [lo, end)
+      if (base + hi > ctx_lo) masked = true;
       if (partly) {
-        masked = true;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -489,14 +516,23 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
     }
     return masked;
   };
-  const bool masked = walk(std::false_type());
-  float z = 0.f;
+  int *again = (int *)(lds + 2 * STAGE);
+  if (threadIdx.x == 0) *again = 0;  // before the walk's first barrier, or the one below
+  if (e0 >= e1) __syncthreads();
+  if (walk(std::false_type())) {
+    float z[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) z = fmaf(o[t][r], 0.f, z);
-  if (__syncthreads_or(masked && w.ctx && !(z == 0.f))) walk(std::true_type());
-  if (!w.ctx) {
+      for (int r = 0; r < 16; ++r) z[r & 3] = fmaf(o[t][r], 0.f, z[r & 3]);
+    if (wctx && !(z[0] + z[1] + (z[2] + z[3]) == 0.f)) *again = 1;
+  }
+  __syncthreads();  // the last block is used by now: LDS is free below
+  if (*again) {
+    walk(std::true_type());
+    __syncthreads();
+  }
+  if (!wctx) {
     mref = -INFINITY;
     lsum = 0.f;
 #pragma unroll
@@ -510,29 +546,46 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
   if (a.direct) {
     const float inv = sum == 0.f ? 0.f : 1.0f / sum;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) store_o32(out + row * HD + t * 32, o[t], inv, hh, w.live);
-  } else if (w.live) {
-    const int64_t rec = row * a.parts + part;
-    float *dst = a.po + rec * HD + 4 * hh;
+    for (int t = 0; t < NT; ++t) store_o32(out + row * HD + t * 32, o[t], inv, hh, live);
+  } else {
+    // Through LDS, so that a row's dims leave as one run of bytes (16 bytes a
+    // lane and row at a time took 1.9 us of a one-block item): 16-byte pieces
+    // XOR-swizzled by the row, the wave's 32 rows in a place of its own.
+    constexpr int LR = HD / 4, RI = 64 / LR;  // lanes of a row, rows of a store
+    char *own = lds + wave * 32 * HD * 4;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; r += 4)
-        *(float4 *)(dst + t * 32 + 2 * r) = make_float4(o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3]);
-    if (hh == 0) *(float2 *)(a.pml + rec * 2) = make_float2(mref, sum);
+      for (int r = 0; r < 16; r += 4) {
+        const int piece = t * 8 + r / 2 + hh;
+        *(float4 *)(own + l32 * HD * 4 + ((piece ^ (l32 % LR)) * 16)) =
+            make_float4(o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3]);
+      }
+    if (live && hh == 0) *(float2 *)(a.pml + (row * a.parts + part) * 2) = make_float2(mref, sum);
+    const uint32_t rows_live = (uint32_t)__ballot(live);
+    // rolled up: the launch's first pass over code costs about 90 clocks per 64
+    // bytes, and this runs once
+#pragma unroll 4
+    for (int i = 0; i < 32 / RI; ++i) {
+      const int x = i * RI + lane / LR;
+      const float4 v = *(const float4 *)(own + x * HD * 4 + (((lane % LR) ^ (x % LR)) * 16));
+      const PrefixRow y = packed_row(a, start, r0, wave * 32 + x, g);
+      if (rows_live >> x & 1)
+        *(float4 *)(a.po + (((int64_t)y.token * Hq + y.head) * a.parts + part) * HD + lane % LR * 4) = v;
+    }
   }
 }
 
 template <typename T, int HD>
-constexpr int TILE_LDS = 4 * 64 * HD * 2;  // two stages of K and V
+constexpr int TILE_LDS = 4 * 64 * HD * 2 + 16;  // two stages of K and V, a flag
 
 template <typename T, int HD, int QW>
 __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) void prefix_tile_kernel(
     const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[TILE_LDS<T, HD>];
   // KV head fastest: with 8 of them each XCD's L2 holds one head's blocks
-  const int Hkv = a.b.kv.n_kv_heads;
-  tile_item<T, HD, QW>(q, out, a, blockIdx.x / Hkv, blockIdx.x % Hkv, lds);
+  const int i = div_by(blockIdx.x, a.by_hkv);
+  tile_item<T, HD, QW>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
 }
 
 // Few rows over a range of entries, on 16x16x32 MFMAs: up to 16 packed rows of a
@@ -557,14 +610,15 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
   int j = -1, r0, e0, e1, part, slot = -1;
   const int shared = a.shared_rows * a.splits;
   if (idx < shared) {
-    r0 = idx % a.shared_rows * 16;
-    part = idx / a.shared_rows;
+    part = div_by(idx, a.by_shared);
+    r0 = (idx - part * a.shared_rows) * 16;
     e0 = part * a.sblk;
     e1 = min(a.nP, e0 + a.sblk);
   } else {
     idx -= shared;
-    const int s = idx / a.otiles;  // all rows' first splits, then their second ones: the grid ends with what few have
-    own_tile<16>(a, idx % a.otiles, j, r0);
+    // all rows' first splits, then their second ones: the grid ends with what few have
+    const int s = div_by(idx, a.by_otiles);
+    own_tile<16>(a, idx - s * a.otiles, j, r0);
     part = a.splits + s;
     slot = a.b.seq_slot[j];
     const int ctx = row_ctx(a.b, j, 0);
@@ -581,8 +635,9 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
     if (id >= 0) off = ((int64_t)id * Hkv + g) * (KV_BLOCK * HD * 2);
   }
   const int off_lo = (int)off, off_hi = (int)(off >> 32);
-  const PrefixRow w = packed_row(a, j, r0 + r16, g);
-  const int ctx = w.live ? w.ctx : 0;
+  const PrefixRow w = packed_row(a, max(j, 0), r0, r16, g);
+  const int seen_ = packed_ctx(a, j, w.t, 1), ctx = max(seen_, 0);
+  const bool live = seen_ >= 0;
   const int ctx_top = (int)~wave_min_u32(~(uint32_t)ctx);
   // rows that see nothing get zeros at the end, whatever is summed for them
   const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
@@ -616,7 +671,7 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
     for (int nt = 0; nt < NT; ++nt) vf[nt] = load8<T>((const T *)(vb + nt * 16 * KV_BLOCK * 2 + vlane));
   };
   v8 qa[KS];
-  const T *qrow = q + ((int64_t)w.token * Hq + w.head) * HD;
+  const T *qrow = q + ((int64_t)(live ? w.token : 0) * Hq + w.head) * HD;
 #pragma unroll
   for (int k = 0; k < KS; ++k) qa[k] = load8<T>(qrow + k * 32 + kq);
   // row 4 quad + i: running maximum (raw scores) and this lane's share of the
@@ -752,7 +807,7 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
   // a wave a row: its lanes over the dims
   for (int r = wave; r < nrows; r += 4) {
     const int token = __builtin_amdgcn_readlane(w.token, r), h = __builtin_amdgcn_readlane(w.head, r);
-    if (!__builtin_amdgcn_readlane((int)w.live, r)) continue;
+    if (!__builtin_amdgcn_readlane((int)live, r)) continue;
     float M = -INFINITY, f[4], L = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) M = fmaxf(M, wm[k * 16 + r]);
@@ -780,8 +835,8 @@ template <typename T, int HD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_decode_kernel(
     const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[std::max(TILE_LDS<T, HD>, ROWS_LDS<T, HD>)];
-  const int Hkv = a.b.kv.n_kv_heads, g = blockIdx.x % Hkv;
-  int i = blockIdx.x / Hkv;
+  int i = div_by(blockIdx.x, a.by_hkv);
+  const int g = blockIdx.x - i * a.b.kv.n_kv_heads;
   const int tiles = a.tiles * a.splits, rows = a.shared_rows * a.splits + a.otiles * a.osplits;
   const int both = min(tiles, rows);
   bool tile = tiles > rows;
@@ -801,7 +856,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 // weights first, then the dims.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, PrefixArgs a) {
-  constexpr int DPL = HD / 64, U = 4;
+  constexpr int DPL = HD / 64, U = 16;
   constexpr float c2 = SCORE_C2<HD>;
   const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
@@ -831,6 +886,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
 #pragma unroll
     for (int d = 0; d < DPL; ++d) o[d] *= f0;
     for (int p = 0; p < n; p += U) {
+      // all requested before any is used; past the last part: 0 of that part again
       float v[U][DPL];
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -838,10 +894,9 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
         for (int d = 0; d < DPL; ++d) v[u][d] = po[(int64_t)(p0 + min(p + u, n - 1)) * HD + d];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (p + u >= n) break;
         const float fu = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), p + u));
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) o[d] += fu * v[u][d];
+        for (int d = 0; d < DPL; ++d) o[d] += fu * (p + u < n ? v[u][d] : 0.f);
       }
     }
   }
@@ -914,6 +969,13 @@ static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   a.otiles = decode ? b.rows * ceil_div(a.G, rto)
                     : (int)std::min((int64_t)b.n_seq * ceil_div((int64_t)std::min(b.max_new, b.rows) * a.G, rto),
                                     (int64_t)b.rows * a.G / rto + b.n_seq);
+  a.by_g = divisor(a.G);
+  a.by_hkv = divisor(Hkv);
+  a.by_splits = divisor(a.splits);
+  a.by_osplits = divisor(a.osplits);
+  a.by_otiles = divisor(a.otiles);
+  a.by_shared = divisor(a.shared_rows);
+  a.by_per = divisor(ceil_div(a.G, rto));
   const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.otiles * a.osplits) * Hkv;
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
   if constexpr (half) {

@@ -527,30 +527,21 @@ def op_init_weight(dst, seed, tensor_id, std):
 
 # ------------------------------------------------------------------ a batch that shares a prefix
 
-def _call(fn, device, args):
-    """fn(*args, stream) on the current stream of `device`, which is made current for the call."""
+def _call(fn, dev, args):
+    """fn(*args, stream) on the current stream of GPU `dev`, which is made current for the call."""
     import torch
-    stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, stream))
+    C_ = torch._C
+    if hasattr(C_, "_cuda_getCurrentRawStream"):  # 2 us less than a Stream object
+        stream = C_._cuda_getCurrentRawStream(dev)
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, stream))
-
-
-def _tensors(device, dtype, **named):
-    """Data pointers of contiguous tensors of one dtype on `device`, in order (None: a null pointer)."""
-    _need(device.type == "cuda", f"tensors on a GPU, got {device}")
-    ptrs = []
-    for name, t in named.items():
-        if t is None:
-            ptrs.append(None)
-            continue
-        if t.dtype != dtype or t.device != device or not t.is_contiguous():
-            raise ValueError(f"{name}: a contiguous {dtype} tensor on {device}, got {t.dtype} on {t.device}"
-                             f"{'' if t.is_contiguous() else ', not contiguous'}")
-        ptrs.append(t.data_ptr())
-    return ptrs
+        stream = torch.cuda.current_stream(dev).cuda_stream
+    if dev == torch.cuda.current_device():
+        rc = fn(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, stream)
+    if rc:
+        _check(rc)
 
 
 def _need(ok, what):
@@ -558,11 +549,45 @@ def _need(ok, what):
         raise ValueError(what)
 
 
+def _gpu(t):
+    """The GPU that t is on."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"tensors on a GPU, got {t.device}")
+    return dev
+
+
+def _pointers(dev, dtype, names, *tensors):
+    """Data pointers of contiguous tensors of one dtype on GPU `dev` (None: a
+    null pointer); `names` are theirs, for the error."""
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+        elif t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+            out.append(t.data_ptr())
+        else:
+            raise ValueError(f"{names.split()[len(out)]}: a contiguous {dtype} tensor on GPU {dev}, got {t.dtype} on "
+                             f"{t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+    return out
+
+
 def _dt3(t):
     import torch
-    d = {torch.float32: LP_F32, torch.bfloat16: LP_BF16, torch.float16: LP_F16}.get(t.dtype)
-    _need(d is not None, f"float32, bfloat16 or float16 tensors, got {t.dtype}")
-    return d
+    d = t.dtype
+    if d is torch.float16:
+        return LP_F16
+    if d is torch.bfloat16:
+        return LP_BF16
+    _need(d is torch.float32, f"float32, bfloat16 or float16 tensors, got {d}")
+    return LP_F32
+
+
+def _cache_shape(kc, vc, hd):
+    n_blocks, hkv, block, khd = kc.shape
+    _need(block == 64 and khd == hd and vc.shape == (n_blocks, hkv, hd, 64),
+          "kc [n_blocks, Hkv, 64, hd], vc [n_blocks, Hkv, hd, 64]")
+    return n_blocks, hkv
 
 
 def op_block_tables(seq_slot, cached, lengths, prefix_blocks, prefix_len, free_blocks, free_head, block_table,
@@ -573,19 +598,20 @@ def op_block_tables(seq_slot, cached, lengths, prefix_blocks, prefix_len, free_b
     free_head [1], block_table [n_slots, max_blocks], seq_start and free_start
     [n + 1], row_slot and row_pos [max_rows]; row_entry int64 [max_rows]."""
     import torch
-    dev, n = seq_slot.device, seq_slot.numel()
-    i32 = _tensors(dev, torch.int32, seq_slot=seq_slot, cached=cached, lengths=lengths, prefix_blocks=prefix_blocks,
-                   free_blocks=free_blocks, free_head=free_head, block_table=block_table, seq_start=seq_start,
-                   free_start=free_start, row_slot=row_slot, row_pos=row_pos)
-    entry, = _tensors(dev, torch.int64, row_entry=row_entry)
-    max_rows = row_entry.numel()
-    _need(cached.numel() == n and lengths.numel() == n and seq_start.numel() == n + 1 and free_start.numel() == n + 1
+    dev, n, max_rows = _gpu(seq_slot), seq_slot.numel(), row_entry.numel()
+    slot, held, length, pre, free, head, table, start, taken, rslot, rpos = _pointers(
+        dev, torch.int32, "seq_slot cached lengths prefix_blocks free_blocks free_head block_table seq_start free_start "
+        "row_slot row_pos", seq_slot, cached, lengths, prefix_blocks, free_blocks, free_head, block_table, seq_start,
+        free_start, row_slot, row_pos)
+    entry, = _pointers(dev, torch.int64, "row_entry", row_entry)
+    n_slots, max_blocks = block_table.shape
+    _need(cached.numel() == lengths.numel() == n and seq_start.numel() == free_start.numel() == n + 1
           and free_head.numel() >= 1, "seq_slot, cached, lengths [n]; seq_start, free_start [n + 1]; free_head [1]")
-    _need(row_slot.numel() == max_rows and row_pos.numel() == max_rows, "row_slot, row_pos and row_entry: one length")
-    _need(prefix_blocks is None or prefix_blocks.numel() * 64 >= prefix_len, "prefix_blocks: ceil(prefix_len / 64)")
+    _need(row_slot.numel() == row_pos.numel() == max_rows, "row_slot, row_pos and row_entry: one length")
+    _need(pre is None or prefix_blocks.numel() * 64 >= prefix_len, "prefix_blocks: ceil(prefix_len / 64)")
     _call(lib().lp_op_block_tables, dev,
-          (i32[0], i32[1], i32[2], n, i32[3], prefix_len, i32[4], free_blocks.numel(), i32[5], i32[6],
-           block_table.shape[0], block_table.shape[1], i32[7], i32[8], i32[9], i32[10], entry, max_rows))
+          (slot, held, length, n, pre, prefix_len, free, free_blocks.numel(), head, table, n_slots, max_blocks, start,
+           taken, rslot, rpos, entry, max_rows))
 
 
 def op_qkv_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, kc, vc):
@@ -593,25 +619,22 @@ def op_qkv_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, kc, vc):
     may be strided), rounds q to q [rows, Hq, hd] and stores k and v in the
     cache at row_entry (lp_op_qkv_append)."""
     import torch
-    dev, dt = q.device, _dt3(q)
+    dt, dev = _dt3(q), _gpu(q)
     rows, hq, hd = q.shape
-    n_blocks, hkv = kc.shape[:2]
-    acts = _tensors(dev, q.dtype, q=q, kc=kc, vc=vc)
-    cos, sin = _tensors(dev, torch.float32, rope_cos=rope_cos, rope_sin=rope_sin)
-    pos, = _tensors(dev, torch.int32, row_pos=row_pos)
-    entry, = _tensors(dev, torch.int64, row_entry=row_entry)
-    _need(qkv.dtype == torch.float32 and qkv.device == dev and qkv.dim() == 2 and (rows == 0 or qkv.stride(1) == 1),
-          "qkv: float32 rows of contiguous columns")
-    _need(tuple(kc.shape) == (n_blocks, hkv, 64, hd) and tuple(vc.shape) == (n_blocks, hkv, hd, 64),
-          "kc [n_blocks, Hkv, 64, hd], vc [n_blocks, Hkv, hd, 64]")
-    _need(tuple(qkv.shape) == (rows, (hq + 2 * hkv) * hd) and row_pos.numel() == rows and row_entry.numel() == rows,
-          "qkv [rows, (Hq + 2 Hkv) hd], row_pos and row_entry [rows]")
+    n_blocks, hkv = _cache_shape(kc, vc, hd)
+    acts = _pointers(dev, q.dtype, "q kc vc", q, kc, vc)
+    cos, sin = _pointers(dev, torch.float32, "rope_cos rope_sin", rope_cos, rope_sin)
+    pos, = _pointers(dev, torch.int32, "row_pos", row_pos)
+    entry, = _pointers(dev, torch.int64, "row_entry", row_entry)
+    width = (hq + 2 * hkv) * hd
+    _need(qkv.dtype is torch.float32 and qkv.get_device() == dev and qkv.shape == (rows, width)
+          and (rows == 0 or qkv.stride(1) == 1), "qkv: float32 [rows, (Hq + 2 Hkv) hd], columns contiguous")
+    _need(row_pos.numel() == row_entry.numel() == rows, "row_pos and row_entry [rows]")
     _need(rope_cos.shape == rope_sin.shape and rope_cos.dim() == 2 and rope_cos.shape[1] == hd // 2,
           "rope_cos, rope_sin [positions, hd / 2]")
-    ld = qkv.stride(0) if rows > 1 else qkv.shape[1]
     _call(lib().lp_op_qkv_append, dev,
-          (dt, qkv.data_ptr(), ld, cos, sin, rope_cos.shape[0], pos, entry, rows, acts[0], acts[1], acts[2], n_blocks,
-           hq, hkv, hd))
+          (dt, qkv.data_ptr(), qkv.stride(0) if rows > 1 else width, cos, sin, rope_cos.shape[0], pos, entry, rows,
+           *acts, n_blocks, hq, hkv, hd))
 
 
 def prefix_decode_attention_ws_bytes(M, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx):
@@ -622,23 +645,21 @@ def prefix_prefill_attention_ws_bytes(rows, n_heads, n_kv_heads, head_dim, prefi
     return lib().lp_op_prefix_prefill_attention_ws_bytes(rows, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx)
 
 
-def _prefix_args(q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws, **index):
-    """What both phases hand over alike: dtype and cache arguments, the index
-    tensors' pointers, and the workspace's pointer and bytes."""
+def _prefix_args(q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws, index, names):
+    """What both phases hand over alike: the GPU, dtype and cache arguments, the
+    index tensors' pointers, heads and head_dim, the workspace's pointer and bytes."""
     import torch
-    dev, dt = q.device, _dt3(q)
-    hd = q.shape[2]
-    n_blocks, hkv = kc.shape[:2]
-    acts = _tensors(dev, q.dtype, q=q, out=out, kc=kc, vc=vc)
-    idx = _tensors(dev, torch.int32, prefix_blocks=prefix_blocks, block_table=block_table, **index)
+    dt, dev = _dt3(q), _gpu(q)
+    hq, hd = q.shape[1:]
+    n_blocks, hkv = _cache_shape(kc, vc, hd)
+    acts = _pointers(dev, q.dtype, "q out kc vc", q, out, kc, vc)
+    pre, table, *idx = _pointers(dev, torch.int32, names, prefix_blocks, block_table, *index)
+    n_slots, max_blocks = block_table.shape
     _need(out.shape == q.shape, "out: shape of q")
-    _need(tuple(kc.shape) == (n_blocks, hkv, 64, hd) and tuple(vc.shape) == (n_blocks, hkv, hd, 64),
-          "kc [n_blocks, Hkv, 64, hd], vc [n_blocks, Hkv, hd, 64]")
-    _need(prefix_blocks is None or prefix_blocks.numel() * 64 >= prefix_len, "prefix_blocks: ceil(prefix_len / 64)")
-    _need(ws is None or (ws.device == dev and ws.is_contiguous()), "ws: contiguous, on the device of q")
-    cache = (dt, *acts, n_blocks, idx[0], prefix_len, idx[1], block_table.shape[0], block_table.shape[1])
+    _need(pre is None or prefix_blocks.numel() * 64 >= prefix_len, "prefix_blocks: ceil(prefix_len / 64)")
+    _need(ws is None or (ws.get_device() == dev and ws.is_contiguous()), "ws: contiguous, on the GPU of q")
     space = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
-    return cache, idx[2:], space
+    return dev, (dt, *acts, n_blocks, pre, prefix_len, table, n_slots, max_blocks), idx, (hq, hkv, hd), space
 
 
 def op_prefix_decode_attention(q, out, kc, vc, prefix_blocks, prefix_len, block_table, row_slot, row_pos, max_ctx, ws):
@@ -647,12 +668,11 @@ def op_prefix_decode_attention(q, out, kc, vc, prefix_blocks, prefix_len, block_
     hd], vc [n_blocks, Hkv, hd, 64]; int32 prefix_blocks (None without a
     prefix), block_table [n_slots, max_blocks], row_slot and row_pos [M]; ws of
     prefix_decode_attention_ws_bytes."""
-    M, hq, hd = q.shape
-    cache, idx, space = _prefix_args(q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws, row_slot=row_slot,
-                                     row_pos=row_pos)
-    _need(row_slot.numel() == M and row_pos.numel() == M, "row_slot, row_pos [M]")
-    _call(lib().lp_op_prefix_decode_attention, q.device,
-          (*cache, *idx, M, hq, kc.shape[1], hd, max_ctx, *space))
+    M = q.shape[0]
+    dev, cache, idx, heads, space = _prefix_args(q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws,
+                                                 (row_slot, row_pos), "prefix_blocks block_table row_slot row_pos")
+    _need(row_slot.numel() == row_pos.numel() == M, "row_slot, row_pos [M]")
+    _call(lib().lp_op_prefix_decode_attention, dev, (*cache, *idx, M, *heads, max_ctx, *space))
 
 
 def op_prefix_prefill_attention(q, out, kc, vc, prefix_blocks, prefix_len, block_table, seq_start, seq_slot, seq_pos,
@@ -662,10 +682,9 @@ def op_prefix_prefill_attention(q, out, kc, vc, prefix_blocks, prefix_len, block
     seq_start [n + 1], seq_slot and seq_pos [n] (position of each sequence's
     first row); the others as for decode, ws of
     prefix_prefill_attention_ws_bytes."""
-    rows, hq, hd = q.shape
-    n = seq_slot.numel()
-    cache, idx, space = _prefix_args(q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws, seq_start=seq_start,
-                                     seq_slot=seq_slot, seq_pos=seq_pos)
+    rows, n = q.shape[0], seq_slot.numel()
+    dev, cache, idx, heads, space = _prefix_args(
+        q, out, kc, vc, prefix_blocks, prefix_len, block_table, ws, (seq_start, seq_slot, seq_pos),
+        "prefix_blocks block_table seq_start seq_slot seq_pos")
     _need(seq_start.numel() == n + 1 and seq_pos.numel() == n, "seq_start [n + 1], seq_slot and seq_pos [n]")
-    _call(lib().lp_op_prefix_prefill_attention, q.device,
-          (*cache, *idx, n, rows, max_new, hq, kc.shape[1], hd, max_ctx, *space))
+    _call(lib().lp_op_prefix_prefill_attention, dev, (*cache, *idx, n, rows, max_new, *heads, max_ctx, *space))
