@@ -40,9 +40,11 @@ struct PrefixArgs {
   int tiles, splits, sblk;    // shared items: row tiles, splits of the prefix, entries of a split
   int shared_rows;            // 16-row tiles of the shared items that take rows_item (tiles is 0 then)
   int otiles, osplits, oblk;  // own items: row tiles, splits of the own entries, entries of a split
+  int own_log, units;         // decode: waves of a row's own item (log 2), workgroups of a split of them
   int parts;                  // splits + osplits
   int direct;                 // one part, written to out by the tile kernel itself
-  Divisor by_g, by_hkv, by_splits, by_osplits, by_otiles, by_shared, by_per;
+  int whole;                  // decode: a workgroup takes all keys of a row
+  Divisor by_g, by_hkv, by_splits, by_osplits, by_units, by_shared, by_per;
   float *po, *pml;            // partial o [rows][n_heads][parts][hd], (m, l) [rows][n_heads][parts][2]
 };
 // A part's m is the largest score before the scale 1/sqrt(hd), its weights are
@@ -589,26 +591,40 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 }
 
 // Few rows over a range of entries, on 16x16x32 MFMAs: up to 16 packed rows of a
-// KV head; wave w takes every fourth entry from the w-th on, its K and V
-// fragments straight from the cache in registers, the next entry's K requested
-// as soon as this one's is used, V likewise.  Online softmax per wave; P goes
-// through LDS into the A operand's layout; the waves' (m, l, o) meet in LDS at
-// the end.  Own items: the query heads of one row.  Shared items (batches of few
-// rows): packed rows.
+// KV head; wave w takes every NW-th entry from the w-th on, 32 keys at a time.
+// Each wave has its own LDS for K and V of 32 keys: K is copied there while the
+// softmax of the keys before runs, V while the scores do.  (Fragments loaded
+// straight from the cache ask for 16 rows with every four lanes on four lines:
+// 21 bytes a clock and CU, 6,200 clocks per 32 keys with eight waves, against
+// 1,900 with one.)  Online softmax per wave; P goes through LDS into the A
+// operand's layout; the waves' (m, l, o) meet in LDS at the end.  Own items: the
+// query heads of one row.  Shared items (batches of few rows): packed rows.
 template <typename T, int HD>
-__device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixArgs &a, int idx, int g, char *lds) {
+constexpr int ROWS_KV = 32 * HD * 2;  // bytes of 32 keys, K or V
+template <typename T, int HD, int NW>
+constexpr int ROWS_LDS = NW * (2 * ROWS_KV<T, HD> + 16 * 40 * 2 + 2 * 16 * 4);
+
+// With WHOLE an item is all that the query heads of one row see, prefix and own
+// entries, and its result goes to out.
+template <typename T, int HD, int NW, bool WHOLE>
+__device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict__ out, const PrefixArgs &a, int idx,
+                                          int g, char *lds) {
   typedef typename Mfma<T>::v8 v8;
   constexpr int KS = HD / 32, NT = HD / 16, LP = 32 + 8;
   constexpr float c2 = SCORE_C2<HD>;
-  float(*wo)[16][HD] = (float(*)[16][HD])lds;                  // [4][16][HD]
-  float *wm = (float *)(lds + 4 * 16 * HD * 4), *wl = wm + 64;  // [4][16] each
-  T(*pls)[LP] = (T(*)[LP])(lds + 4 * 16 * HD * 4 + 512);       // [4 * 16][LP]
+  constexpr int KV = ROWS_KV<T, HD>, ND = KV / 1024;  // copies of 1 KB
+  constexpr int CK = HD / 8, KR = 64 / CK;            // 16-byte pieces of a K row, rows of a copy
+  static_assert(16 * HD * 4 <= 2 * KV, "o of a wave in the place of its K and V");
+  float *wm = (float *)(lds + NW * 2 * KV), *wl = wm + NW * 16;  // [NW][16] each
+  T(*pls)[LP] = (T(*)[LP])(lds + NW * (2 * KV + 2 * 16 * 4));    // [NW * 16][LP]
   const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads, P = a.b.prefix_len;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int r16 = lane & 15, quad = lane >> 4, kq = quad * 8;
   pls += wave * 16;
-  int j = -1, r0, e0, e1, part, slot = -1;
-  const int shared = a.shared_rows * a.splits;
+  int j = -1, r0, e0, e1, part = 0, slot = -1;
+  const int shared = WHOLE ? 0 : a.shared_rows * a.splits;
+  // waves that share an item's entries: all, or of a row's own ones 2^own_log
+  int log = NW == 8 ? 3 : 2;
   if (idx < shared) {
     part = div_by(idx, a.by_shared);
     r0 = (idx - part * a.shared_rows) * 16;
@@ -616,17 +632,20 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
     e1 = min(a.nP, e0 + a.sblk);
   } else {
     idx -= shared;
+    if (!WHOLE) log = a.own_log;
     // all rows' first splits, then their second ones: the grid ends with what few have
-    const int s = div_by(idx, a.by_otiles);
-    own_tile<16>(a, idx - s * a.otiles, j, r0);
+    const int s = WHOLE ? 0 : div_by(idx, a.by_units);
+    const int u = ((idx - s * a.units) << (WHOLE ? 0 : 2 - log)) + (wave >> log);
+    own_tile<16>(a, min(u, a.otiles - 1), j, r0);
     part = a.splits + s;
     slot = a.b.seq_slot[j];
-    const int ctx = row_ctx(a.b, j, 0);
-    e0 = a.nP + s * a.oblk;
-    e1 = min(e0 + a.oblk, ctx > P ? a.nP + (ctx + KV_BLOCK - 1) / KV_BLOCK - a.F : 0);
-    if (e0 >= e1) return;  // the join reads no such part
+    const int ctx = u < a.otiles ? row_ctx(a.b, j, 0) : 0;
+    const int end = ctx > P ? a.nP + (ctx + KV_BLOCK - 1) / KV_BLOCK - a.F : WHOLE ? (ctx + KV_BLOCK - 1) / KV_BLOCK : 0;
+    e0 = WHOLE ? 0 : a.nP + s * a.oblk;
+    e1 = WHOLE ? end : min(e0 + a.oblk, end);
   }
   const bool own = j >= 0;
+  const int nth = wave & ((1 << log) - 1);  // the wave's place among them
   // Byte offsets of the entries' blocks (head included), -1 for none: lane i
   // holds that of entry e0 + i (an item has at most 64).
   int64_t off = -1;
@@ -641,34 +660,42 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
   const int ctx_top = (int)~wave_min_u32(~(uint32_t)ctx);
   // rows that see nothing get zeros at the end, whatever is summed for them
   const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
-  // the wave's entries that have a block some row sees, and those of them that
-  // not every row sees whole (rows inside the prefix), which come after the rest
-  const int first = e0 + lane < a.nP ? (e0 + lane) * KV_BLOCK : (a.F + e0 + lane - a.nP) * KV_BLOCK;
-  const int last = own ? INT_MAX : P;
-  const uint64_t mine = 0x1111111111111111ull << wave;
-  const uint64_t seen = __ballot(off >= 0 && first < ctx_top) & mine;
-  const uint64_t mixed = own ? 0 : seen & __ballot(min(first + KV_BLOCK, last) > ctx_lo);
-  // K and V of 32 keys: keys 16 nt + r16 of the half, dims 32 k + kq .. of K;
-  // dim 16 nt + r16, keys kq .. of V
-  v8 kf[2][KS], vf[NT];
-  const uint32_t klane = (r16 * HD + kq) * 2, vlane = (r16 * KV_BLOCK + kq) * 2;
+  // the wave's entries that have a block some row sees (and some row its second
+  // half), and those of them that not every row sees whole (rows inside the
+  // prefix), which come after the rest
+  const bool pre = e0 + lane < a.nP;
+  const int first = pre ? (e0 + lane) * KV_BLOCK : (a.F + e0 + lane - a.nP) * KV_BLOCK;
+  const int from = pre ? 0 : P, to = min(pre ? P : INT_MAX, ctx_top);  // its positions [from, to)
+  const uint64_t mine = ~0ull / ((1ull << (1 << log)) - 1) << nth;  // every 2^log-th
+  const uint64_t seen = __ballot(off >= 0 && first < to) & mine;
+  const uint64_t second = __ballot(first + 32 < to);
+  const uint64_t mixed = own ? 0 : seen & __ballot(min(first + KV_BLOCK, to) > ctx_lo);
+  // copies into this wave's LDS, the 16-byte pieces of a row XOR-swizzled
+  char *ks = lds + wave * 2 * KV, *vs = ks + KV;
+  const uint32_t kl = lds_addr(ks), vl = kl + KV;
+  uint32_t ko[16 / KR];  // byte offsets of this lane's pieces, rows 0 .. 15
+#pragma unroll
+  for (int c = 0; c < 16 / KR; ++c) {
+    const int row = c * KR + lane / CK;
+    ko[c] = row * HD * 2 + ((lane % CK) ^ (row & (CK - 1))) * 16;
+  }
+  const uint32_t vo = (lane >> 2) * KV_BLOCK * 2 + ((lane & 3) ^ ((lane >> 3) & 3)) * 16;
   int64_t at;
   auto place = [&](int i, int h) __attribute__((always_inline)) {  // half h of entry e0 + i
     at = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, i) << 32) |
                    (uint32_t)__builtin_amdgcn_readlane(off_lo, i));
     return __builtin_amdgcn_readlane(first, i) + h * 32;
   };
-  auto load_k = [&](int h) __attribute__((always_inline)) {
+  auto copy_k = [&](int h) __attribute__((always_inline)) {
     const char *kb = (const char *)a.b.kv.k + at + h * 32 * HD * 2;
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int k = 0; k < KS; ++k) kf[nt][k] = load8<T>((const T *)(kb + (nt * 16 * HD + k * 32) * 2 + klane));
+    for (int c = 0; c < ND; ++c)
+      dma16s(kb + c / (16 / KR) * 16 * HD * 2, ko[c % (16 / KR)], kl + c * 1024);
   };
-  auto load_v = [&](int h) __attribute__((always_inline)) {
+  auto copy_v = [&](int h) __attribute__((always_inline)) {
     const char *vb = (const char *)a.b.kv.v + at + h * 32 * 2;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) vf[nt] = load8<T>((const T *)(vb + nt * 16 * KV_BLOCK * 2 + vlane));
+    for (int c = 0; c < ND; ++c) dma16s(vb + c * 16 * KV_BLOCK * 2, vo, vl + c * 1024);
   };
   v8 qa[KS];
   const T *qrow = q + ((int64_t)(live ? w.token : 0) * Hq + w.head) * HD;
@@ -689,12 +716,15 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) s[nt] = Mfma<T>::m16(qa[k], kf[nt][k], s[nt]);
+      for (int nt = 0; nt < 2; ++nt) {
+        const v8 f = *(const v8 *)(ks + (nt * 16 + r16) * HD * 2 + (((k * 4 + quad) ^ (r16 & (CK - 1))) * 16));
+        s[nt] = Mfma<T>::m16(qa[k], f, s[nt]);
+      }
   };
-  // keys [lo, hi) of the 32 at `base` are there
-  auto bounds = [&](int base, int &lo, int &hi) __attribute__((always_inline)) {
-    lo = own ? max(0, P - base) : 0;
-    hi = min(32, min(last, ctx_top) - base);
+  // keys [lo, hi) of the 32 at `base`, of entry e0 + i, are there
+  auto bounds = [&](int i, int base, int &lo, int &hi) __attribute__((always_inline)) {
+    lo = max(0, __builtin_amdgcn_readlane(from, i) - base);
+    hi = min(32, __builtin_amdgcn_readlane(to, i) - base);
   };
   // s[nt][i]: row 4 quad + i, key nt * 16 + r16, to weights in LDS
   auto weights = [&](int base, int lo, int hi) __attribute__((always_inline)) {
@@ -724,28 +754,20 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
   uint64_t left = seen & ~mixed;
   if (left) {
     int i = __builtin_ctzll(left), h = 0, base = place(i, 0);
-    load_k(0);
-    __builtin_amdgcn_sched_barrier(0);
-    load_v(0);
-    __builtin_amdgcn_sched_barrier(0);
-    // One half; with `more`, the next one's K and V are requested as soon as
-    // their registers are free.  The last half has code of its own: where loads
-    // may or may not have been issued, the compiler waits for all of them.
-    auto step = [&](auto more_) __attribute__((always_inline)) {
-      constexpr bool more = decltype(more_)::value;
+    copy_k(0);
+    copy_v(0);
+    for (int n = __builtin_popcountll(left) + __builtin_popcountll(left & second); n > 0; --n) {
       int lo, hi, nbase = 0;
-      bounds(base, lo, hi);
+      bounds(i, base, lo, hi);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");  // K is there, V may not be
       scores();
-      if constexpr (more) {
-        h ^= 1;
-        if (!h) {
-          left &= left - 1;
-          i = __builtin_ctzll(left);
-        }
+      if (n > 1) {
+        h = (int)(second >> i & 1) & (h ^ 1);
+        left = h ? left : left & (left - 1);
+        i = __builtin_ctzll(left);
         nbase = place(i, h);
-        __builtin_amdgcn_sched_barrier(0);
-        load_k(h);
-        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
+        copy_k(h);
       }
       weights(base, lo, hi);
       // V outside [lo, hi) is stale and may hold anything, and 0 * NaN is not 0
@@ -756,18 +778,21 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
         keep[y] = (key >= lo && key < hi ? 0xFFFFu : 0u) | (key + 1 >= lo && key + 1 < hi ? 0xFFFF0000u : 0u);
       }
       const v8 pa = load8<T>(&pls[r16][kq]);
+      if (n > 1)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");
+      else
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-        o[nt] = Mfma<T>::m16(pa, __builtin_bit_cast(v8, __builtin_bit_cast(u32x4_tt, vf[nt]) & keep), o[nt]);
-      if constexpr (more) {
-        __builtin_amdgcn_sched_barrier(0);
-        load_v(h);
-        __builtin_amdgcn_sched_barrier(0);
-        base = nbase;
+      for (int nt = 0; nt < NT; ++nt) {
+        const u32x4_tt f = *(const u32x4_tt *)(vs + (nt * 16 + r16) * 64 + ((quad ^ ((r16 >> 1) & 3)) * 16));
+        o[nt] = Mfma<T>::m16(pa, __builtin_bit_cast(v8, f & keep), o[nt]);
       }
-    };
-    while (h == 0 || (left & (left - 1))) step(std::true_type());
-    step(std::false_type());
+      if (n > 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
+        copy_v(h);
+      }
+      base = nbase;
+    }
   }
   // a key at a time, each added to the rows that see it (a weight of 0 does not
   // cancel V that is infinite or NaN)
@@ -775,9 +800,11 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
 #pragma unroll 1
     for (int h = 0; h < 2; ++h) {
       int lo, hi;
-      const int base = place(__builtin_ctzll(left), h);
-      bounds(base, lo, hi);
-      load_k(h);
+      const int i = __builtin_ctzll(left), base = place(i, h);
+      bounds(i, base, lo, hi);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      copy_k(h);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       scores();
       weights(base, lo, hi);
       const T *vb = (const T *)((const char *)a.b.kv.v + at) + r16 * KV_BLOCK + h * 32;
@@ -792,6 +819,7 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
         }
       }
     }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // o goes where K and V were
   const int nrows = own ? min(16, a.G - r0) : 16;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -800,56 +828,65 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, const PrefixA
     if (r16 == 0) wm[wave * 16 + r] = mx[i], wl[wave * 16 + r] = t;
     if (r < nrows) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) wo[wave][r][nt * 16 + r16] = o[nt][i];
+      for (int nt = 0; nt < NT; ++nt) ((float *)ks)[r * HD + nt * 16 + r16] = o[nt][i];
     }
   }
   __syncthreads();
+  if (!WHOLE && e0 >= e1) return;  // the join reads no such part
   // a wave a row: its lanes over the dims
-  for (int r = wave; r < nrows; r += 4) {
+  const int w0 = wave - nth;
+  for (int r = nth; r < nrows; r += 1 << log) {
     const int token = __builtin_amdgcn_readlane(w.token, r), h = __builtin_amdgcn_readlane(w.head, r);
     if (!__builtin_amdgcn_readlane((int)live, r)) continue;
-    float M = -INFINITY, f[4], L = 0.f;
+    float M = -INFINITY, L = 0.f, v[HD / 64];
+    for (int k = w0; k < w0 + (1 << log); ++k) M = fmaxf(M, wm[k * 16 + r]);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) M = fmaxf(M, wm[k * 16 + r]);
+    for (int d = 0; d < HD / 64; ++d) v[d] = 0.f;
+    for (int k = w0; k < w0 + (1 << log); ++k) {
+      const float m = wm[k * 16 + r], f = m == M ? 1.f : __builtin_amdgcn_exp2f((m - M) * c2);
+      L += f * wl[k * 16 + r];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      f[k] = wm[k * 16 + r] == M ? 1.f : __builtin_amdgcn_exp2f((wm[k * 16 + r] - M) * c2);
-      L += f[k] * wl[k * 16 + r];
+      for (int d = 0; d < HD / 64; ++d) v[d] += f * ((const float *)(lds + k * 2 * KV))[r * HD + d * 64 + lane];
     }
-    const int64_t rec = ((int64_t)token * Hq + h) * a.parts + part;
     const bool none = __builtin_amdgcn_readlane(ctx, r) == 0;
-    for (int d = lane; d < HD; d += 64)
-      a.po[rec * HD + d] =
-          none ? 0.f : (f[0] * wo[0][r][d] + f[1] * wo[1][r][d]) + (f[2] * wo[2][r][d] + f[3] * wo[3][r][d]);
-    if (lane == 0) *(float2 *)(a.pml + rec * 2) = none ? make_float2(-INFINITY, 0.f) : make_float2(M, L);
+    const int64_t row = (int64_t)token * Hq + h, rec = row * a.parts + part;
+#pragma unroll
+    for (int d = 0; d < HD / 64; ++d) {
+      if (none) v[d] = 0.f;
+      if constexpr (WHOLE)
+        out[row * HD + d * 64 + lane] = Act<T>::st(L == 0.f ? 0.f : v[d] / L);
+      else
+        a.po[rec * HD + d * 64 + lane] = v[d];
+    }
+    if (!WHOLE && lane == 0) *(float2 *)(a.pml + rec * 2) = none ? make_float2(-INFINITY, 0.f) : make_float2(M, L);
   }
 }
 
-template <typename T, int HD>
-constexpr int ROWS_LDS = 4 * 16 * HD * 4 + 512 + 4 * 16 * 40 * 2;
-
 // Decode: shared items of 128 rows, which the matrix cores bound, and items of
 // few rows (the rows' own, and the shared ones of small batches), which memory
-// bounds, dealt out in turn so that a CU has some of each.
+// bounds; the longer ones first.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_decode_kernel(
     const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
-  __shared__ __attribute__((aligned(1024))) char lds[std::max(TILE_LDS<T, HD>, ROWS_LDS<T, HD>)];
+  __shared__ __attribute__((aligned(1024))) char lds[std::max(TILE_LDS<T, HD>, ROWS_LDS<T, HD, 4>)];
   int i = div_by(blockIdx.x, a.by_hkv);
   const int g = blockIdx.x - i * a.b.kv.n_kv_heads;
-  const int tiles = a.tiles * a.splits, rows = a.shared_rows * a.splits + a.otiles * a.osplits;
-  const int both = min(tiles, rows);
-  bool tile = tiles > rows;
-  if (i < 2 * both) {
-    tile = i % 2 == 0;
-    i /= 2;
-  } else {
-    i -= both;
-  }
-  if (tile)
+  const int tiles = a.tiles * a.splits;
+  if (i < tiles)
     tile_item<T, HD, 4>(q, out, a, i, g, lds);
   else
-    rows_item<T, HD>(q, a, i, g, lds);
+    rows_item<T, HD, 4, false>(q, out, a, i - tiles, g, lds);
+}
+
+// Small decode batches: a workgroup of eight waves per row and KV head takes all
+// of its keys, the prefix's too.  Every row reads the prefix for itself, from the
+// L2, and no second launch joins anything.
+template <typename T, int HD>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void prefix_row_kernel(
+    const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[ROWS_LDS<T, HD, 8>];
+  const int i = div_by(blockIdx.x, a.by_hkv);
+  rows_item<T, HD, 8, true>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
 }
 
 // Joins the parts of a (token, head), a wave each: its lanes hold the parts'
@@ -909,6 +946,15 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
 
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
+// A decode batch whose rows each see at most WHOLE_ENTRIES blocks, and whose rows
+// and KV heads are at most WHOLE_ITEMS, takes a workgroup per row and KV head
+// (graphs of calls, 8B heads: 32 rows over 553 + 60 tokens 12.5 us against 16.2
+// in two launches, over 1,000 + 100, 19 blocks, 16.9 against 19.5; one row over
+// 100 + 60 7.0 against 9.4, 553 + 60 10.0 against 9.5, 1,100 + 60 13.0 against
+// 9.6; 64 rows over 553 + 60, 512 workgroups, 22.4 against 20.5; 7B heads, 4 rows
+// over 553 + 60, 128 workgroups, 11.3 against 12.5).
+constexpr int WHOLE_ENTRIES = 12, WHOLE_ITEMS = 256;
+
 // Row tiles and splits.
 static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_heads, int n_kv_heads, int prefix_len,
                         int max_ctx) {
@@ -920,6 +966,10 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   const bool few = half && decode && packed <= 64;
   const int rt = half ? few ? 16 : 128 : 64;
   const int tiles = a.nP ? ceil_div(packed, rt) : 0;
+  if (half && decode && a.nP + own <= WHOLE_ENTRIES && (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads <= WHOLE_ITEMS) {
+    a.whole = 1;
+    return;
+  }
   a.tiles = few ? 0 : tiles;
   a.shared_rows = few ? tiles : 0;
   if (a.nP) {
@@ -929,10 +979,21 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
     a.splits = ceil_div(a.nP, a.sblk);
   }
   a.oblk = std::max(1, own);
+  a.own_log = 2;
+  if (decode && half) {
+    const int64_t pairs = (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads;
+    while (a.own_log && ((pairs << a.own_log) > 512 || 1 << a.own_log > own)) --a.own_log;
+  }
   if (decode) {
     const int want = std::max(1, 512 / (int)std::min((int64_t)rows * n_kv_heads, (int64_t)512));
     a.oblk = std::max(1, ceil_div(own, std::min(want, std::max(1, ceil_div(own, 4)))));
-    if (half) a.oblk = std::min(a.oblk, 64);
+    // Many rows: one wave an item, of four blocks (two waves and up: eight), so
+    // that long rows end with the others; at most 16 parts a row while an item's
+    // 64 blocks allow, for max_ctx far above the rows' contexts.  8B heads, 64
+    // rows of 300 over 2,000 tokens, waves x blocks: 1 x 4 31.6 us, 2 x 4 36.3,
+    // 2 x 8 33.0, 4 x 8 35.6, 4 x all 35.5; 13B heads, 16 of 300: 46.0, -, 49.8,
+    // 46.9, 46.6, 1 x all 81.6.
+    if (half) a.oblk = std::min(std::max(std::min(a.oblk, a.own_log ? 8 : 4), ceil_div(own, 16)), 64);
   }
   if (half && !decode && (int64_t)tiles * n_kv_heads >= 512) {
     a.splits = a.tiles = 0;
@@ -969,24 +1030,27 @@ static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   a.otiles = decode ? b.rows * ceil_div(a.G, rto)
                     : (int)std::min((int64_t)b.n_seq * ceil_div((int64_t)std::min(b.max_new, b.rows) * a.G, rto),
                                     (int64_t)b.rows * a.G / rto + b.n_seq);
+  a.units = decode && half ? ceil_div((int64_t)a.otiles << a.own_log, 4) : a.otiles;
   a.by_g = divisor(a.G);
   a.by_hkv = divisor(Hkv);
   a.by_splits = divisor(a.splits);
   a.by_osplits = divisor(a.osplits);
-  a.by_otiles = divisor(a.otiles);
+  a.by_units = divisor(a.units);
   a.by_shared = divisor(a.shared_rows);
   a.by_per = divisor(ceil_div(a.G, rto));
-  const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.otiles * a.osplits) * Hkv;
+  const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.units * a.osplits) * Hkv;
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
   if constexpr (half) {
-    if (decode)
+    if (a.whole)
+      prefix_row_kernel<T, HD><<<grid((int64_t)a.otiles * Hkv), 512, 0, s>>>(q, out, a);
+    else if (decode)
       prefix_decode_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
     else
       prefix_tile_kernel<T, HD, 4><<<grid(items), 256, 0, s>>>(q, out, a);
   } else {
     prefix_attn_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, a);
   }
-  if (!a.direct)
+  if (!a.direct && !a.whole)
     prefix_join_kernel<T, HD><<<grid(ceil_div((int64_t)b.rows * b.n_heads, 4)), 256, 0, s>>>(out, a);
 }
 
