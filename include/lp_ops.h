@@ -230,7 +230,8 @@ int lp_op_block_tables(const int32_t *seq_slot, const int32_t *cached, const int
  * row_entry, all rounded to dtype once.  K and V of a row with an entry
  * outside 0 .. 64 n_blocks - 1 are left out; of a row with a position outside
  * 0 .. n_pos - 1, everything.  No two rows may have the same entry.  qkv and
- * the tables start on 8 bytes, ld is even; head_dim 64 or 128. */
+ * the tables start on 8 bytes, ld is even; head_dim 64 or 128; rows (Hq + 2
+ * Hkv) at most 2^23. */
 int lp_op_qkv_append(int32_t dtype, const float *qkv, int64_t ld, const float *rope_cos, const float *rope_sin,
                      int32_t n_pos, const int32_t *row_pos, const int64_t *row_entry, int32_t rows, void *q,
                      void *k_cache, void *v_cache, int64_t n_blocks, int32_t n_heads, int32_t n_kv_heads,

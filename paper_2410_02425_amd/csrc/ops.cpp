@@ -240,7 +240,8 @@ extern "C" int lp_op_qkv_append(int32_t dtype, const float *qkv, int64_t ld, con
   OPCHK(head_dim == 64 || head_dim == 128, "qkv append: head_dim must be 64 or 128");
   OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "qkv append: dtype");
   OPCHK(rows >= 0 && n_pos > 0 && n_blocks > 0 && ld % 2 == 0 &&
-            ld >= ((int64_t)n_heads + 2 * (int64_t)n_kv_heads) * head_dim,
+            ld >= ((int64_t)n_heads + 2 * (int64_t)n_kv_heads) * head_dim &&
+            rows * ((int64_t)n_heads + 2 * (int64_t)n_kv_heads) <= 1 << 23,
         "qkv append: sizes");
   if (rows == 0) return LP_OK;  // no rows: nothing is read or written
   OPCHK(qkv && rope_cos && rope_sin && row_pos && row_entry && q && k_cache && v_cache, "qkv append: pointers");
