@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "kernels.hpp"
 
 namespace lp {
@@ -40,6 +42,15 @@ struct Act<f16_t> {
   static __device__ __forceinline__ float ld(f16_t v) { return (float)v; }
   static __device__ __forceinline__ f16_t st(float v) { return (f16_t)v; }
 };
+
+// Rounded to the nearest, NaN of any kind kept.
+template <typename T>
+__device__ __forceinline__ T round_to(float v) {
+  if constexpr (std::is_same_v<T, bf16_t>)
+    return __builtin_bit_cast(T, (__bf16)v);
+  else
+    return (T)v;
+}
 
 // MFMA instructions per 16-bit element type: 16x16x32 and 32x32x16 tiles,
 // fp32 accumulation.
@@ -248,7 +259,6 @@ __device__ __forceinline__ void store_o32(T *dst, const floatx16_t &o, float inv
 // a rounded mc is within 2^-13, which moves a weight of 1 by 8.5e-5, less than
 // its rounding to 16 bits (2.4e-4 in f16).
 constexpr float PFA_LARGE = 4096.f;
-
 
 // Rotary embedding of one pair (x0, x1) = (dimension i, dimension i + hd/2)
 // at angle theta, cs = cos theta, sn = sin theta.  Every kernel that rotates

@@ -135,117 +135,54 @@ __device__ __forceinline__ bool own_tile(const PrefixArgs &a, int u, int &j, int
   return false;
 }
 
-// An entry's block id (-1: none), first position and valid places [lo, hi).
-struct PrefixEntry {
-  int id, base, lo, hi;
-};
-__device__ __forceinline__ PrefixEntry prefix_entry(const PrefixArgs &a, int slot, int e) {
-  PrefixEntry x;
+// An entry's block id, -1 for none.
+__device__ __forceinline__ int prefix_entry(const PrefixArgs &a, int slot, int e) {
+  int id = -1;
   if (e < a.nP) {
-    x.base = e * KV_BLOCK;
-    x.lo = 0;
-    x.hi = min(KV_BLOCK, a.b.prefix_len - x.base);
-    x.id = a.b.prefix_blocks[e];
+    id = a.b.prefix_blocks[e];
   } else {
     const int blk = a.F + e - a.nP;
-    x.base = blk * KV_BLOCK;
-    x.lo = max(0, a.b.prefix_len - x.base);
-    x.hi = KV_BLOCK;
-    x.id = slot >= 0 && slot < a.b.n_slots && blk < a.b.kv.max_blocks
-               ? a.b.kv.block_table[(int64_t)slot * a.b.kv.max_blocks + blk]
-               : -1;
+    if (slot >= 0 && slot < a.b.n_slots && blk < a.b.kv.max_blocks)
+      id = a.b.kv.block_table[(int64_t)slot * a.b.kv.max_blocks + blk];
   }
-  if (x.id < 0 || x.id >= a.b.kv.n_blocks) x.id = -1;
-  return x;
+  return id < a.b.kv.n_blocks ? id : -1;
 }
 
-// One workgroup per (64 packed rows, KV head, entry range); four threads hold a
-// row's dims, the keys go through LDS block by block, with a running maximum.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void prefix_attn_kernel(const T *__restrict__ q, PrefixArgs a) {
-  constexpr int Q4 = HD / 4;  // dims per thread
-  __shared__ T ks[64][HD + 2];
-  __shared__ T vs[64][HD + 2];
-  const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads;
-  int idx = blockIdx.x, j = -1, r0, e0, e1, part, start = 0, n = 0;
-  const int g = idx % Hkv;
-  idx /= Hkv;
-  if (idx < a.tiles * a.splits) {
-    part = idx % a.splits;
-    r0 = idx / a.splits * 64;
-    e0 = part * a.sblk;
-    e1 = min(a.nP, e0 + a.sblk);
-  } else {
-    idx -= a.tiles * a.splits;
-    const int s = idx % a.osplits;
-    if (!own_tile<64>(a, idx / a.osplits, j, r0)) return;
-    seq_rows(a.b, j, start, n);
-    part = a.splits + s;
-    e0 = a.nP + s * a.oblk;
-    e1 = e0 + a.oblk;
-  }
-  const int slot = j < 0 ? -1 : a.b.seq_slot[j];
-  const int qi = threadIdx.x >> 2, qq = threadIdx.x & 3;
-  const PrefixRow w = packed_row(a, start, r0, qi, g);
-  const int seen = packed_ctx(a, j, w.t, n), ctx = max(seen, 0);
-  const bool live = seen >= 0;
-  __shared__ int top;  // the largest context of the tile
-  if (threadIdx.x == 0) top = 0;
-  __syncthreads();
-  atomicMax(&top, ctx);
-  __syncthreads();
-  const int most = top;
-  float qv[Q4], o[Q4];
-  const T *qr = q + ((int64_t)w.token * Hq + w.head) * HD + qq * Q4;
+// Operands come in 16-byte pieces: lane l has row (or column) l % 16, elements
+// E (l / 16) .. of a run of 4 E.  16-bit types: E = 8, one MFMA over 32; fp32: E =
+// 4, four over 4 each, the run taken in the same other order on both sides.
+template <typename T>
+struct Piece {
+  static constexpr int E = 16 / (int)sizeof(T);
+  static __device__ __forceinline__ floatx4_t mma(u32x4_tt a, u32x4_tt b, floatx4_t c) {
+    if constexpr (sizeof(T) == 2) {
+      typedef typename Mfma<T>::v8 v8;
+      return Mfma<T>::m16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c);
+    } else {
 #pragma unroll
-  for (int t = 0; t < Q4; ++t) {
-    qv[t] = live ? Act<T>::ld(qr[t]) : 0.f;
-    o[t] = 0.f;
-  }
-  float mx = -INFINITY, l = 0.f;
-  constexpr float c2 = SCORE_C2<HD>;
-  for (int e = e0; e < e1; ++e) {
-    const PrefixEntry x = prefix_entry(a, slot, e);
-    if (x.base + x.lo >= most) break;
-    if (x.id < 0) continue;
-    const int64_t base = ((int64_t)x.id * Hkv + g) * KV_BLOCK * HD;
-    const T *kbp = (const T *)a.b.kv.k + base;
-    const T *vbp = (const T *)a.b.kv.v + base;
-    __syncthreads();
-    for (int i = threadIdx.x; i < 64 * HD; i += 256) {
-      ks[i / HD][i % HD] = kbp[i];
-      vs[i % 64][i / 64] = vbp[i];
-    }
-    __syncthreads();
-    const int end = min(x.hi, most - x.base);
-    for (int p = x.lo; p < end; ++p) {
-      float sc = 0.f;
-#pragma unroll
-      for (int t = 0; t < Q4; ++t) sc += qv[t] * Act<T>::ld(ks[p][qq * Q4 + t]);
-      sc += __shfl_xor(sc, 1, 64);
-      sc += __shfl_xor(sc, 2, 64);
-      if (x.base + p >= ctx) continue;  // uniform across the 4 threads of a row
-      const float mn = fmaxf(mx, sc);
-      const float corr = mx == mn ? 1.f : __builtin_amdgcn_exp2f((mx - mn) * c2);
-      const float pe = mn == -INFINITY && sc == sc ? 0.f : __builtin_amdgcn_exp2f((sc - mn) * c2);
-      l = l * corr + pe;
-#pragma unroll
-      for (int t = 0; t < Q4; ++t) o[t] = o[t] * corr + pe * Act<T>::ld(vs[p][qq * Q4 + t]);
-      mx = mn;
+      for (int e = 0; e < 4; ++e)
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[e]), __uint_as_float(b[e]), c, 0, 0, 0);
+      return c;
     }
   }
-  if (live) {
-    const int64_t rec = ((int64_t)w.token * Hq + w.head) * a.parts + part;
-    float *dst = a.po + rec * HD + qq * Q4;
-#pragma unroll
-    for (int t = 0; t < Q4; ++t) dst[t] = o[t];
-    if (qq == 0) *(float2 *)(a.pml + rec * 2) = make_float2(mx, l);
+  // word y of a piece of keys k0 ..: the bits of those in [lo, hi)
+  static __device__ __forceinline__ uint32_t keep(int k0, int y, int lo, int hi) {
+    if constexpr (sizeof(T) == 2) {
+      const int key = k0 + 2 * y;
+      return (key >= lo && key < hi ? 0xFFFFu : 0u) | (key + 1 >= lo && key + 1 < hi ? 0xFFFF0000u : 0u);
+    } else {
+      return k0 + y >= lo && k0 + y < hi ? ~0u : 0u;
+    }
   }
-}
+  // whether a word holds an infinity or NaN
+  static __device__ __forceinline__ bool odd(uint32_t w) {
+    if constexpr (std::is_same_v<T, float>) return (w & 0x7F800000u) == 0x7F800000u;
+    constexpr uint32_t X = std::is_same_v<T, bf16_t> ? 0x7F80u : 0x7C00u;
+    return (w & X) == X || (w & X << 16) == X << 16;
+  }
+};
 
-// ------------------------------------------------------------------ 16-bit types
-
-// Many rows over a range of entries, on 32x32x16 MFMAs: a workgroup owns 32 QW
+// Many rows of a 16-bit type over a range of entries, on 32x32x16 MFMAs: a workgroup owns 32 QW
 // packed rows, 32 to a wave, and walks its entries' blocks, which are copied
 // into LDS for all its waves (two stages: the next block lands while the
 // current one is used) in the cache's own order, with the 16-byte pieces of a
@@ -277,104 +214,111 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
   const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads, P = a.b.prefix_len;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int l32 = lane & 31, hh = lane >> 5;
-  int j = -1, r0, e0, e1, part, most = INT_MAX, slot = -1, start = 0, n = a.b.rows;
-  if (idx < a.tiles * a.splits) {
-    const int tile = div_by(idx, a.by_splits);
-    part = idx - tile * a.splits;
-    r0 = tile * RT;
-    e0 = part * a.sblk;
-    e1 = min(a.nP, e0 + a.sblk);
-  } else {
-    idx -= a.tiles * a.splits;
-    const int u = div_by(idx, a.by_osplits), s = idx - u * a.osplits;
-    if (!own_tile<RT>(a, u, j, r0)) return;
-    part = a.splits + s;
-    slot = a.b.seq_slot[j];
-    seq_rows(a.b, j, start, n);
-    most = row_ctx(a.b, j, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
-    e0 = (a.splits ? a.nP : 0) + s * a.oblk;
-    e1 = min(e0 + a.oblk, most > P ? a.nP + (most + KV_BLOCK - 1) / KV_BLOCK - a.F : (most + KV_BLOCK - 1) / KV_BLOCK);
-  }
-  // What the first copies wait for is requested first, with the rows' q: a
-  // walk of few blocks is one memory round trip after the other.
-  const PrefixRow w = packed_row(a, start, r0, wave * 32 + l32, g);
-  v8 qb[KS];  // Q^T as the B operand: this lane's row, dims 16 k + 8 hh ..
-  {
-    const T *qr = q + ((int64_t)(w.t < n ? w.token : 0) * Hq + w.head) * HD + hh * 8;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) qb[k] = load8<T>(qr + k * 16);
-  }
-  // Byte offsets of the entries' blocks (head included), -1 for none: lane i
-  // holds that of entry win + i, the wave reads them back with readlane.
-  int win = e0, off_lo, off_hi;
-  auto window = [&]() __attribute__((always_inline)) {
-    int64_t off = -1;
-    if (win + lane < e1) {
-      const int id = prefix_entry(a, slot, win + lane).id;
-      if (id >= 0) off = ((int64_t)id * Hkv + g) * PB;
+  floatx16_t o[NT];
+  float mref, lsum;
+  int r0 = 0, part = 0, start = 0, seen = -1;
+  PrefixRow w{};
+  int *again = (int *)(lds + 2 * STAGE);
+  // The item from its index to its (m, l, o); returns whether some rows of the
+  // wave saw a block only in part, or leaves early (a tile past the last).
+  // Called again for a tile whose result is not finite, it reads everything
+  // anew: what it kept over the first walk would cost that one's registers.
+  auto item = [&](auto careful_, int idx, bool &none) __attribute__((always_inline)) {
+    constexpr bool careful = decltype(careful_)::value;
+    int j = -1, e0, e1, most = INT_MAX, slot = -1, n = a.b.rows;
+    start = 0;
+    none = false;
+    if (idx < a.tiles * a.splits) {
+      const int tile = div_by(idx, a.by_splits);
+      part = idx - tile * a.splits;
+      r0 = tile * RT;
+      e0 = part * a.sblk;
+      e1 = min(a.nP, e0 + a.sblk);
+    } else {
+      idx -= a.tiles * a.splits;
+      const int u = div_by(idx, a.by_osplits), s = idx - u * a.osplits;
+      if (!own_tile<RT>(a, u, j, r0)) {
+        none = true;
+        return false;
+      }
+      part = a.splits + s;
+      slot = a.b.seq_slot[j];
+      seq_rows(a.b, j, start, n);
+      most = row_ctx(a.b, j, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
+      e0 = (a.splits ? a.nP : 0) + s * a.oblk;
+      const int blocks = (most + KV_BLOCK - 1) / KV_BLOCK;
+      e1 = min(e0 + a.oblk, most > P ? a.nP + blocks - a.F : blocks);
     }
-    off_lo = (int)off;
-    off_hi = (int)(off >> 32);
-    asm volatile("" : "+v"(off_lo), "+v"(off_hi));  // the wait for the load stands here
-  };
-  auto offset = [&](int e) __attribute__((always_inline)) {
-    return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, e - win) << 32) |
-                     (uint32_t)__builtin_amdgcn_readlane(off_lo, e - win));
-  };
-  constexpr int KR = 1024 / (HD * 2);
-  const uint32_t lds0 = lds_addr(lds) + wave * ND * 1024;
-  auto swz = [](int row) __attribute__((always_inline)) { return CK == 16 ? row & 15 : (row >> 1) & 7; };
-  uint32_t ko[ND], vo[ND];  // byte offsets of this lane's pieces inside a block
+    // What the first copies wait for is requested first, with the rows' q: a
+    // walk of few blocks is one memory round trip after the other.
+    w = packed_row(a, start, r0, wave * 32 + l32, g);
+    v8 qb[KS];  // Q^T as the B operand: this lane's row, dims 16 k + 8 hh ..
+    {
+      const T *qr = q + ((int64_t)(w.t < n ? w.token : 0) * Hq + w.head) * HD + hh * 8;
 #pragma unroll
-  for (int c = 0; c < ND; ++c) {
-    const int m = wave * ND + c, kr = m * KR + lane / CK, vr = m * 8 + (lane >> 3);
-    ko[c] = kr * HD * 2 + ((lane % CK) ^ swz(kr)) * 16;
-    vo[c] = vr * KV_BLOCK * 2 + ((lane & 7) ^ ((vr >> 1) & 7)) * 16;
-  }
-  bool have[2];  // the stage holds a block
-  auto issue = [&](int e) __attribute__((always_inline)) {
-    if (e >= win + 64) {
-      win = e;
-      window();
+      for (int k = 0; k < KS; ++k) qb[k] = load8<T>(qr + k * 16);
     }
-    const int64_t off = offset(e);
-    const int b = (e - e0) & 1;
-    have[0] = b ? have[0] : off >= 0;
-    have[1] = b ? off >= 0 : have[1];
-    if (off < 0) return;
-    const uint32_t st = lds0 + b * STAGE;
+    // Byte offsets of the entries' blocks (head included), -1 for none: lane i
+    // holds that of entry win + i, the wave reads them back with readlane.
+    int win = e0, off_lo, off_hi;
+    auto window = [&]() __attribute__((always_inline)) {
+      int64_t off = -1;
+      if (win + lane < e1) {
+        const int id = prefix_entry(a, slot, win + lane);
+        if (id >= 0) off = ((int64_t)id * Hkv + g) * PB;
+      }
+      off_lo = (int)off;
+      off_hi = (int)(off >> 32);
+      asm volatile("" : "+v"(off_lo), "+v"(off_hi));  // the wait for the load stands here
+    };
+    auto offset = [&](int e) __attribute__((always_inline)) {
+      return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, e - win) << 32) |
+                       (uint32_t)__builtin_amdgcn_readlane(off_lo, e - win));
+    };
+    constexpr int KR = 1024 / (HD * 2);
+    const uint32_t lds0 = lds_addr(lds) + wave * ND * 1024;
+    auto swz = [](int row) __attribute__((always_inline)) { return CK == 16 ? row & 15 : (row >> 1) & 7; };
+    uint32_t ko[ND], vo[ND];  // byte offsets of this lane's pieces inside a block
 #pragma unroll
     for (int c = 0; c < ND; ++c) {
-      dma16s((const char *)a.b.kv.k + off, ko[c], st + c * 1024);
-      dma16s((const char *)a.b.kv.v + off, vo[c], st + PB + c * 1024);
+      const int m = wave * ND + c, kr = m * KR + lane / CK, vr = m * 8 + (lane >> 3);
+      ko[c] = kr * HD * 2 + ((lane % CK) ^ swz(kr)) * 16;
+      vo[c] = vr * KV_BLOCK * 2 + ((lane & 7) ^ ((vr >> 1) & 7)) * 16;
     }
-  };
-  auto begin = [&]() __attribute__((always_inline)) {  // the first two blocks
-    win = e0;
-    if (e0 < e1) {
+    bool have[2];  // the stage holds a block
+    auto issue = [&](int e) __attribute__((always_inline)) {
+      if (e >= win + 64) {
+        win = e;
+        window();
+      }
+      const int64_t off = offset(e);
+      const int b = (e - e0) & 1;
+      have[0] = b ? have[0] : off >= 0;
+      have[1] = b ? off >= 0 : have[1];
+      if (off < 0) return;
+      const uint32_t st = lds0 + b * STAGE;
+#pragma unroll
+      for (int c = 0; c < ND; ++c) {
+        dma16s((const char *)a.b.kv.k + off, ko[c], st + c * 1024);
+        dma16s((const char *)a.b.kv.v + off, vo[c], st + PB + c * 1024);
+      }
+    };
+    if (e0 < e1) {  // the first two blocks
       window();
       issue(e0);
       if (e0 + 1 < e1) issue(e0 + 1);
     }
-  };
-  begin();
-  const int seen = packed_ctx(a, j, w.t, n), wctx = max(seen, 0);
-  const bool live = seen >= 0;
-  // rows that do not exist or see nothing (zeros at the end, whatever is summed
-  // for them) ask for no mask
-  const int ctx = wctx ? wctx : INT_MAX;
-  const int ctx_lo = (int)wave_min_u32((uint32_t)ctx);
-  const int ctx_top = (int)~wave_min_u32(~(uint32_t)wctx);
-  const int krow = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
-  const int kfb = krow * HD * 2, kfx = (hh ^ swz(krow)) << 4;
-  const int vfb = l32 * KV_BLOCK * 2, vfx = (hh ^ ((l32 >> 1) & 7)) << 4;
+    seen = packed_ctx(a, j, w.t, n);
+    const int wctx = max(seen, 0);
+    // rows that do not exist or see nothing (zeros at the end, whatever is summed
+    // for them) ask for no mask
+    const int ctx = wctx ? wctx : INT_MAX;
+    const int ctx_lo = (int)wave_min_u32((uint32_t)ctx);
+    const int ctx_top = (int)~wave_min_u32(~(uint32_t)wctx);
+    const int krow = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
+    const int kfb = krow * HD * 2, kfx = (hh ^ swz(krow)) << 4;
+    const int vfb = l32 * KV_BLOCK * 2, vfx = (hh ^ ((l32 >> 1) & 7)) << 4;
 
-  floatx16_t o[NT];
-  float mref, lsum;
-  // the entries' walk; returns whether a block was seen whole by some rows of
-  // the wave only
-  auto walk = [&](auto careful_) __attribute__((always_inline)) {
-    constexpr bool careful = decltype(careful_)::value;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -385,7 +329,6 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
     lsum = 0.f;
     bool large = false;   // wave-uniform: a row's |mc| is past PFA_LARGE
     bool masked = false;  // wave-uniform: a block that only some rows see whole
-    if constexpr (careful) begin();
     for (int e = e0; e < e1; ++e) {
       const bool mine = e < a.nP;
       const int base = mine ? e * KV_BLOCK : (a.F + e - a.nP) * KV_BLOCK;
@@ -491,15 +434,14 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
 #pragma unroll 1
           for (int i = 0; i < 32; ++i) {
             const int lim = __builtin_amdgcn_readlane(end, i);
+            int at = vfb;
+            asm volatile("" : "+v"(at));  // not held in registers over the rows
             floatx16_t acc = o[t];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              u32x4_tt f = *(const u32x4_tt *)(vs + vfb + t * 32 * KV_BLOCK * 2 + (vfx ^ (k << 5)));
+              u32x4_tt f = *(const u32x4_tt *)(vs + at + t * 32 * KV_BLOCK * 2 + (vfx ^ (k << 5)));
 #pragma unroll
-              for (int x = 0; x < 4; ++x) {
-                const int key = k * 16 + hh * 8 + 2 * x;
-                f[x] &= (key < lim ? 0xFFFFu : 0u) | (key + 1 < lim ? 0xFFFF0000u : 0u);
-              }
+              for (int x = 0; x < 4; ++x) f[x] &= Piece<T>::keep(k * 16 + hh * 8, x, 0, lim);
               acc = Mfma<T>::m32(__builtin_bit_cast(v8, f), pb[k], acc);
             }
 #pragma unroll
@@ -518,22 +460,28 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
     }
     return masked;
   };
-  int *again = (int *)(lds + 2 * STAGE);
   if (threadIdx.x == 0) *again = 0;  // before the walk's first barrier, or the one below
-  if (e0 >= e1) __syncthreads();
-  if (walk(std::false_type())) {
+  bool none;
+  const bool masked = item(std::false_type(), idx, none);
+  if (none) return;
+  __syncthreads();
+  if (masked) {
     float z[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) z[r & 3] = fmaf(o[t][r], 0.f, z[r & 3]);
-    if (wctx && !(z[0] + z[1] + (z[2] + z[3]) == 0.f)) *again = 1;
+    if (seen > 0 && !(z[0] + z[1] + (z[2] + z[3]) == 0.f)) *again = 1;
   }
   __syncthreads();  // the last block is used by now: LDS is free below
   if (*again) {
-    walk(std::true_type());
+    int opaque = idx;
+    asm volatile("" : "+s"(opaque));
+    item(std::true_type(), opaque, none);
     __syncthreads();
   }
+  const bool live = seen >= 0;
+  const int wctx = max(seen, 0);
   if (!wctx) {
     mref = -INFINITY;
     lsum = 0.f;
@@ -590,38 +538,45 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   tile_item<T, HD, QW>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
 }
 
-// Few rows over a range of entries, on 16x16x32 MFMAs: up to 16 packed rows of a
-// KV head; wave w takes every NW-th entry from the w-th on, 32 keys at a time.
+// Few rows over a range of entries, on 16x16 MFMAs: up to 16 packed rows of a KV
+// head; wave w takes every NW-th entry from the w-th on, 32 keys at a time.
 // Each wave has its own LDS for K and V of 32 keys: K is copied there while the
 // softmax of the keys before runs, V while the scores do.  (Fragments loaded
 // straight from the cache ask for 16 rows with every four lanes on four lines:
 // 21 bytes a clock and CU, 6,200 clocks per 32 keys with eight waves, against
 // 1,900 with one.)  Online softmax per wave; P goes through LDS into the A
 // operand's layout; the waves' (m, l, o) meet in LDS at the end.  Own items: the
-// query heads of one row.  Shared items (batches of few rows): packed rows.
+// query heads of one row, or in fp32 prefill 16 packed rows of a sequence.
+// Shared items (batches of few rows, and fp32): packed rows.
+
 template <typename T, int HD>
-constexpr int ROWS_KV = 32 * HD * 2;  // bytes of 32 keys, K or V
+constexpr int ROWS_KV = 32 * HD * (int)sizeof(T);  // bytes of 32 keys, K or V
+template <typename T>
+constexpr int ROWS_LP = 32 + 16 / (int)sizeof(T);  // a row of P in LDS
 template <typename T, int HD, int NW>
-constexpr int ROWS_LDS = NW * (2 * ROWS_KV<T, HD> + 16 * 40 * 2 + 2 * 16 * 4);
+constexpr int ROWS_LDS = NW * (2 * ROWS_KV<T, HD> + 16 * ROWS_LP<T> * (int)sizeof(T) + 2 * 16 * 4);
 
 // With WHOLE an item is all that the query heads of one row see, prefix and own
 // entries, and its result goes to out.
 template <typename T, int HD, int NW, bool WHOLE>
 __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict__ out, const PrefixArgs &a, int idx,
                                           int g, char *lds) {
-  typedef typename Mfma<T>::v8 v8;
-  constexpr int KS = HD / 32, NT = HD / 16, LP = 32 + 8;
+  constexpr int S = (int)sizeof(T), E = Piece<T>::E;
+  constexpr int KS = HD / (4 * E), NT = HD / 16, PS = 32 / (4 * E), LP = ROWS_LP<T>;
   constexpr float c2 = SCORE_C2<HD>;
-  constexpr int KV = ROWS_KV<T, HD>, ND = KV / 1024;  // copies of 1 KB
-  constexpr int CK = HD / 8, KR = 64 / CK;            // 16-byte pieces of a K row, rows of a copy
+  constexpr int KV = ROWS_KV<T, HD>, ND = KV / 1024;         // copies of 1 KB
+  constexpr int CK = HD / E, KR = 64 / CK;                   // pieces of a K row, rows of a copy
+  constexpr int CV = 32 / E, VR = 64 / CV;                   // pieces of a V row (32 keys of a dim), rows of a copy
+  constexpr int KX = CK < 16 ? CK - 1 : 15;                  // pieces are XOR-swizzled by the row's low bits
   static_assert(16 * HD * 4 <= 2 * KV, "o of a wave in the place of its K and V");
+  auto vx = [](int row) __attribute__((always_inline)) { return CV == 4 ? (row >> 1) & 3 : row & 7; };
   float *wm = (float *)(lds + NW * 2 * KV), *wl = wm + NW * 16;  // [NW][16] each
   T(*pls)[LP] = (T(*)[LP])(lds + NW * (2 * KV + 2 * 16 * 4));    // [NW * 16][LP]
   const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads, P = a.b.prefix_len;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int r16 = lane & 15, quad = lane >> 4, kq = quad * 8;
+  const int r16 = lane & 15, quad = lane >> 4;
   pls += wave * 16;
-  int j = -1, r0, e0, e1, part = 0, slot = -1;
+  int j = -1, r0, e0, e1, part = 0, slot = -1, start = 0, n = 1;
   const int shared = WHOLE ? 0 : a.shared_rows * a.splits;
   // waves that share an item's entries: all, or of a row's own ones 2^own_log
   int log = NW == 8 ? 3 : 2;
@@ -636,11 +591,17 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
     // all rows' first splits, then their second ones: the grid ends with what few have
     const int s = WHOLE ? 0 : div_by(idx, a.by_units);
     const int u = ((idx - s * a.units) << (WHOLE ? 0 : 2 - log)) + (wave >> log);
-    own_tile<16>(a, min(u, a.otiles - 1), j, r0);
+    // past the last tile (prefill's bound of them is loose): nothing, but for the barrier
+    bool some = u < a.otiles && own_tile<16>(a, u, j, r0);
+    if (!some) j = 0, r0 = 0;
     part = a.splits + s;
     slot = a.b.seq_slot[j];
-    const int ctx = u < a.otiles ? row_ctx(a.b, j, 0) : 0;
-    const int end = ctx > P ? a.nP + (ctx + KV_BLOCK - 1) / KV_BLOCK - a.F : WHOLE ? (ctx + KV_BLOCK - 1) / KV_BLOCK : 0;
+    seq_rows(a.b, j, start, n);
+    if (!some) n = 0;
+    // the last row sees most
+    const int ctx = some ? row_ctx(a.b, j, min(div_by(r0 + 15, a.by_g), n - 1)) : 0;
+    const int blocks = (ctx + KV_BLOCK - 1) / KV_BLOCK;
+    const int end = ctx > P ? a.nP + blocks - a.F : WHOLE ? blocks : 0;
     e0 = WHOLE ? 0 : a.nP + s * a.oblk;
     e1 = WHOLE ? end : min(e0 + a.oblk, end);
   }
@@ -650,36 +611,33 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
   // holds that of entry e0 + i (an item has at most 64).
   int64_t off = -1;
   if (e0 + lane < e1) {
-    const int id = prefix_entry(a, slot, e0 + lane).id;
-    if (id >= 0) off = ((int64_t)id * Hkv + g) * (KV_BLOCK * HD * 2);
+    const int id = prefix_entry(a, slot, e0 + lane);
+    if (id >= 0) off = ((int64_t)id * Hkv + g) * (KV_BLOCK * HD * S);
   }
   const int off_lo = (int)off, off_hi = (int)(off >> 32);
-  const PrefixRow w = packed_row(a, max(j, 0), r0, r16, g);
-  const int seen_ = packed_ctx(a, j, w.t, 1), ctx = max(seen_, 0);
+  const PrefixRow w = packed_row(a, start, r0, r16, g);
+  const int seen_ = packed_ctx(a, j, w.t, n), ctx = max(seen_, 0);
   const bool live = seen_ >= 0;
   const int ctx_top = (int)~wave_min_u32(~(uint32_t)ctx);
   // rows that see nothing get zeros at the end, whatever is summed for them
   const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
-  // the wave's entries that have a block some row sees (and some row its second
-  // half), and those of them that not every row sees whole (rows inside the
-  // prefix), which come after the rest
+  // the wave's entries that have a block some row sees, and some row its second half
   const bool pre = e0 + lane < a.nP;
   const int first = pre ? (e0 + lane) * KV_BLOCK : (a.F + e0 + lane - a.nP) * KV_BLOCK;
   const int from = pre ? 0 : P, to = min(pre ? P : INT_MAX, ctx_top);  // its positions [from, to)
-  const uint64_t mine = ~0ull / ((1ull << (1 << log)) - 1) << nth;  // every 2^log-th
-  const uint64_t seen = __ballot(off >= 0 && first < to) & mine;
+  const uint64_t mine = ~0ull / ((1ull << (1 << log)) - 1) << nth;     // every 2^log-th
+  uint64_t left = __ballot(off >= 0 && first < to) & mine;
   const uint64_t second = __ballot(first + 32 < to);
-  const uint64_t mixed = own ? 0 : seen & __ballot(min(first + KV_BLOCK, to) > ctx_lo);
-  // copies into this wave's LDS, the 16-byte pieces of a row XOR-swizzled
+  // copies into this wave's LDS
   char *ks = lds + wave * 2 * KV, *vs = ks + KV;
   const uint32_t kl = lds_addr(ks), vl = kl + KV;
   uint32_t ko[16 / KR];  // byte offsets of this lane's pieces, rows 0 .. 15
 #pragma unroll
   for (int c = 0; c < 16 / KR; ++c) {
     const int row = c * KR + lane / CK;
-    ko[c] = row * HD * 2 + ((lane % CK) ^ (row & (CK - 1))) * 16;
+    ko[c] = row * HD * S + ((lane % CK) ^ (row & KX)) * 16;
   }
-  const uint32_t vo = (lane >> 2) * KV_BLOCK * 2 + ((lane & 3) ^ ((lane >> 3) & 3)) * 16;
+  const uint32_t vo = lane / CV * KV_BLOCK * S + ((lane % CV) ^ vx(lane / CV)) * 16;
   int64_t at;
   auto place = [&](int i, int h) __attribute__((always_inline)) {  // half h of entry e0 + i
     at = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, i) << 32) |
@@ -687,20 +645,19 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
     return __builtin_amdgcn_readlane(first, i) + h * 32;
   };
   auto copy_k = [&](int h) __attribute__((always_inline)) {
-    const char *kb = (const char *)a.b.kv.k + at + h * 32 * HD * 2;
+    const char *kb = (const char *)a.b.kv.k + at + h * KV;
 #pragma unroll
-    for (int c = 0; c < ND; ++c)
-      dma16s(kb + c / (16 / KR) * 16 * HD * 2, ko[c % (16 / KR)], kl + c * 1024);
+    for (int c = 0; c < ND; ++c) dma16s(kb + c / (16 / KR) * 16 * HD * S, ko[c % (16 / KR)], kl + c * 1024);
   };
   auto copy_v = [&](int h) __attribute__((always_inline)) {
-    const char *vb = (const char *)a.b.kv.v + at + h * 32 * 2;
+    const char *vb = (const char *)a.b.kv.v + at + h * 32 * S;
 #pragma unroll
-    for (int c = 0; c < ND; ++c) dma16s(vb + c * 16 * KV_BLOCK * 2, vo, vl + c * 1024);
+    for (int c = 0; c < ND; ++c) dma16s(vb + c * VR * KV_BLOCK * S, vo, vl + c * 1024);
   };
-  v8 qa[KS];
-  const T *qrow = q + ((int64_t)(live ? w.token : 0) * Hq + w.head) * HD;
+  u32x4_tt qa[KS];
+  const T *qrow = q + ((int64_t)(live ? w.token : 0) * Hq + w.head) * HD + quad * E;
 #pragma unroll
-  for (int k = 0; k < KS; ++k) qa[k] = load8<T>(qrow + k * 32 + kq);
+  for (int k = 0; k < KS; ++k) qa[k] = *(const u32x4_tt *)(qrow + k * 4 * E);
   // row 4 quad + i: running maximum (raw scores) and this lane's share of the
   // sum; o[nt][i]: its dim nt * 16 + r16
   float mx[4], sm[4];
@@ -710,117 +667,121 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
   for (int nt = 0; nt < NT; ++nt) o[nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < 4; ++i) mx[i] = -INFINITY, sm[i] = 0.f, rctx[i] = __shfl(ctx, 4 * quad + i, 64);
-  auto scores = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) s[nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        const v8 f = *(const v8 *)(ks + (nt * 16 + r16) * HD * 2 + (((k * 4 + quad) ^ (r16 & (CK - 1))) * 16));
-        s[nt] = Mfma<T>::m16(qa[k], f, s[nt]);
-      }
-  };
-  // keys [lo, hi) of the 32 at `base`, of entry e0 + i, are there
-  auto bounds = [&](int i, int base, int &lo, int &hi) __attribute__((always_inline)) {
-    lo = max(0, __builtin_amdgcn_readlane(from, i) - base);
-    hi = min(32, __builtin_amdgcn_readlane(to, i) - base);
-  };
-  // s[nt][i]: row 4 quad + i, key nt * 16 + r16, to weights in LDS
-  auto weights = [&](int base, int lo, int hi) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int end = min(hi, rctx[i] - base);
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        const int key = nt * 16 + r16;
-        s[nt][i] = key >= lo && key < end ? s[nt][i] : -INFINITY;
-      }
-      const float v = fmaxf(mx[i], row16_max(fmaxf(s[0][i], s[1][i])));
-      const float m0 = v == -INFINITY ? 0.f : v;
-      const float corr = mx[i] == v ? 1.f : __builtin_amdgcn_exp2f((mx[i] - v) * c2);
-      mx[i] = v;
-      sm[i] *= corr;
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        const float p = __builtin_amdgcn_exp2f((s[nt][i] - m0) * c2);
-        sm[i] += p;
-        pls[4 * quad + i][nt * 16 + r16] = Act<T>::st(p);
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) o[nt][i] *= corr;
-    }
-  };
-  uint64_t left = seen & ~mixed;
   if (left) {
     int i = __builtin_ctzll(left), h = 0, base = place(i, 0);
     copy_k(0);
     copy_v(0);
-    for (int n = __builtin_popcountll(left) + __builtin_popcountll(left & second); n > 0; --n) {
-      int lo, hi, nbase = 0;
-      bounds(i, base, lo, hi);
+    for (int halves = __builtin_popcountll(left) + __builtin_popcountll(left & second); halves > 0; --halves) {
+      // keys [lo, hi) of the 32 at `base` are there
+      const int lo = max(0, __builtin_amdgcn_readlane(from, i) - base);
+      const int hi = min(32, __builtin_amdgcn_readlane(to, i) - base);
+      const int here = base;
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");  // K is there, V may not be
-      scores();
-      if (n > 1) {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) s[nt] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          const char *f = ks + (nt * 16 + r16) * HD * S + (((k * 4 + quad) ^ (r16 & KX)) * 16);
+          s[nt] = Piece<T>::mma(qa[k], *(const u32x4_tt *)f, s[nt]);
+        }
+      if (halves > 1) {
         h = (int)(second >> i & 1) & (h ^ 1);
         left = h ? left : left & (left - 1);
         i = __builtin_ctzll(left);
-        nbase = place(i, h);
+        base = place(i, h);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
         copy_k(h);
       }
-      weights(base, lo, hi);
-      // V outside [lo, hi) is stale and may hold anything, and 0 * NaN is not 0
-      u32x4_tt keep;
+      // s[nt][y]: row 4 quad + y, key nt * 16 + r16, to weights in LDS
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
-        const int key = kq + 2 * y;
-        keep[y] = (key >= lo && key < hi ? 0xFFFFu : 0u) | (key + 1 >= lo && key + 1 < hi ? 0xFFFF0000u : 0u);
+        const int end = min(hi, rctx[y] - here);
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          const int key = nt * 16 + r16;
+          s[nt][y] = key >= lo && key < end ? s[nt][y] : -INFINITY;
+        }
+        const float v = fmaxf(mx[y], row16_max(fmaxf(s[0][y], s[1][y])));
+        const float m0 = v == -INFINITY ? 0.f : v;
+        const float corr = mx[y] == v ? 1.f : __builtin_amdgcn_exp2f((mx[y] - v) * c2);
+        mx[y] = v;
+        sm[y] *= corr;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          const float p = __builtin_amdgcn_exp2f((s[nt][y] - m0) * c2);
+          sm[y] += p;
+          pls[4 * quad + y][nt * 16 + r16] = round_to<T>(p);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) o[nt][y] *= corr;
       }
-      const v8 pa = load8<T>(&pls[r16][kq]);
-      if (n > 1)
+      u32x4_tt pa[PS];
+#pragma unroll
+      for (int k = 0; k < PS; ++k) pa[k] = *(const u32x4_tt *)&pls[r16][(k * 4 + quad) * E];
+      if (halves > 1)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");
       else
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      // V outside [lo, hi) is stale and may hold anything, and 0 * NaN is not 0.
+      // Inside, where rows see different keys, a weight of 0 cancels V unless it
+      // is infinite or NaN: then row by row, each with V of its own keys alone.
+      bool odd = false;
+      if (ctx_lo < here + hi) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const u32x4_tt f = *(const u32x4_tt *)(vs + (nt * 16 + r16) * 64 + ((quad ^ ((r16 >> 1) & 3)) * 16));
-        o[nt] = Mfma<T>::m16(pa, __builtin_bit_cast(v8, f & keep), o[nt]);
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int k = 0; k < PS; ++k) {
+            const int dim = nt * 16 + r16;
+            const u32x4_tt f = *(const u32x4_tt *)(vs + dim * 32 * S + (((k * 4 + quad) ^ vx(dim)) * 16));
+#pragma unroll
+            for (int y = 0; y < 4; ++y) odd |= Piece<T>::odd(f[y]);
+          }
+        odd = __any(odd);
       }
-      if (n > 1) {
+      if (odd) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          int dim = nt * 16 + r16;
+#pragma unroll 1
+          for (int r = 0; r < 16; ++r) {
+            const int lim = min(hi, __builtin_amdgcn_readlane(ctx, r) - here);
+            asm volatile("" : "+v"(dim));  // V is read anew, not held in registers over the rows
+            floatx4_t acc = o[nt];
+#pragma unroll
+            for (int k = 0; k < PS; ++k) {
+              u32x4_tt f = *(const u32x4_tt *)(vs + dim * 32 * S + (((k * 4 + quad) ^ vx(dim)) * 16));
+#pragma unroll
+              for (int y = 0; y < 4; ++y) f[y] &= Piece<T>::keep((k * 4 + quad) * E, y, lo, lim);
+              acc = Piece<T>::mma(pa[k], f, acc);
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y) o[nt][y] = 4 * quad + y == r ? acc[y] : o[nt][y];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < PS; ++k) {
+          u32x4_tt keep;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) keep[y] = Piece<T>::keep((k * 4 + quad) * E, y, lo, hi);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const int dim = nt * 16 + r16;
+            const u32x4_tt f = *(const u32x4_tt *)(vs + dim * 32 * S + (((k * 4 + quad) ^ vx(dim)) * 16));
+            o[nt] = Piece<T>::mma(pa[k], f & keep, o[nt]);
+          }
+        }
+      }
+      if (halves > 1) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
         copy_v(h);
       }
-      base = nbase;
     }
   }
-  // a key at a time, each added to the rows that see it (a weight of 0 does not
-  // cancel V that is infinite or NaN)
-  for (left = mixed; left; left &= left - 1)
-#pragma unroll 1
-    for (int h = 0; h < 2; ++h) {
-      int lo, hi;
-      const int i = __builtin_ctzll(left), base = place(i, h);
-      bounds(i, base, lo, hi);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      copy_k(h);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      scores();
-      weights(base, lo, hi);
-      const T *vb = (const T *)((const char *)a.b.kv.v + at) + r16 * KV_BLOCK + h * 32;
-#pragma unroll 1
-      for (int key = 0; key < hi; ++key) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float v = Act<T>::ld(vb[nt * 16 * KV_BLOCK + key]);
-#pragma unroll
-          for (int y = 0; y < 4; ++y)
-            if (base + key < rctx[y]) o[nt][y] = fmaf(Act<T>::ld(pls[4 * quad + y][key]), v, o[nt][y]);
-        }
-      }
-    }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // o goes where K and V were
-  const int nrows = own ? min(16, a.G - r0) : 16;
+  const int nrows = own && !a.b.seq_start ? min(16, a.G - r0) : 16;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = 4 * quad + i;
@@ -832,7 +793,7 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
     }
   }
   __syncthreads();
-  if (!WHOLE && e0 >= e1) return;  // the join reads no such part
+  if (!WHOLE && !a.b.seq_start && e0 >= e1) return;  // decode's join reads no such part
   // a wave a row: its lanes over the dims
   const int w0 = wave - nth;
   for (int r = nth; r < nrows; r += 1 << log) {
@@ -854,7 +815,7 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
     for (int d = 0; d < HD / 64; ++d) {
       if (none) v[d] = 0.f;
       if constexpr (WHOLE)
-        out[row * HD + d * 64 + lane] = Act<T>::st(L == 0.f ? 0.f : v[d] / L);
+        out[row * HD + d * 64 + lane] = round_to<T>(L == 0.f ? 0.f : v[d] / L);
       else
         a.po[rec * HD + d * 64 + lane] = v[d];
     }
@@ -862,31 +823,39 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
   }
 }
 
-// Decode: shared items of 128 rows, which the matrix cores bound, and items of
-// few rows (the rows' own, and the shared ones of small batches), which memory
-// bounds; the longer ones first.
+// Decode in 16-bit types: shared items of 128 rows, which the matrix cores
+// bound, and items of few rows (the rows' own, and the shared ones of small
+// batches), which memory bounds; the longer ones first.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_decode_kernel(
     const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[std::max(TILE_LDS<T, HD>, ROWS_LDS<T, HD, 4>)];
-  int i = div_by(blockIdx.x, a.by_hkv);
-  const int g = blockIdx.x - i * a.b.kv.n_kv_heads;
-  const int tiles = a.tiles * a.splits;
+  const int i = div_by(blockIdx.x, a.by_hkv), g = blockIdx.x - i * a.b.kv.n_kv_heads, tiles = a.tiles * a.splits;
   if (i < tiles)
     tile_item<T, HD, 4>(q, out, a, i, g, lds);
   else
     rows_item<T, HD, 4, false>(q, out, a, i - tiles, g, lds);
 }
 
-// Small decode batches: a workgroup of eight waves per row and KV head takes all
-// of its keys, the prefix's too.  Every row reads the prefix for itself, from the
-// L2, and no second launch joins anything.
+// Items of few rows alone (fp32, in both phases).
 template <typename T, int HD>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void prefix_row_kernel(
-    const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
-  __shared__ __attribute__((aligned(1024))) char lds[ROWS_LDS<T, HD, 8>];
+__global__ __launch_bounds__(256) void prefix_rows_kernel(const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[ROWS_LDS<T, HD, 4>];
   const int i = div_by(blockIdx.x, a.by_hkv);
-  rows_item<T, HD, 8, true>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
+  rows_item<T, HD, 4, false>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
+}
+
+// Small decode batches: a workgroup of eight waves (four where LDS holds no
+// more) per row and KV head takes all of its keys, the prefix's too.  Every row
+// reads the prefix for itself, from the L2, and no second launch joins anything.
+template <typename T, int HD>
+constexpr int WHOLE_WAVES = HD * sizeof(T) <= 256 ? 8 : 4;
+template <typename T, int HD>
+__global__ __launch_bounds__(512) void prefix_row_kernel(const T *__restrict__ q, T *__restrict__ out,
+                                                           PrefixArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[ROWS_LDS<T, HD, WHOLE_WAVES<T, HD>>];
+  const int i = div_by(blockIdx.x, a.by_hkv);
+  rows_item<T, HD, WHOLE_WAVES<T, HD>, true>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
 }
 
 // Joins the parts of a (token, head), a wave each: its lanes hold the parts'
@@ -939,7 +908,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
   }
   const float inv = L == 0.f ? 0.f : 1.0f / L;
 #pragma unroll
-  for (int d = 0; d < DPL; ++d) out[row * HD + lane * DPL + d] = Act<T>::st(o[d] * inv);
+  for (int d = 0; d < DPL; ++d) out[row * HD + lane * DPL + d] = round_to<T>(o[d] * inv);
 }
 
 // ------------------------------------------------------------------ plan
@@ -963,10 +932,10 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   a.F = prefix_len / KV_BLOCK;
   int own = max_ctx > prefix_len ? ceil_div(max_ctx, KV_BLOCK) - a.F : 0;
   const int64_t packed = (int64_t)rows * a.G;
-  const bool few = half && decode && packed <= 64;
-  const int rt = half ? few ? 16 : 128 : 64;
+  const bool few = !half || (decode && packed <= 64);
+  const int rt = few ? 16 : 128;
   const int tiles = a.nP ? ceil_div(packed, rt) : 0;
-  if (half && decode && a.nP + own <= WHOLE_ENTRIES && (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads <= WHOLE_ITEMS) {
+  if (decode && a.nP + own <= WHOLE_ENTRIES && (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads <= WHOLE_ITEMS) {
     a.whole = 1;
     return;
   }
@@ -980,7 +949,7 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   }
   a.oblk = std::max(1, own);
   a.own_log = 2;
-  if (decode && half) {
+  if (decode) {
     const int64_t pairs = (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads;
     while (a.own_log && ((pairs << a.own_log) > 512 || 1 << a.own_log > own)) --a.own_log;
   }
@@ -993,7 +962,9 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
     // rows of 300 over 2,000 tokens, waves x blocks: 1 x 4 31.6 us, 2 x 4 36.3,
     // 2 x 8 33.0, 4 x 8 35.6, 4 x all 35.5; 13B heads, 16 of 300: 46.0, -, 49.8,
     // 46.9, 46.6, 1 x all 81.6.
-    if (half) a.oblk = std::min(std::max(std::min(a.oblk, a.own_log ? 8 : 4), ceil_div(own, 16)), 64);
+    a.oblk = std::min(std::max(std::min(a.oblk, a.own_log ? 8 : 4), ceil_div(own, 16)), 64);
+  } else if (!half) {
+    a.oblk = std::max(1, std::min(own, 64));
   }
   if (half && !decode && (int64_t)tiles * n_kv_heads >= 512) {
     a.splits = a.tiles = 0;
@@ -1002,18 +973,24 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   }
   a.osplits = ceil_div(own, a.oblk);
   a.parts = a.splits + a.osplits;
-  a.direct = a.parts == 1 && half && !few && (!decode || a.splits);
+  a.direct = a.parts == 1 && !few && (!decode || a.splits);
 }
 
+// Partials of any plan of at most these rows and contexts, so that a workspace
+// for a batch's limits serves its smaller steps.  A row has at most one part per
+// four blocks.  Shared: the splits times the row tiles are about 512 workgroups
+// over the KV heads, so rows times splits stay under 512 x 128 / n_heads where
+// splits are more than one, or, of 64 blocks an item, than nP / 64.  Own: at most
+// 16, or own / 64.
 size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_heads, int head_dim, int prefix_len,
                                  int max_ctx) {
-  size_t most = 0;
-  for (bool half : {false, true}) {
-    PrefixArgs a{};
-    prefix_plan(a, decode, half, rows, n_heads, n_kv_heads, prefix_len, max_ctx);
-    most = std::max(most, (size_t)rows * n_heads * a.parts * (head_dim + 2) * sizeof(float));
-  }
-  return most;
+  const int64_t nP = ceil_div(std::min(prefix_len, max_ctx), KV_BLOCK);
+  const int64_t own = max_ctx > prefix_len ? ceil_div(max_ctx, KV_BLOCK) - prefix_len / KV_BLOCK : 0;
+  const int64_t r = rows, quarter = (own + 3) / 4, each = (own + 63) / 64;
+  const int64_t shared = std::min(r * ((nP + 3) / 4), std::max(r * std::max<int64_t>(1, (nP + 63) / 64),
+                                                               (int64_t)65536 / n_heads));
+  const int64_t of_row = decode ? std::min(quarter, std::max<int64_t>(16, each)) : each;
+  return (size_t)(shared + r * of_row) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
 template <typename T, int HD>
@@ -1026,11 +1003,11 @@ static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   prefix_plan(a, decode, half, b.rows, b.n_heads, Hkv, b.prefix_len, b.max_ctx);
   a.po = ws;
   a.pml = ws + (size_t)b.rows * b.n_heads * a.parts * HD;
-  const int rto = !half ? 64 : decode ? 16 : 128;
+  const int rto = decode || !half ? 16 : 128;
   a.otiles = decode ? b.rows * ceil_div(a.G, rto)
                     : (int)std::min((int64_t)b.n_seq * ceil_div((int64_t)std::min(b.max_new, b.rows) * a.G, rto),
                                     (int64_t)b.rows * a.G / rto + b.n_seq);
-  a.units = decode && half ? ceil_div((int64_t)a.otiles << a.own_log, 4) : a.otiles;
+  a.units = decode ? ceil_div((int64_t)a.otiles << a.own_log, 4) : a.otiles;
   a.by_g = divisor(a.G);
   a.by_hkv = divisor(Hkv);
   a.by_splits = divisor(a.splits);
@@ -1040,15 +1017,15 @@ static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   a.by_per = divisor(ceil_div(a.G, rto));
   const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.units * a.osplits) * Hkv;
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
-  if constexpr (half) {
-    if (a.whole)
-      prefix_row_kernel<T, HD><<<grid((int64_t)a.otiles * Hkv), 512, 0, s>>>(q, out, a);
-    else if (decode)
+  if (a.whole) {
+    prefix_row_kernel<T, HD><<<grid((int64_t)a.otiles * Hkv), WHOLE_WAVES<T, HD> * 64, 0, s>>>(q, out, a);
+  } else if constexpr (half) {
+    if (decode)
       prefix_decode_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
     else
       prefix_tile_kernel<T, HD, 4><<<grid(items), 256, 0, s>>>(q, out, a);
   } else {
-    prefix_attn_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, a);
+    prefix_rows_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
   }
   if (!a.direct && !a.whole)
     prefix_join_kernel<T, HD><<<grid(ceil_div((int64_t)b.rows * b.n_heads, 4)), 256, 0, s>>>(out, a);

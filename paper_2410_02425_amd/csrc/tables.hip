@@ -172,15 +172,6 @@ void launch_block_tables(const TableStep &t, hipStream_t s) {
 
 // ------------------------------------------------------------------ QKV append
 
-// Rounded to the nearest, NaN of any kind kept.
-template <typename T>
-__device__ __forceinline__ T round_to(float v) {
-  if constexpr (std::is_same_v<T, bf16_t>)
-    return __builtin_bit_cast(T, (__bf16)v);
-  else
-    return (T)v;
-}
-
 // W values from / to consecutive places, in one access.
 template <int W>
 struct Floats {
