@@ -859,10 +859,10 @@ __global__ __launch_bounds__(512) void prefix_row_kernel(const T *__restrict__ q
 }
 
 // Joins the parts of a (token, head), a wave each: its lanes hold the parts'
-// weights first, then the dims.
-template <typename T, int HD>
+// weights first, then the dims, U parts requested at a time.
+template <typename T, int HD, int U>
 __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, PrefixArgs a) {
-  constexpr int DPL = HD / 64, U = 16;
+  constexpr int DPL = HD / 64;
   constexpr float c2 = SCORE_C2<HD>;
   const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
@@ -924,6 +924,33 @@ static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // over 553 + 60, 128 workgroups, 11.3 against 12.5).
 constexpr int WHOLE_ENTRIES = 12, WHOLE_ITEMS = 256;
 
+// Blocks of a split of the prefix for `items` tiles and KV heads.  In units of a
+// block's time where two workgroups share a CU (about 2 us), an item of n blocks
+// takes n + 4, 512 run at once, the work spread over them ends half the shortest
+// item after its mean, and a split costs its partials' way to memory and back.
+// Splits are even, or the last one is half as long, so that other items begin
+// where it ends.  Measured (graphs of calls; prompts' rows x tokens of prefix,
+// blocks of a split): 8B 640 x 1,500 6 blocks 53.4 us, 8 46.7, 12 44.0, 24 55.5;
+// 7B 547 x 4,000 16 blocks 96.8, 21 87.4, 24 76.0, 32 82.5; 8B 200 x 2,000 4 blocks
+// 28.7, 8 28.8, 11 32.1; 13B 240 x 1,000 4 blocks 32.6, 6 27.9, 8 29.3.
+static int tile_split(int nP, int64_t items, int64_t rows_heads, int64_t own_items, int own_blocks) {
+  constexpr double FIXED = 4, PART = 1.3e-4;
+  int best = nP;
+  double least = 0;
+  for (int s = 1; s <= ceil_div(nP, 4) && (s == 1 || items * s <= 512); ++s)
+    for (const int n : {ceil_div(nP, s), (int)(nP / (s - 0.5))}) {
+      if (n > nP || n < 1 || ceil_div(nP, n) != s) continue;
+      const double work = (items * (s * FIXED + nP) + own_items * (FIXED + own_blocks)) / 512;
+      const double last = nP - (s - 1) * n;
+      const double t = std::max(n + FIXED, work + (last + FIXED) / 2) + s * rows_heads * PART;
+      if (least == 0 || t < least) {
+        least = t;
+        best = n;
+      }
+    }
+  return best;
+}
+
 // Row tiles and splits.
 static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_heads, int n_kv_heads, int prefix_len,
                         int max_ctx) {
@@ -941,12 +968,17 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   }
   a.tiles = few ? 0 : tiles;
   a.shared_rows = few ? tiles : 0;
-  if (a.nP) {
+  if (a.nP && few) {
     const int want = std::max(1, 512 / std::max(1, tiles * n_kv_heads));
-    a.sblk = ceil_div(a.nP, std::min(want, ceil_div(a.nP, 4)));
-    if (few) a.sblk = std::min(a.sblk, 64);
-    a.splits = ceil_div(a.nP, a.sblk);
+    a.sblk = std::min(ceil_div(a.nP, std::min(want, ceil_div(a.nP, 4))), 64);
+  } else if (a.nP) {
+    // own items: the sequences' tiles, half of the longest's blocks each, or
+    // (decode) a fourth of a workgroup and four blocks a row
+    const int64_t items = (int64_t)tiles * n_kv_heads, rows_heads = (int64_t)rows * n_heads;
+    a.sblk = tile_split(a.nP, items, rows_heads, decode ? (int64_t)rows * n_kv_heads / 4 : items,
+                        decode ? std::min(own, 4) : (own + 1) / 2);
   }
+  a.splits = a.nP ? ceil_div(a.nP, a.sblk) : 0;
   a.oblk = std::max(1, own);
   a.own_log = 2;
   if (decode) {
@@ -1027,8 +1059,13 @@ static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   } else {
     prefix_rows_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
   }
-  if (!a.direct && !a.whole)
-    prefix_join_kernel<T, HD><<<grid(ceil_div((int64_t)b.rows * b.n_heads, 4)), 256, 0, s>>>(out, a);
+  if (!a.direct && !a.whole) {
+    const dim3 joins = grid(ceil_div((int64_t)b.rows * b.n_heads, 4));
+    if (a.parts <= 4)
+      prefix_join_kernel<T, HD, 4><<<joins, 256, 0, s>>>(out, a);
+    else
+      prefix_join_kernel<T, HD, 16><<<joins, 256, 0, s>>>(out, a);
+  }
 }
 
 template <typename T>
