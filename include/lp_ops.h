@@ -240,10 +240,11 @@ int lp_op_qkv_append(int32_t dtype, const float *qkv, int64_t ld, const float *r
 /* Decode attention with a shared prefix: row m of q, out [M][Hq][hd] reads
  * positions 0 .. row_pos[m] of slot row_slot[m], those below P from the
  * prefix's blocks, which are read once for the whole batch.  Contexts longer
- * than max_ctx are clamped to it (max_ctx, prefix_len and M Hq at most 2^30).
- * A row that reads nothing (position -1, no
- * such slot, all its blocks missing) gets zeros.  Any group Hq / Hkv; head_dim
- * 64 or 128 in every dtype; 64 * max_blocks >= max_ctx where max_ctx > P.
+ * than max_ctx are clamped to it (max_ctx, prefix_len and M Hq at most 2^30;
+ * sizes whose work fills 2^23 workgroups, from M Hq = 2^25 on, are refused).
+ * A row that reads nothing (position -1, no such slot, all its blocks missing)
+ * gets zeros.  Any group Hq / Hkv; head_dim 64 or 128 in every dtype;
+ * 64 * max_blocks >= max_ctx where max_ctx > P.
  * ws: at least lp_op_prefix_decode_attention_ws_bytes of the same sizes (0
  * for sizes that are refused). */
 size_t lp_op_prefix_decode_attention_ws_bytes(int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -263,7 +264,7 @@ int lp_op_prefix_decode_attention(int32_t dtype, const void *q, void *out, const
  * the prefix, one longer than it, or none of it).  Contexts and rows that read
  * nothing as for decode.  max_new bounds the rows of every sequence (rows of a
  * longer one from max_new on hold no result); rows of no sequence stay as they
- * are.  seq_start ascends; what of it lies outside 0 .. rows is left out. */
+ * are.  Sizes as for decode.  seq_start ascends; what of it lies outside 0 .. rows is left out. */
 size_t lp_op_prefix_prefill_attention_ws_bytes(int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                                int32_t prefix_len, int32_t max_ctx);
 int lp_op_prefix_prefill_attention(int32_t dtype, const void *q, void *out, const void *k_cache, const void *v_cache,

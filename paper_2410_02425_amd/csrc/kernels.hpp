@@ -167,8 +167,9 @@ struct PrefixBatch {
 };
 size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_heads, int head_dim, int prefix_len,
                                  int max_ctx);
+// False, with nothing launched, where the sizes need more workgroups than a launch may have.
 template <typename T>
-void launch_prefix_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s);
+bool launch_prefix_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s);
 
 // Block tables, row offsets and cache entries of a step (see lp_op_block_tables).
 struct TableStep {

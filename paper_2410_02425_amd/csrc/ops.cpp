@@ -208,7 +208,7 @@ extern "C" int lp_op_init_weight(int32_t dtype, void *dst, uint64_t seed, int32_
 
 // ------------------------------------------------------------------ a batch that shares a prefix
 
-constexpr int32_t PREFIX_MAX_POS = 1 << 30;  // prefix and context lengths, (row, head) pairs
+constexpr int32_t PREFIX_MAX_POS = 1 << 30;  // prefix and context lengths, sequences, (row, head) pairs
 
 static bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
 
@@ -218,7 +218,8 @@ extern "C" int lp_op_block_tables(const int32_t *seq_slot, const int32_t *cached
                                   int32_t *block_table, int32_t n_slots, int32_t max_blocks, int32_t *seq_start,
                                   int32_t *free_start, int32_t *row_slot, int32_t *row_pos, int64_t *row_entry,
                                   int32_t max_rows, void *stream) {
-  OPCHK(n_seq >= 0 && prefix_len >= 0 && prefix_len <= PREFIX_MAX_POS && n_free >= 0 && n_slots > 0 && max_blocks > 0 && max_rows >= 0,
+  OPCHK(n_seq >= 0 && n_seq <= PREFIX_MAX_POS && prefix_len >= 0 && prefix_len <= PREFIX_MAX_POS && n_free >= 0 &&
+            n_slots > 0 && max_blocks > 0 && max_rows >= 0,
         "block tables: sizes");
   if (n_seq == 0) return LP_OK;  // no sequences: nothing is read or written
   OPCHK(seq_slot && cached && lengths && free_head && block_table && seq_start && free_start,
@@ -284,7 +285,7 @@ static int prefix_attention(int32_t dtype, const void *q, void *out, const Prefi
   OPCHK(prefix_sizes(b.rows, b.n_heads, b.kv.n_kv_heads, b.kv.head_dim, b.prefix_len, b.max_ctx),
         "prefix attention: sizes (rows, heads, head_dim 64 or 128, prefix_len, max_ctx)");
   OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "prefix attention: dtype");
-  OPCHK(b.n_seq >= 0 && b.kv.n_blocks > 0 && b.n_slots > 0 && b.max_new > 0, "prefix attention: sizes");
+  OPCHK(b.n_seq >= 0 && b.n_seq <= PREFIX_MAX_POS && b.kv.n_blocks > 0 && b.n_slots > 0 && b.max_new > 0, "prefix attention: sizes");
   OPCHK(b.kv.max_blocks > 0 && (b.max_ctx <= b.prefix_len || (int64_t)b.kv.max_blocks * KV_BLOCK >= b.max_ctx),
         "prefix attention: max_blocks too small for max_ctx");
   if (b.rows == 0 || b.n_seq == 0) return LP_OK;  // no rows: nothing is read or written
@@ -297,12 +298,14 @@ static int prefix_attention(int32_t dtype, const void *q, void *out, const Prefi
                                                 b.prefix_len, b.max_ctx);
   OPCHK(need == 0 || (ws && ws_bytes >= need), "prefix attention: ws");
   hipStream_t s = (hipStream_t)stream;
+  bool fits;
   if (dtype == LP_BF16)
-    launch_prefix_attention<bf16_t>((const bf16_t *)q, (bf16_t *)out, b, (float *)ws, s);
+    fits = launch_prefix_attention<bf16_t>((const bf16_t *)q, (bf16_t *)out, b, (float *)ws, s);
   else if (dtype == LP_F16)
-    launch_prefix_attention<f16_t>((const f16_t *)q, (f16_t *)out, b, (float *)ws, s);
+    fits = launch_prefix_attention<f16_t>((const f16_t *)q, (f16_t *)out, b, (float *)ws, s);
   else
-    launch_prefix_attention<float>((const float *)q, (float *)out, b, (float *)ws, s);
+    fits = launch_prefix_attention<float>((const float *)q, (float *)out, b, (float *)ws, s);
+  OPCHK(fits, "prefix attention: more rows, heads and blocks than one launch takes");
   return op_status();
 }
 

@@ -182,9 +182,9 @@ struct Piece {
   }
 };
 
-// Many rows of a 16-bit type over a range of entries, on 32x32x16 MFMAs: a workgroup owns 32 QW
-// packed rows, 32 to a wave, and walks its entries' blocks, which are copied
-// into LDS for all its waves (two stages: the next block lands while the
+// Many rows of a 16-bit type over a range of entries, on 32x32x16 MFMAs: a
+// workgroup owns 128 packed rows, 32 to a wave, and walks its entries' blocks,
+// which are copied into LDS for all its waves (two stages: the next block lands while the
 // current one is used) in the cache's own order, with the 16-byte pieces of a
 // row XOR-swizzled against bank conflicts.
 //   S^T = K Q^T: a lane holds one row's scores, so the softmax's maximum and sum
@@ -199,11 +199,11 @@ struct Piece {
 // are not: their weight is 0 for the others, which is enough unless V is
 // infinite or NaN there.  A tile whose result is not finite is therefore
 // computed again with every row's own V (`careful`), once.
-template <typename T, int HD, int QW>
+template <typename T, int HD>
 __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict__ out, const PrefixArgs &a, int idx,
                                           int g, char *lds) {
   typedef typename Mfma<T>::v8 v8;
-  constexpr int RT = QW * 32;
+  constexpr int QW = 4, RT = QW * 32;  // waves, rows
   constexpr int KS = HD / 16;         // contraction steps of S over head_dim
   constexpr int NT = HD / 32;         // 32-dim tiles of O^T
   constexpr int CK = HD / 8;          // 16-byte pieces of a K row
@@ -498,9 +498,8 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
 #pragma unroll
     for (int t = 0; t < NT; ++t) store_o32(out + row * HD + t * 32, o[t], inv, hh, live);
   } else {
-    // Through LDS, so that a row's dims leave as one run of bytes (16 bytes a
-    // lane and row at a time took 1.9 us of a one-block item): 16-byte pieces
-    // XOR-swizzled by the row, the wave's 32 rows in a place of its own.
+    // Through LDS, so that a row's dims leave as one run of bytes: 16-byte
+    // pieces XOR-swizzled by the row, the wave's 32 rows in a place of its own.
     constexpr int LR = HD / 4, RI = 64 / LR;  // lanes of a row, rows of a store
     char *own = lds + wave * 32 * HD * 4;
 #pragma unroll
@@ -513,8 +512,6 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
       }
     if (live && hh == 0) *(float2 *)(a.pml + (row * a.parts + part) * 2) = make_float2(mref, sum);
     const uint32_t rows_live = (uint32_t)__ballot(live);
-    // rolled up: the launch's first pass over code costs about 90 clocks per 64
-    // bytes, and this runs once
 #pragma unroll 4
     for (int i = 0; i < 32 / RI; ++i) {
       const int x = i * RI + lane / LR;
@@ -529,13 +526,13 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
 template <typename T, int HD>
 constexpr int TILE_LDS = 4 * 64 * HD * 2 + 16;  // two stages of K and V, a flag
 
-template <typename T, int HD, int QW>
-__global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) void prefix_tile_kernel(
+template <typename T, int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_tile_kernel(
     const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[TILE_LDS<T, HD>];
   // KV head fastest: with 8 of them each XCD's L2 holds one head's blocks
   const int i = div_by(blockIdx.x, a.by_hkv);
-  tile_item<T, HD, QW>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
+  tile_item<T, HD>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
 }
 
 // Few rows over a range of entries, on 16x16 MFMAs: up to 16 packed rows of a KV
@@ -832,7 +829,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
   __shared__ __attribute__((aligned(1024))) char lds[std::max(TILE_LDS<T, HD>, ROWS_LDS<T, HD, 4>)];
   const int i = div_by(blockIdx.x, a.by_hkv), g = blockIdx.x - i * a.b.kv.n_kv_heads, tiles = a.tiles * a.splits;
   if (i < tiles)
-    tile_item<T, HD, 4>(q, out, a, i, g, lds);
+    tile_item<T, HD>(q, out, a, i, g, lds);
   else
     rows_item<T, HD, 4, false>(q, out, a, i - tiles, g, lds);
 }
@@ -937,7 +934,8 @@ static int tile_split(int nP, int64_t items, int64_t rows_heads, int64_t own_ite
   constexpr double FIXED = 4, PART = 1.3e-4;
   int best = nP;
   double least = 0;
-  for (int s = 1; s <= ceil_div(nP, 4) && (s == 1 || items * s <= 512); ++s)
+  for (int s = 1; s <= ceil_div(nP, 4) && (s == 1 || items * s <= 512); ++s) {
+    if (s > 1 && items * (s * FIXED + nP) / 512 + s * rows_heads * PART > least) break;  // more only cost more
     for (const int n : {ceil_div(nP, s), (int)(nP / (s - 0.5))}) {
       if (n > nP || n < 1 || ceil_div(nP, n) != s) continue;
       const double work = (items * (s * FIXED + nP) + own_items * (FIXED + own_blocks)) / 512;
@@ -948,6 +946,7 @@ static int tile_split(int nP, int64_t items, int64_t rows_heads, int64_t own_ite
         best = n;
       }
     }
+  }
   return best;
 }
 
@@ -959,7 +958,11 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   a.F = prefix_len / KV_BLOCK;
   int own = max_ctx > prefix_len ? ceil_div(max_ctx, KV_BLOCK) - a.F : 0;
   const int64_t packed = (int64_t)rows * a.G;
-  const bool few = !half || (decode && packed <= 64);
+  // Shared items of 16 rows in fp32 (prefix_rows_kernel), and for up to two of
+  // them (graphs of calls, packed rows: 16-row items against 128-row ones): 8B 8
+  // rows over 2,000 tokens (32) 15.5 us against 16.9; 8B 16 rows (64) 18.6 and
+  // 18.8; 13B 64 rows over 8,000 (64) 101 and 79; 70B 16 rows over 8,000 (128) 32 and 24.
+  const bool few = !half || (decode && packed <= 32);
   const int rt = few ? 16 : 128;
   const int tiles = a.nP ? ceil_div(packed, rt) : 0;
   if (decode && a.nP + own <= WHOLE_ENTRIES && (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads <= WHOLE_ITEMS) {
@@ -969,6 +972,7 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   a.tiles = few ? 0 : tiles;
   a.shared_rows = few ? tiles : 0;
   if (a.nP && few) {
+    // about 512 workgroups, of four blocks (a wave each, or 128 keys) and up
     const int want = std::max(1, 512 / std::max(1, tiles * n_kv_heads));
     a.sblk = std::min(ceil_div(a.nP, std::min(want, ceil_div(a.nP, 4))), 64);
   } else if (a.nP) {
@@ -998,6 +1002,11 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   } else if (!half) {
     a.oblk = std::max(1, std::min(own, 64));
   }
+  // Prompts whose tiles fill two workgroups a CU walk the prefix and their own
+  // blocks in one item, and nothing is joined: 70B three prompts of 2,100 over
+  // 4,096 tokens 686 us against 800, 13B eight of 250 over 1,000 97 against 121; with
+  // fewer the prefix's splits share the work better: 70B 32 of 30 over 2,000, 480
+  // tiles, 107 us in splits, 125 in one walk (13B two of 800 over 3,000: 167 and 145).
   if (half && !decode && (int64_t)tiles * n_kv_heads >= 512) {
     a.splits = a.tiles = 0;
     own += a.nP;
@@ -1026,7 +1035,7 @@ size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_he
 }
 
 template <typename T, int HD>
-static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s) {
+static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s) {
   PrefixArgs a{};
   a.b = b;
   const int Hkv = b.kv.n_kv_heads;
@@ -1048,6 +1057,8 @@ static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   a.by_shared = divisor(a.shared_rows);
   a.by_per = divisor(ceil_div(a.G, rto));
   const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.units * a.osplits) * Hkv;
+  const int64_t joins = ((int64_t)b.rows * b.n_heads + 3) / 4;
+  if (std::max(items, joins) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads, 512 to a workgroup
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
   if (a.whole) {
     prefix_row_kernel<T, HD><<<grid((int64_t)a.otiles * Hkv), WHOLE_WAVES<T, HD> * 64, 0, s>>>(q, out, a);
@@ -1055,28 +1066,25 @@ static void launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
     if (decode)
       prefix_decode_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
     else
-      prefix_tile_kernel<T, HD, 4><<<grid(items), 256, 0, s>>>(q, out, a);
+      prefix_tile_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
   } else {
     prefix_rows_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
   }
   if (!a.direct && !a.whole) {
-    const dim3 joins = grid(ceil_div((int64_t)b.rows * b.n_heads, 4));
     if (a.parts <= 4)
-      prefix_join_kernel<T, HD, 4><<<joins, 256, 0, s>>>(out, a);
+      prefix_join_kernel<T, HD, 4><<<grid(joins), 256, 0, s>>>(out, a);
     else
-      prefix_join_kernel<T, HD, 16><<<joins, 256, 0, s>>>(out, a);
+      prefix_join_kernel<T, HD, 16><<<grid(joins), 256, 0, s>>>(out, a);
   }
+  return true;
 }
 
 template <typename T>
-void launch_prefix_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s) {
-  if (b.kv.head_dim == 128)
-    launch_prefix_hd<T, 128>(q, out, b, ws, s);
-  else
-    launch_prefix_hd<T, 64>(q, out, b, ws, s);
+bool launch_prefix_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s) {
+  return b.kv.head_dim == 128 ? launch_prefix_hd<T, 128>(q, out, b, ws, s) : launch_prefix_hd<T, 64>(q, out, b, ws, s);
 }
 
-#define INST(T) template void launch_prefix_attention<T>(const T *, T *, const PrefixBatch &, float *, hipStream_t);
+#define INST(T) template bool launch_prefix_attention<T>(const T *, T *, const PrefixBatch &, float *, hipStream_t);
 INST(float)
 INST(bf16_t)
 INST(f16_t)

@@ -7,6 +7,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
+import test_device_code as device_code
 from oracle import transformer as T
 from paper_2410_02425_amd import lp
 
@@ -690,6 +691,187 @@ def test_two_streams_at_once():
         assert all(torch.equal(o, alone[k]) for o in outs[k])
 
 
+# ------------------------------------------------------------------ calls of other shapes
+
+@gpu
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,n", [("f16", 8, 2, 128, 40), ("bf16", 16, 16, 64, 45), ("f32", 24, 1, 64, 12)])
+def test_decode_batches_of_odd_rows(dtype, Hq, Hkv, hd, n):
+    """Rows inside the prefix before and behind an infinite value, padding rows,
+    the same slot twice, a max_ctx and a table far above any context."""
+    rng = np.random.default_rng(n)
+    P, bad = 700, 300
+    ctx = [P + 1 + 29 * i for i in range(n)]
+    b = Batch(rng, dtype, Hkv, hd, P, ctx)
+    b.table = np.concatenate([b.table, np.full((b.table.shape[0], 1500), -1)], axis=1)
+    rows = [(j, c - 1) for j, c in enumerate(ctx)]
+    rows += [(0, -1), (1, 12), (1, bad - 1), (1, bad), (2, 64), (2, 64), (0, -5), (3, ctx[3] - 1), (3, 0), (4, P - 1)]
+    q = values(rng, (len(rows), Hq, hd), dtype)
+
+    def check(got, m):
+        j, p = rows[m]
+        ref, tol = b.reference(q[m:m + 1], j, [p])
+        assert np.all(np.abs(got[m:m + 1] - ref) <= tol), (m, np.nanmax(np.abs(got[m:m + 1] - ref) / tol))
+
+    b.clean = b.vc.clone()
+    for top in (None, b.table.shape[1] * 64):
+        got = run_decode(b, q, rows, Hq, max_ctx=top)
+        for m, (_, p) in enumerate(rows):
+            if p < 0:
+                assert np.all(got[m] == 0)
+            else:
+                check(got, m)
+        b.vc[int(b.pre[bad // 64]), :, :, bad % 64] = float("inf")
+        got = run_decode(b, q, rows, Hq, max_ctx=top)
+        for m, (_, p) in enumerate(rows):
+            if p < 0:
+                assert np.all(got[m] == 0)
+            elif p < bad:
+                check(got, m)
+            else:
+                assert not np.isfinite(got[m]).any()
+        b.vc.copy_(b.clean)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,P,seqs", [
+    ("f16", 64, 64, 64, 130, [(0, 900), (-30, 100), (3, 0), (40, 17)]),
+    ("bf16", 64, 8, 128, 70, [(0, 1), (0, 1000), (200, 90)]),
+    ("f32", 8, 8, 64, 200, [(0, 150), (0, 0), (0, 0), (-200, 90)]),
+])
+def test_prefill_of_many_rows(dtype, Hq, Hkv, hd, P, seqs):
+    """Batches whose tiles fill the GPU, with sequences that have no new row,
+    infinite values behind some rows, and a max_ctx and max_new above any."""
+    rng = np.random.default_rng(Hq + P)
+    b = Batch(rng, dtype, Hkv, hd, P, [P + c + n for c, n in seqs])
+    rows = 3 + sum(n for _, n in seqs) + 2
+    q = values(rng, (rows, Hq, hd), dtype)
+    calls = [(j, P + c, n) for j, (c, n) in enumerate(seqs)]
+    got = run_prefill(b, q, calls, Hq, start=3, tail=2)
+    big = run_prefill(b, q, calls, Hq, start=3, tail=2, max_ctx=b.table.shape[1] * 64, max_new=5000)
+    for out in (got, big):
+        assert np.all(out[:3] == 7) and np.all(out[-2:] == 7)
+    # every 7th row and the last ones
+    r, long = 3, max(range(len(seqs)), key=lambda j: seqs[j][1])
+    for j, p, n in calls:
+        some = np.unique(np.concatenate([np.arange(0, n, 7), np.arange(max(0, n - 3), n)])).astype(int)
+        if n:
+            ref, tol = b.reference(q[r:r + n][some], j, p + some)
+            for out in (got, big):
+                assert np.all(np.abs(out[r:r + n][some] - ref) <= tol), j
+        if j == long:
+            first = r
+        r += n
+    j, p, n = calls[long]
+    at = p + n // 2
+    blk = b.table[b.slot[j], at // 64] if at >= P else b.pre[at // 64]
+    b.vc[int(blk), :, :, at % 64] = float("-inf")
+    odd = run_prefill(b, q, calls, Hq, start=3, tail=2)
+    behind = np.arange(first + n // 2, first + n)
+    assert not np.isfinite(odd[behind]).any()
+    before = np.setdiff1d(np.arange(rows), behind)
+    assert np.array_equal(odd[before], got[before])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_rows_past_max_new(dtype):
+    """Of a sequence with more rows than max_new the first max_new are right,
+    and those of the next sequences."""
+    rng = np.random.default_rng(8)
+    P, Hq, Hkv, hd = 100, 8, 2, 64
+    b = Batch(rng, dtype, Hkv, hd, P, [P + 90, P + 20])
+    q = values(rng, (112, Hq, hd), dtype)
+    got = run_prefill(b, q, [(0, P, 90), (1, P, 20)], Hq, max_new=40, tail=2)
+    for j, r, n in ((0, 0, 40), (1, 90, 20)):
+        ref, tol = b.reference(q[r:r + n], j, np.arange(P, P + n))
+        assert np.all(np.abs(got[r:r + n] - ref) <= tol)
+    assert np.all(got[110:] == 7)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_caches_past_4_gib(dtype):
+    """Blocks whose byte (f32: also element) offsets pass 32 bits: what a small cache gives, to the bit."""
+    rng = np.random.default_rng(21)
+    Hq, Hkv, hd, P = 16, 8, 128, 200
+    ctx = [P + 1 + 40 * i for i in range(12)]
+    b = Batch(rng, dtype, Hkv, hd, P, ctx)
+    n = 34000                     # of 131,072 or 262,144 bytes
+    big_k = torch.empty(n, Hkv, 64, hd, dtype=TYPES[dtype], device=DEV)
+    big_v = torch.empty(n, Hkv, hd, 64, dtype=TYPES[dtype], device=DEV)
+    big_k[-b.n_blocks:] = b.kc
+    big_v[-b.n_blocks:] = b.vc
+    up = n - b.n_blocks
+
+    def call(f, *args):
+        small = f(b, *args)
+        keep = b.kc, b.vc, b.pre, b.pre_t, b.table
+        b.kc, b.vc, b.pre, b.pre_t, b.table = big_k, big_v, b.pre + up, b.pre_t + up, np.where(b.table >= 0, b.table + up, -1)
+        large = f(b, *args)
+        b.kc, b.vc, b.pre, b.pre_t, b.table = keep
+        assert np.isfinite(small).all() and np.array_equal(small, large)
+
+    q = values(rng, (700, Hq, hd), dtype)
+    for m in (2, 12):             # few rows, and many
+        call(run_decode, q[:m], [(j, ctx[j] - 1) for j in range(m)], Hq)
+    rows = [(j, ctx[j] - 1) for j in range(12)] * 12
+    call(run_decode, q[:144], rows, Hq)
+    call(run_prefill, q[:100], [(0, P, 1), (11, 300, 99)], Hq)
+    entry = torch.arange(n * 64 - 70, n * 64 - 5, dtype=torch.int64, device=DEV)
+    qkv = torch.randn(65, (Hq + 2 * Hkv) * hd, device=DEV)
+    cos, sin = (torch.from_numpy(x).to(DEV) for x in rope_tables(65, hd))
+    pos, qo = torch.arange(65, dtype=torch.int32, device=DEV), torch.empty(65, Hq, hd, dtype=TYPES[dtype], device=DEV)
+    lp.op_qkv_append(qkv, cos, sin, pos, entry, qo, big_k, big_v)
+    small_k, small_v = torch.zeros_like(big_k[:2]), torch.zeros_like(big_v[:2])
+    lp.op_qkv_append(qkv, cos, sin, pos, entry - (n - 2) * 64, qo, small_k, small_v)
+    for s in (0, 1):
+        lo, hi = (58, 64) if s == 0 else (0, 59)
+        assert torch.equal(big_k[n - 2 + s][:, lo:hi], small_k[s][:, lo:hi])
+        assert torch.equal(big_v[n - 2 + s][:, :, lo:hi], small_v[s][:, :, lo:hi])
+        assert small_k[s][:, lo:hi].any()
+
+
+@gpu
+def test_graphs_that_share_a_workspace():
+    """A prefill and a decode step captured with the same workspace, replayed in
+    turn with eager work between, against the eager results."""
+    rng = np.random.default_rng(30)
+    Hq, Hkv, hd, P, n = 32, 8, 128, 900, 20
+    b = Batch(rng, "f16", Hkv, hd, P, [P + 60 + i for i in range(n)])
+    table, slot, top, new = i32(b.table), i32(b.slot), P + 100, 30
+    qp = torch.from_numpy(values(rng, (n * new, Hq, hd), "f16")).half().to(DEV)
+    qd = torch.from_numpy(values(rng, (n, Hq, hd), "f16")).half().to(DEV)
+    start, first = i32(np.arange(n + 1) * new), i32([P + 10] * n)
+    pos = i32([P + 59 + i for i in range(n)])
+    ws = torch.empty(max(lp.prefix_decode_attention_ws_bytes(n, Hq, Hkv, hd, P, top),
+                         lp.prefix_prefill_attention_ws_bytes(n * new, Hq, Hkv, hd, P, top)), dtype=torch.uint8, device=DEV)
+    outs = [torch.zeros_like(qp), torch.zeros_like(qd)]
+
+    def prefill():
+        lp.op_prefix_prefill_attention(qp, outs[0], b.kc, b.vc, b.pre_t, P, table, start, slot, first, new, top, ws)
+
+    def decode():
+        lp.op_prefix_decode_attention(qd, outs[1], b.kc, b.vc, b.pre_t, P, table, slot, pos, top, ws)
+
+    want, graphs = [], []
+    for k, f in enumerate((prefill, decode)):
+        f()
+        torch.cuda.synchronize()
+        want.append(outs[k].clone())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            f()
+        graphs.append(graph)
+    for _ in range(4):
+        for k in (0, 1):
+            outs[k].fill_(9)
+            ws.random_(0, 256)
+            graphs[k].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(outs[k], want[k])
+            assert torch.isfinite(outs[k]).all()
+
+
 # ------------------------------------------------------------------ refusals (no GPU is touched)
 
 F16, F32, OK, EINVAL = lp.LP_F16, lp.LP_F32, lp.LP_OK, lp.LP_EINVAL
@@ -707,7 +889,8 @@ def test_block_tables_refusals():
 
     assert call(n=0) == OK
     assert f(None, None, None, 0, None, 0, None, 0, None, None, 1, 1, None, None, None, None, None, 0, None) == OK
-    for bad in (dict(n=-1), dict(P=-1), dict(P=(1 << 30) + 1), dict(n_free=-1), dict(n_slots=0), dict(wide=0), dict(max_rows=-1)):
+    for bad in (dict(n=-1), dict(P=-1), dict(P=(1 << 30) + 1), dict(n_free=-1), dict(n_slots=0), dict(wide=0),
+                dict(max_rows=-1), dict(n=(1 << 30) + 1)):
         assert call(**bad) == EINVAL, bad
         assert call(n=0, **{k: v for k, v in bad.items() if k != "n"}) == (EINVAL if "n" not in bad else OK)
     for k in ("slot", "cached", "lengths", "pre", "free", "head", "table", "seq_start", "free_start", "row_slot",
@@ -801,3 +984,23 @@ def test_binding_refuses_shapes_on_the_gpu():
     with pytest.raises(lp.LPError):
         lp.op_prefix_decode_attention(**{**good, "ws": ws[:64]})
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("decode", [True, False])
+def test_work_past_one_launch_is_refused(decode):
+    """Sizes within the limits each, whose workgroups together are too many."""
+    L = lp.lib()
+    f = L.lp_op_prefix_decode_attention if decode else L.lp_op_prefix_prefill_attention
+    for dtype, rows, Hq, Hkv, P, ctx in ((F16, 1 << 22, 8, 2, 100, 500), (F32, 1 << 20, 16, 16, 1 << 20, (1 << 20) + 70),
+                                         (F16, 1 << 20, 16, 16, 64, 1 << 29), (F32, 1 << 22, 8, 2, 0, 500)):
+        if dtype == F16 and rows == 1 << 20 and not decode:
+            continue                      # one workgroup takes all blocks of a tile there
+        seqs = [A, A, rows] if decode else [A, A, A, rows, rows, 1]
+        args = [dtype, A, A, A, A, 50, A, P, A, 4, 1 << 24, *seqs, Hq, Hkv, 64, ctx, A, 1 << 60, None]
+        assert f(*args) == EINVAL, (dtype, rows)
+        assert "launch" in L.lp_last_error(None).decode()
+
+
+def test_loads_into_lds_keep_their_wait_states(tmp_path):
+    """What is checked of the other kernels' loads into LDS, for these."""
+    device_code.test_loads_into_lds_keep_their_wait_states("prefix", tmp_path)
