@@ -618,13 +618,14 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
   const int ctx_top = (int)~wave_min_u32(~(uint32_t)ctx);
   // rows that see nothing get zeros at the end, whatever is summed for them
   const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
-  // the wave's entries that have a block some row sees, and some row its second half
+  // the wave's entries that have a block some row sees; those of which some row
+  // sees the second half, and no row the first
   const bool pre = e0 + lane < a.nP;
   const int first = pre ? (e0 + lane) * KV_BLOCK : (a.F + e0 + lane - a.nP) * KV_BLOCK;
   const int from = pre ? 0 : P, to = min(pre ? P : INT_MAX, ctx_top);  // its positions [from, to)
   const uint64_t mine = ~0ull / ((1ull << (1 << log)) - 1) << nth;     // every 2^log-th
-  uint64_t left = __ballot(off >= 0 && first < to) & mine;
-  const uint64_t second = __ballot(first + 32 < to);
+  uint64_t left = __ballot(off >= 0 && first < to && from < to) & mine;
+  const uint64_t second = __ballot(first + 32 < to), late = __ballot(first + 32 <= from);
   // copies into this wave's LDS
   char *ks = lds + wave * 2 * KV, *vs = ks + KV;
   const uint32_t kl = lds_addr(ks), vl = kl + KV;
@@ -665,10 +666,10 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
 #pragma unroll
   for (int i = 0; i < 4; ++i) mx[i] = -INFINITY, sm[i] = 0.f, rctx[i] = __shfl(ctx, 4 * quad + i, 64);
   if (left) {
-    int i = __builtin_ctzll(left), h = 0, base = place(i, 0);
-    copy_k(0);
-    copy_v(0);
-    for (int halves = __builtin_popcountll(left) + __builtin_popcountll(left & second); halves > 0; --halves) {
+    int i = __builtin_ctzll(left), h = (int)(late >> i & 1), base = place(i, h);
+    copy_k(h);
+    copy_v(h);
+    for (int halves = __builtin_popcountll(left & ~late) + __builtin_popcountll(left & second); halves > 0; --halves) {
       // keys [lo, hi) of the 32 at `base` are there
       const int lo = max(0, __builtin_amdgcn_readlane(from, i) - base);
       const int hi = min(32, __builtin_amdgcn_readlane(to, i) - base);
@@ -685,8 +686,11 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
         }
       if (halves > 1) {
         h = (int)(second >> i & 1) & (h ^ 1);
-        left = h ? left : left & (left - 1);
-        i = __builtin_ctzll(left);
+        if (!h) {
+          left &= left - 1;
+          i = __builtin_ctzll(left);
+          h = (int)(late >> i & 1);
+        }
         base = place(i, h);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
         copy_k(h);
@@ -929,7 +933,9 @@ constexpr int WHOLE_ENTRIES = 12, WHOLE_ITEMS = 256;
 // where it ends.  Measured (graphs of calls; prompts' rows x tokens of prefix,
 // blocks of a split): 8B 640 x 1,500 6 blocks 53.4 us, 8 46.7, 12 44.0, 24 55.5;
 // 7B 547 x 4,000 16 blocks 96.8, 21 87.4, 24 76.0, 32 82.5; 8B 200 x 2,000 4 blocks
-// 28.7, 8 28.8, 11 32.1; 13B 240 x 1,000 4 blocks 32.6, 6 27.9, 8 29.3.
+// 28.7, 8 28.8, 11 32.1; 13B 240 x 1,000 4 blocks 32.6, 6 27.9, 8 29.3; 64 decode
+// rows, 8B x 8,000 6 blocks 50.3, 10 40.3, 16 46.2; 70B x 16,000 10 74.7, 16 77.5,
+// 20 63.1, 25 69.3.
 static int tile_split(int nP, int64_t items, int64_t rows_heads, int64_t own_items, int own_blocks) {
   constexpr double FIXED = 4, PART = 1.3e-4;
   int best = nP;
@@ -971,18 +977,6 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   }
   a.tiles = few ? 0 : tiles;
   a.shared_rows = few ? tiles : 0;
-  if (a.nP && few) {
-    // about 512 workgroups, of four blocks (a wave each, or 128 keys) and up
-    const int want = std::max(1, 512 / std::max(1, tiles * n_kv_heads));
-    a.sblk = std::min(ceil_div(a.nP, std::min(want, ceil_div(a.nP, 4))), 64);
-  } else if (a.nP) {
-    // own items: the sequences' tiles, half of the longest's blocks each, or
-    // (decode) a fourth of a workgroup and four blocks a row
-    const int64_t items = (int64_t)tiles * n_kv_heads, rows_heads = (int64_t)rows * n_heads;
-    a.sblk = tile_split(a.nP, items, rows_heads, decode ? (int64_t)rows * n_kv_heads / 4 : items,
-                        decode ? std::min(own, 4) : (own + 1) / 2);
-  }
-  a.splits = a.nP ? ceil_div(a.nP, a.sblk) : 0;
   a.oblk = std::max(1, own);
   a.own_log = 2;
   if (decode) {
@@ -1002,6 +996,18 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   } else if (!half) {
     a.oblk = std::max(1, std::min(own, 64));
   }
+  if (a.nP && few) {
+    // about 512 workgroups, of four blocks (a wave each, or 128 keys) and up
+    const int want = std::max(1, 512 / std::max(1, tiles * n_kv_heads));
+    a.sblk = std::min(ceil_div(a.nP, std::min(want, ceil_div(a.nP, 4))), 64);
+  } else if (a.nP) {
+    // own items: a row's (as above), or the sequences' tiles, half of the longest's blocks each
+    const int64_t items = (int64_t)tiles * n_kv_heads, rows_heads = (int64_t)rows * n_heads;
+    const int64_t of_rows = (((int64_t)rows * n_kv_heads) << a.own_log) / 4 * ceil_div(own, a.oblk);
+    a.sblk = tile_split(a.nP, items, rows_heads, decode ? of_rows : items,
+                        decode ? std::min(own, a.oblk) >> a.own_log : (own + 1) / 2);
+  }
+  a.splits = a.nP ? ceil_div(a.nP, a.sblk) : 0;
   // Prompts whose tiles fill two workgroups a CU walk the prefix and their own
   // blocks in one item, and nothing is joined: 70B three prompts of 2,100 over
   // 4,096 tokens 686 us against 800, 13B eight of 250 over 1,000 97 against 121; with
