@@ -536,7 +536,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void p
 }
 
 // Few rows over a range of entries, on 16x16 MFMAs: up to 16 packed rows of a KV
-// head; wave w takes every NW-th entry from the w-th on, 32 keys at a time.
+// head, walked 32 keys at a time; waves that share an item take half blocks in turn.
 // Each wave has its own LDS for K and V of 32 keys: K is copied there while the
 // softmax of the keys before runs, V while the scores do.  (Fragments loaded
 // straight from the cache ask for 16 rows with every four lanes on four lines:
@@ -618,14 +618,17 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
   const int ctx_top = (int)~wave_min_u32(~(uint32_t)ctx);
   // rows that see nothing get zeros at the end, whatever is summed for them
   const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
-  // the wave's entries that have a block some row sees; those of which some row
-  // sees the second half, and no row the first
+  // Entries with a block of which some row sees the first half, the second half,
+  // of those that are this wave's: all of the item's, or where waves share it one
+  // half of every 2^(log - 1)-th.
   const bool pre = e0 + lane < a.nP;
   const int first = pre ? (e0 + lane) * KV_BLOCK : (a.F + e0 + lane - a.nP) * KV_BLOCK;
   const int from = pre ? 0 : P, to = min(pre ? P : INT_MAX, ctx_top);  // its positions [from, to)
-  const uint64_t mine = ~0ull / ((1ull << (1 << log)) - 1) << nth;     // every 2^log-th
-  uint64_t left = __ballot(off >= 0 && first < to && from < to) & mine;
-  const uint64_t second = __ballot(first + 32 < to), late = __ballot(first + 32 <= from);
+  const uint64_t mine = log ? ~0ull / ((1ull << (1 << (log - 1))) - 1) << (nth >> 1) : ~0ull;
+  const bool some_key = off >= 0 && first < to && from < to;
+  const uint64_t half0 = log && nth & 1 ? 0 : __ballot(some_key && from < first + 32) & mine;
+  const uint64_t half1 = log && !(nth & 1) ? 0 : __ballot(some_key && first + 32 < to) & mine;
+  uint64_t left = half0 | half1;
   // copies into this wave's LDS
   char *ks = lds + wave * 2 * KV, *vs = ks + KV;
   const uint32_t kl = lds_addr(ks), vl = kl + KV;
@@ -666,10 +669,10 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
 #pragma unroll
   for (int i = 0; i < 4; ++i) mx[i] = -INFINITY, sm[i] = 0.f, rctx[i] = __shfl(ctx, 4 * quad + i, 64);
   if (left) {
-    int i = __builtin_ctzll(left), h = (int)(late >> i & 1), base = place(i, h);
+    int i = __builtin_ctzll(left), h = (int)(~half0 >> i & 1), base = place(i, h);
     copy_k(h);
     copy_v(h);
-    for (int halves = __builtin_popcountll(left & ~late) + __builtin_popcountll(left & second); halves > 0; --halves) {
+    for (int halves = __builtin_popcountll(half0) + __builtin_popcountll(half1); halves > 0; --halves) {
       // keys [lo, hi) of the 32 at `base` are there
       const int lo = max(0, __builtin_amdgcn_readlane(from, i) - base);
       const int hi = min(32, __builtin_amdgcn_readlane(to, i) - base);
@@ -685,11 +688,11 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
           s[nt] = Piece<T>::mma(qa[k], *(const u32x4_tt *)f, s[nt]);
         }
       if (halves > 1) {
-        h = (int)(second >> i & 1) & (h ^ 1);
+        h = (int)(half1 >> i & 1) & (h ^ 1);
         if (!h) {
           left &= left - 1;
           i = __builtin_ctzll(left);
-          h = (int)(late >> i & 1);
+          h = (int)(~half0 >> i & 1);
         }
         base = place(i, h);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
