@@ -862,14 +862,16 @@ __global__ __launch_bounds__(512) void prefix_row_kernel(const T *__restrict__ q
   rows_item<T, HD, WHOLE_WAVES<T, HD>, true>(q, out, a, i, blockIdx.x - i * a.b.kv.n_kv_heads, lds);
 }
 
-// Joins the parts of a (token, head), a wave each: its lanes hold the parts'
-// weights first, then the dims, U parts requested at a time.
-template <typename T, int HD, int U>
+// Joins the parts of a (token, head), a wave each, or with more than 16 parts
+// four: its lanes hold the weights of 64 parts first, then the dims of U parts
+// at a time; of four waves each takes 16 of the 64, and they add up in LDS.
+template <typename T, int HD, int U, int W>
 __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, PrefixArgs a) {
+  static_assert(W == 1 || (W == 4 && U == 16), "a fourth of 64 parts in one step");
   constexpr int DPL = HD / 64;
   constexpr float c2 = SCORE_C2<HD>;
-  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t row = W == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
   const int64_t t = row / a.b.n_heads;
   if (t >= a.b.rows) return;
   int parts = a.parts;
@@ -895,7 +897,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
     M = mn;
 #pragma unroll
     for (int d = 0; d < DPL; ++d) o[d] *= f0;
-    for (int p = 0; p < n; p += U) {
+    for (int p = W == 1 ? 0 : wave * U; p < n; p += W * U) {
       // all requested before any is used; past the last part: 0 of that part again
       float v[U][DPL];
 #pragma unroll
@@ -910,6 +912,18 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
       }
     }
   }
+  if constexpr (W > 1) {
+    __shared__ float sums[W - 1][HD];
+#pragma unroll
+    for (int d = 0; d < DPL; ++d)
+      if (wave) sums[wave - 1][lane * DPL + d] = o[d];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int d = 0; d < DPL; ++d)
+#pragma unroll
+      for (int w = 0; w < W - 1; ++w) o[d] += sums[w][lane * DPL + d];
+  }
   const float inv = L == 0.f ? 0.f : 1.0f / L;
 #pragma unroll
   for (int d = 0; d < DPL; ++d) out[row * HD + lane * DPL + d] = round_to<T>(o[d] * inv);
@@ -921,12 +935,18 @@ static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // A decode batch whose rows each see at most WHOLE_ENTRIES blocks, and whose rows
 // and KV heads are at most WHOLE_ITEMS, takes a workgroup per row and KV head
-// (graphs of calls, 8B heads: 32 rows over 553 + 60 tokens 12.5 us against 16.2
-// in two launches, over 1,000 + 100, 19 blocks, 16.9 against 19.5; one row over
-// 100 + 60 7.0 against 9.4, 553 + 60 10.0 against 9.5, 1,100 + 60 13.0 against
-// 9.6; 64 rows over 553 + 60, 512 workgroups, 22.4 against 20.5; 7B heads, 4 rows
-// over 553 + 60, 128 workgroups, 11.3 against 12.5).
+// (graphs of calls, 8B heads: 32 rows over 553 + 60 tokens, 12 blocks, 12.2 us
+// against 14.9 in two launches, over 1,000 + 100, 19 blocks, 16.5 against 15.6; one
+// row over 300 + 60 8.2 against 9.7, 553 + 60 9.8 against 9.5, 1,000 + 60, 18
+// blocks, 11.9 against 10.0; 64 rows over 553 + 60, 512 workgroups, 22.4 against
+// 20.5; 7B heads, 4 rows over 553 + 60, 128 workgroups, 11.0 against 12.2).
 constexpr int WHOLE_ENTRIES = 12, WHOLE_ITEMS = 256;
+
+// Splits of a prefix of nP blocks at most: of two blocks, but for longer prefixes
+// of four, as parts cost the join (graphs of calls: 8B 32 rows over 1,000 tokens
+// 2 blocks 15.6 us, 4 17.3; fp32 32 small rows over 1,000 13.4 and 15.9; 8B 8 rows
+// over 2,000 14.5 and 15.1; one row over 6,000 14.8 and 13.4).
+static int most_splits(int nP) { return nP <= 32 ? ceil_div(nP, 2) : std::max(16, ceil_div(nP, 4)); }
 
 // Blocks of a split of the prefix for `items` tiles and KV heads.  In units of a
 // block's time where two workgroups share a CU (about 2 us), an item of n blocks
@@ -943,7 +963,7 @@ static int tile_split(int nP, int64_t items, int64_t rows_heads, int64_t own_ite
   constexpr double FIXED = 4, PART = 1.3e-4;
   int best = nP;
   double least = 0;
-  for (int s = 1; s <= ceil_div(nP, 4) && (s == 1 || items * s <= 512); ++s) {
+  for (int s = 1; s <= most_splits(nP) && (s == 1 || items * s <= 512); ++s) {
     if (s > 1 && items * (s * FIXED + nP) / 512 + s * rows_heads * PART > least) break;  // more only cost more
     for (const int n : {ceil_div(nP, s), (int)(nP / (s - 0.5))}) {
       if (n > nP || n < 1 || ceil_div(nP, n) != s) continue;
@@ -1000,9 +1020,12 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
     a.oblk = std::max(1, std::min(own, 64));
   }
   if (a.nP && few) {
-    // about 512 workgroups, of four blocks (a wave each, or 128 keys) and up
+    // Up to 512 workgroups, and up to 24 parts while a part is at most 32 blocks:
+    // 8B, graphs of calls, one row over 6,000 tokens 2 blocks 14.8 us, 4 13.4, 8
+    // 15.4; one over 16,000 4 blocks 22.3, 8 19.8, 12 19.5, 20 24.6.
     const int want = std::max(1, 512 / std::max(1, tiles * n_kv_heads));
-    a.sblk = std::min(ceil_div(a.nP, std::min(want, ceil_div(a.nP, 4))), 64);
+    const int most = std::min(most_splits(a.nP), std::max(24, a.nP / 32));
+    a.sblk = std::min(ceil_div(a.nP, std::min(want, most)), 64);
   } else if (a.nP) {
     // own items: a row's (as above), or the sequences' tiles, half of the longest's blocks each
     const int64_t items = (int64_t)tiles * n_kv_heads, rows_heads = (int64_t)rows * n_heads;
@@ -1028,7 +1051,7 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
 
 // Partials of any plan of at most these rows and contexts, so that a workspace
 // for a batch's limits serves its smaller steps.  A row has at most one part per
-// four blocks.  Shared: the splits times the row tiles are about 512 workgroups
+// four blocks, or one per two up to 16.  Shared: the splits times the row tiles are about 512 workgroups
 // over the KV heads, so rows times splits stay under 512 x 128 / n_heads where
 // splits are more than one, or, of 64 blocks an item, than nP / 64.  Own: at most
 // 16, or own / 64.
@@ -1037,8 +1060,8 @@ size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_he
   const int64_t nP = ceil_div(std::min(prefix_len, max_ctx), KV_BLOCK);
   const int64_t own = max_ctx > prefix_len ? ceil_div(max_ctx, KV_BLOCK) - prefix_len / KV_BLOCK : 0;
   const int64_t r = rows, quarter = (own + 3) / 4, each = (own + 63) / 64;
-  const int64_t shared = std::min(r * ((nP + 3) / 4), std::max(r * std::max<int64_t>(1, (nP + 63) / 64),
-                                                               (int64_t)65536 / n_heads));
+  const int64_t shared = std::min(r * most_splits((int)nP),
+                                  std::max(r * std::max<int64_t>(1, (nP + 63) / 64), (int64_t)65536 / n_heads));
   const int64_t of_row = decode ? std::min(quarter, std::max<int64_t>(16, each)) : each;
   return (size_t)(shared + r * of_row) * n_heads * (head_dim + 2) * sizeof(float);
 }
@@ -1066,7 +1089,7 @@ static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   a.by_shared = divisor(a.shared_rows);
   a.by_per = divisor(ceil_div(a.G, rto));
   const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.units * a.osplits) * Hkv;
-  const int64_t joins = ((int64_t)b.rows * b.n_heads + 3) / 4;
+  const int64_t joins = a.parts <= 16 ? ((int64_t)b.rows * b.n_heads + 3) / 4 : (int64_t)b.rows * b.n_heads;
   if (std::max(items, joins) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads, 512 to a workgroup
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
   if (a.whole) {
@@ -1081,9 +1104,11 @@ static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   }
   if (!a.direct && !a.whole) {
     if (a.parts <= 4)
-      prefix_join_kernel<T, HD, 4><<<grid(joins), 256, 0, s>>>(out, a);
+      prefix_join_kernel<T, HD, 4, 1><<<grid(joins), 256, 0, s>>>(out, a);
+    else if (a.parts <= 16)
+      prefix_join_kernel<T, HD, 16, 1><<<grid(joins), 256, 0, s>>>(out, a);
     else
-      prefix_join_kernel<T, HD, 16><<<grid(joins), 256, 0, s>>>(out, a);
+      prefix_join_kernel<T, HD, 16, 4><<<grid(joins), 256, 0, s>>>(out, a);
   }
   return true;
 }
