@@ -33,9 +33,10 @@ __device__ __forceinline__ int saturated(int64_t v) { return (int)min(v, (int64_
 
 // A step is a scan over the sequences (rows and blocks) and independent stores:
 // nothing but latency at any size that a service has (256 requests, 65,000 rows:
-// 1.1 MB).  So one launch: every workgroup scans all sequences for itself, keeps
-// what it needs of each in LDS, and takes its share of the table rows (a wave a
-// sequence) and of the packed rows (a thread each, its sequence by bisection).
+// 1.1 MB, 5.2 us; 64 requests of one row 3.8 us).  So one launch: every workgroup
+// scans all sequences for itself, keeps what it needs of each in LDS, and takes
+// its share of the table rows (a wave a sequence) and of the packed rows (a
+// thread each, its sequence by bisection).
 // With WHOLE = false the sums come from a launch of their own (table_scan_kernel)
 // and the sequences are read again: more sequences than LDS holds, or a free_head
 // inside free_start, which workgroups that start late would find updated.
@@ -262,9 +263,12 @@ static void launch_append(const QkvAppend &a, T *q, T *k, T *v, hipStream_t s) {
     const int v_wgs = (a.rows + TR - 1) / TR * a.n_kv_heads;
     qkv_append_kernel<T, HD, W, TR><<<v_wgs + a.rows * per, 256, 0, s>>>(a, q, k, v, v_wgs);
   };
-  // 64-row tiles store whole 128-byte runs; 16-row ones give a decode batch,
-  // whose rows are scattered anyway, four times the workgroups
-  if (a.rows > 256)
+  // 64-row tiles of V store whole 128-byte runs; 16-row ones are four times the
+  // workgroups, until the larger ones fill the GPU too (graphs of calls, 16-row
+  // against 64-row tiles: 8B heads 64 decode rows 4.0 us against 8.1, 1,000 rows of
+  // four prompts, 128 large tiles, 7.2 and 8.3, 4,200 rows, 528, 25.7 and 24.7; 7B
+  // heads 1,000 rows, 512, 12.3 and 12.1)
+  if ((int64_t)((a.rows + 63) / 64) * a.n_kv_heads >= 512)
     run(std::integral_constant<int, 64>());
   else
     run(std::integral_constant<int, 16>());

@@ -154,6 +154,8 @@ APPEND_CASES = [
     ("f16", 8, 2, 64, [(0, 200), (61, 9)], 0), ("bf16", 6, 2, 128, [(3, 130), (250, 70)], 6),
     ("f32", 4, 4, 64, [(0, 37), (64, 64)], 0), ("f32", 5, 1, 128, [(1, 63), (127, 2)], 2),
     ("f16", 40, 40, 128, [(30, 70)], 2), ("f16", 3, 3, 64, [(7, 8), (0, 8), (56, 16)], 0),
+    # V in 64-row tiles, whole blocks and ragged ones
+    ("bf16", 64, 64, 64, [(0, 256), (7, 200)], 0), ("f16", 96, 96, 128, [(3, 333)], 2), ("f32", 64, 64, 64, [(64, 450)], 0),
 ]
 
 
