@@ -2,8 +2,9 @@
  * checks and kernel timing.  They launch exactly the kernels the engine runs
  * (those of the last section, a batch that shares a prefix, are for callers
  * that plan their own steps), on caller-provided device buffers,
- * asynchronously on `hip_stream` (a hipStream_t, NULL for the null stream).  All pointers are device pointers
- * unless stated otherwise; the caller owns every buffer.  Each returns LP_OK or
+ * asynchronously on `hip_stream` (a hipStream_t, NULL for the null stream).
+ * All pointers are device pointers unless stated otherwise; the caller owns
+ * every buffer.  Each returns LP_OK or
  * LP_EINVAL (bad sizes; checked before any launch) or LP_EHIP (launch error);
  * lp_last_error(NULL) then holds a message.  A call with no rows (M, rows or
  * n_seq equal to 0) checks its sizes, then returns LP_OK without a launch or
