@@ -775,6 +775,53 @@ def test_prefill_of_many_rows(dtype, Hq, Hkv, hd, P, seqs):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("f16", 8, 2, 128), ("bf16", 32, 2, 64), ("f32", 4, 2, 64)])
+def test_rows_that_only_read_the_prefix(dtype, Hq, Hkv, hd):
+    """No row has a block of its own: decode rows and prompts inside a prefix of two blocks, and of many."""
+    rng = np.random.default_rng(hd + Hq)
+    for P in (128, 1000):
+        b = Batch(rng, dtype, Hkv, hd, P, [P, P, P])
+        rows = [(m % 3, [-1, 0, P - 1, 63, 64, m % P][m % 6]) for m in range(140)]
+        q = values(rng, (140, Hq, hd), dtype)
+        got = run_decode(b, q, rows, Hq)
+        for m, (j, p) in enumerate(rows):
+            if p < 0:
+                assert np.all(got[m] == 0)
+            else:
+                ref, tol = b.reference(q[m:m + 1], j, [p])
+                assert np.all(np.abs(got[m:m + 1] - ref) <= tol), m
+        seqs = [(0, 0, 70), (1, P - 30, 30), (2, 40, 37)]
+        got = run_prefill(b, q, seqs, Hq, start=1, tail=2)
+        assert np.all(got[:1] == 7) and np.all(got[-2:] == 7)
+        r = 1
+        for j, p, n in seqs:
+            ref, tol = b.reference(q[r:r + n], j, np.arange(p, p + n))
+            assert np.all(np.abs(got[r:r + n] - ref) <= tol), j
+            r += n
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prefill_of_a_padded_batch(dtype):
+    """150 places for sequences of which five have rows, the others none and no slot."""
+    rng = np.random.default_rng(150)
+    P, Hq, Hkv, hd = 90, 8, 2, 64
+    new = np.zeros(150, int)
+    new[[3, 63, 64, 100, 149]] = [40, 1, 33, 70, 9]
+    b = Batch(rng, dtype, Hkv, hd, P, [P + n for n in new])
+    q = values(rng, (new.sum() + 4, Hq, hd), dtype)
+    got = run_prefill(b, q, [(j, P, n) for j, n in enumerate(new)], Hq, tail=4,
+                      slots=[s if n else -1 for s, n in zip(b.slot, new)])
+    assert np.all(got[-4:] == 7)
+    r = 0
+    for j, n in enumerate(new):
+        if n:
+            ref, tol = b.reference(q[r:r + n], j, np.arange(P, P + n))
+            assert np.all(np.abs(got[r:r + n] - ref) <= tol), j
+        r += n
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_rows_past_max_new(dtype):
     """Of a sequence with more rows than max_new the first max_new are right,
