@@ -1014,18 +1014,19 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   a.own_log = 2;
   if (decode) {
     const int64_t pairs = (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads;
-    while (a.own_log && ((pairs << a.own_log) > 512 || 1 << a.own_log > own)) --a.own_log;
+    while (a.own_log && (1 << a.own_log > own || (a.own_log == 2 && pairs > 256))) --a.own_log;
   }
   if (decode) {
     const int want = std::max(1, 512 / (int)std::min((int64_t)rows * n_kv_heads, (int64_t)512));
     a.oblk = std::max(1, ceil_div(own, std::min(want, std::max(1, ceil_div(own, 4)))));
-    // Many rows: one wave an item, of four blocks (two waves and up: eight), so
-    // that long rows end with the others; at most 16 parts a row while an item's
-    // 64 blocks allow, for max_ctx far above the rows' contexts.  8B heads, 64
-    // rows of 300 over 2,000 tokens, waves x blocks: 1 x 4 31.6 us, 2 x 4 36.3,
-    // 2 x 8 33.0, 4 x 8 35.6, 4 x all 35.5; 13B heads, 16 of 300: 46.0, -, 49.8,
-    // 46.9, 46.6, 1 x all 81.6.
-    a.oblk = std::min(std::max(std::min(a.oblk, a.own_log ? 8 : 4), ceil_div(own, 16)), 64);
+    // Two waves an item (four in batches of up to 256 rows and KV heads), of
+    // six blocks (eight), so that long rows end with the others; at most 16 parts
+    // a row while an item's 64 blocks allow, for max_ctx far above the rows'
+    // contexts.  Waves x blocks: 8B heads, 64 rows of 300 over 2,000 tokens 1 x 4
+    // 31.5 us, 2 x 6 29.8, 2 x 8 32.4, 4 x 8 32.7; 64 of 2,000 over 64 138, 125, 125,
+    // 123; 13B, 64 of 300 over 2,000 108, 104; 70B, 48 of 300 over 4,000 33.5, 33.3,
+    // 33.8, 38.0; 8B, 32 of 600 over 500, 256 pairs, -, 24.5, -, 23.9.
+    a.oblk = std::min(std::max(std::min(a.oblk, 4 + 2 * a.own_log), ceil_div(own, 16)), 64);
   } else if (!half) {
     a.oblk = std::max(1, std::min(own, 64));
   }
