@@ -217,6 +217,7 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
   floatx16_t o[NT];
   float mref, lsum;
   int r0 = 0, part = 0, start = 0, seen = -1;
+  bool walked = false;
   PrefixRow w{};
   int *again = (int *)(lds + 2 * STAGE);
   // The item from its index to its (m, l, o); returns whether some rows of the
@@ -249,6 +250,7 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
       const int blocks = (most + KV_BLOCK - 1) / KV_BLOCK;
       e1 = min(e0 + a.oblk, most > P ? a.nP + blocks - a.F : blocks);
     }
+    walked = e0 < e1;
     // What the first copies wait for is requested first, with the rows' q: a
     // walk of few blocks is one memory round trip after the other.
     w = packed_row(a, start, r0, wave * 32 + l32, g);
@@ -511,7 +513,7 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
             make_float4(o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3]);
       }
     if (live && hh == 0) *(float2 *)(a.pml + (row * a.parts + part) * 2) = make_float2(mref, sum);
-    const uint32_t rows_live = (uint32_t)__ballot(live);
+    const uint32_t rows_live = walked ? (uint32_t)__ballot(live) : 0;  // the join skips o of empty parts
 #pragma unroll 4
     for (int i = 0; i < 32 / RI; ++i) {
       const int x = i * RI + lane / LR;
@@ -823,7 +825,7 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
       if (none) v[d] = 0.f;
       if constexpr (WHOLE)
         out[row * HD + d * 64 + lane] = round_to<T>(L == 0.f ? 0.f : v[d] / L);
-      else
+      else if (e0 < e1)
         a.po[rec * HD + d * 64 + lane] = v[d];
     }
     if (!WHOLE && lane == 0) *(float2 *)(a.pml + rec * 2) = none ? make_float2(-INFINITY, 0.f) : make_float2(M, L);
@@ -902,7 +904,8 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
     const float2 x = lane < n ? ml[p0 + lane] : make_float2(-INFINITY, 0.f);
     const float mn = fmaxf(M, wave_max(x.x));
     const float f0 = M == mn ? 1.f : __builtin_amdgcn_exp2f((M - mn) * c2);
-    const float f = x.x == mn ? 1.f : __builtin_amdgcn_exp2f((x.x - mn) * c2);
+    const uint64_t filled = __ballot(x.x != -INFINITY);  // a part without keys has no o
+    const float f = x.x == -INFINITY ? 0.f : x.x == mn ? 1.f : __builtin_amdgcn_exp2f((x.x - mn) * c2);
     L = L * f0 + wave_sum(f * x.y);
     M = mn;
 #pragma unroll
@@ -918,7 +921,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
       for (int u = 0; u < U; ++u) {
         const float fu = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), p + u));
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) o[d] += fu * (p + u < n ? v[u][d] : 0.f);
+        for (int d = 0; d < DPL; ++d) o[d] += fu * (filled >> (p + u) & 1 ? v[u][d] : 0.f);
       }
     }
   }
@@ -1027,8 +1030,16 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
     // 123; 13B, 64 of 300 over 2,000 108, 104; 70B, 48 of 300 over 4,000 33.5, 33.3,
     // 33.8, 38.0; 8B, 32 of 600 over 500, 256 pairs, -, 24.5, -, 23.9.
     a.oblk = std::min(std::max(std::min(a.oblk, 4 + 2 * a.own_log), ceil_div(own, 16)), 64);
-  } else if (!half) {
-    a.oblk = std::max(1, std::min(own, 64));
+  } else {
+    // Prompts' own blocks are split where their tiles leave half the GPU idle,
+    // to four blocks, past 64 tiles to 16.  New + cached tokens, whole against
+    // split: 8B one prompt of 30 + 4,000 116 us and 24, 50 + 400 25 and 18, 500 + 400
+    // (128 tiles) 52 and 62 in halves of 8; eight of 50 + 2,000 (104 tiles) 108 and
+    // 68; one of 1,000 (256 tiles) 63 and 68; fp32 20 + 3,000 67 and 16.
+    const int items = (int)std::min((int64_t)ceil_div(packed, rt) * n_kv_heads, (int64_t)512);
+    const int want = std::max(1, 256 / items);
+    a.oblk = std::max(std::min(own, items <= 64 ? 4 : 16), ceil_div(own, want));
+    a.oblk = std::max(1, half ? a.oblk : std::min(a.oblk, 64));
   }
   if (a.nP && few) {
     // Up to 512 workgroups, and up to 24 parts while a part is at most 32 blocks:
@@ -1041,8 +1052,8 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
     // own items: a row's (as above), or the sequences' tiles, half of the longest's blocks each
     const int64_t items = (int64_t)tiles * n_kv_heads, rows_heads = (int64_t)rows * n_heads;
     const int64_t of_rows = (((int64_t)rows * n_kv_heads) << a.own_log) / 4 * ceil_div(own, a.oblk);
-    a.sblk = tile_split(a.nP, items, rows_heads, decode ? of_rows : items,
-                        decode ? std::min(own, a.oblk) >> a.own_log : (own + 1) / 2);
+    a.sblk = tile_split(a.nP, items, rows_heads, decode ? of_rows : items * ceil_div(own, a.oblk),
+                        decode ? std::min(own, a.oblk) >> a.own_log : (std::min(own, a.oblk) + 1) / 2);
   }
   a.splits = a.nP ? ceil_div(a.nP, a.sblk) : 0;
   // Prompts whose tiles fill two workgroups a CU walk the prefix and their own
@@ -1062,10 +1073,10 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
 
 // Partials of any plan of at most these rows and contexts, so that a workspace
 // for a batch's limits serves its smaller steps.  A row has at most one part per
-// four blocks, or one per two up to 16.  Shared: the splits times the row tiles are about 512 workgroups
-// over the KV heads, so rows times splits stay under 512 x 128 / n_heads where
-// splits are more than one, or, of 64 blocks an item, than nP / 64.  Own: at most
-// 16, or own / 64.
+// four blocks, or one per two up to 16.  Splits times row tiles are up to 512
+// workgroups over the KV heads, so rows times splits stay under 512 x 128 /
+// n_heads where splits are more than one, or, of 64 blocks an item, than nP / 64
+// (prefill's own: than own / 64).  A decode row's own: at most 16, or own / 64.
 size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_heads, int head_dim, int prefix_len,
                                  int max_ctx) {
   const int64_t nP = ceil_div(std::min(prefix_len, max_ctx), KV_BLOCK);
@@ -1073,8 +1084,9 @@ size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_he
   const int64_t r = rows, quarter = (own + 3) / 4, each = (own + 63) / 64;
   const int64_t shared = std::min(r * most_splits((int)nP),
                                   std::max(r * std::max<int64_t>(1, (nP + 63) / 64), (int64_t)65536 / n_heads));
-  const int64_t of_row = decode ? std::min(quarter, std::max<int64_t>(16, each)) : each;
-  return (size_t)(shared + r * of_row) * n_heads * (head_dim + 2) * sizeof(float);
+  const int64_t of_rows = decode ? r * std::min(quarter, std::max<int64_t>(16, each))
+                                 : std::min(r * quarter, std::max(r * each, (int64_t)65536 / n_heads));
+  return (size_t)(shared + of_rows) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
 template <typename T, int HD>

@@ -348,6 +348,9 @@ PREFILL_CASES = [
     ("bf16", 32, 8, 128, 300, [(0, 700), (0, 3)]), ("f16", 16, 2, 128, 4000, [(0, 3), (0, 9)]),
     ("f16", 8, 1, 64, 777, [(i % 5, 1 + i % 7) for i in range(70)]), ("bf16", 16, 16, 128, 640, [(0, 12)] * 11),
     ("f16", 8, 8, 64, 40, [(2500, 130), (0, 2)]),
+    # few tiles over long contexts of their own, beside rows that have none
+    ("f32", 4, 2, 64, 70, [(1500, 30), (0, 40), (-70, 10), (-30, 1)]), ("bf16", 8, 1, 128, 500, [(-500, 20), (3000, 9), (0, 1)]),
+    ("f16", 4, 4, 128, 0, [(0, 1), (1300, 64), (0, 0), (0, 300)]),
 ]
 
 
