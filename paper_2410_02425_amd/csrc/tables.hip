@@ -264,11 +264,12 @@ static void launch_append(const QkvAppend &a, T *q, T *k, T *v, hipStream_t s) {
     qkv_append_kernel<T, HD, W, TR><<<v_wgs + a.rows * per, 256, 0, s>>>(a, q, k, v, v_wgs);
   };
   // 64-row tiles of V store whole 128-byte runs; 16-row ones are four times the
-  // workgroups, until the larger ones fill the GPU too (graphs of calls, 16-row
+  // workgroups, until there is a large one for each CU (graphs of calls, 16-row
   // against 64-row tiles: 8B heads 64 decode rows 4.0 us against 8.1, 1,000 rows of
-  // four prompts, 128 large tiles, 7.2 and 8.3, 4,200 rows, 528, 25.7 and 24.7; 7B
-  // heads 1,000 rows, 512, 12.3 and 12.1)
-  if ((int64_t)((a.rows + 63) / 64) * a.n_kv_heads >= 512)
+  // four prompts, 128 large tiles, 7.2 and 8.3, 1,500 rows, 190, 10.8 and 10.9,
+  // 2,600, 330, 15.0 and 14.4, 4,200, 528, 25.7 and 24.7; 7B heads 500 rows, 256, 8.1
+  // and 8.4, 800, 400, 11.3 and 11.3)
+  if ((int64_t)((a.rows + 63) / 64) * a.n_kv_heads >= 256)
     run(std::integral_constant<int, 64>());
   else
     run(std::integral_constant<int, 16>());
