@@ -285,7 +285,8 @@ static int prefix_attention(int32_t dtype, const void *q, void *out, const Prefi
   OPCHK(prefix_sizes(b.rows, b.n_heads, b.kv.n_kv_heads, b.kv.head_dim, b.prefix_len, b.max_ctx),
         "prefix attention: sizes (rows, heads, head_dim 64 or 128, prefix_len, max_ctx)");
   OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "prefix attention: dtype");
-  OPCHK(b.n_seq >= 0 && b.n_seq <= PREFIX_MAX_POS && b.kv.n_blocks > 0 && b.n_slots > 0 && b.max_new > 0, "prefix attention: sizes");
+  OPCHK(b.n_seq >= 0 && b.n_seq <= PREFIX_MAX_POS && b.kv.n_blocks > 0 && b.n_slots > 0 && b.max_new > 0,
+        "prefix attention: sizes");
   OPCHK(b.kv.max_blocks > 0 && (b.max_ctx <= b.prefix_len || (int64_t)b.kv.max_blocks * KV_BLOCK >= b.max_ctx),
         "prefix attention: max_blocks too small for max_ctx");
   if (b.rows == 0 || b.n_seq == 0) return LP_OK;  // no rows: nothing is read or written

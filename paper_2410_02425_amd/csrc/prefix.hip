@@ -911,7 +911,8 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
 #pragma unroll
     for (int d = 0; d < DPL; ++d) o[d] *= f0;
     for (int p = W == 1 ? 0 : wave * U; p < n; p += W * U) {
-      // all requested before any is used; past the last part: 0 of that part again
+      // all requested before any is used, and before it is known which parts have
+      // keys (half a microsecond a call); past the last part: 0 of that part again
       float v[U][DPL];
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -1013,13 +1014,10 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   }
   a.tiles = few ? 0 : tiles;
   a.shared_rows = few ? tiles : 0;
-  a.oblk = std::max(1, own);
   a.own_log = 2;
   if (decode) {
     const int64_t pairs = (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads;
     while (a.own_log && (1 << a.own_log > own || (a.own_log == 2 && pairs > 256))) --a.own_log;
-  }
-  if (decode) {
     const int want = std::max(1, 512 / (int)std::min((int64_t)rows * n_kv_heads, (int64_t)512));
     a.oblk = std::max(1, ceil_div(own, std::min(want, std::max(1, ceil_div(own, 4)))));
     // Two waves an item (four in batches of up to 256 rows and KV heads), of
