@@ -13,6 +13,7 @@
 // e of the prefix, entry nP + i is own block F + i of the sequence, F =
 // floor(P / 64) being the first that is not all prefix.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "device.hpp"
@@ -973,10 +974,10 @@ static int most_splits(int nP) { return nP <= 32 ? ceil_div(nP, 2) : std::max(16
 // 28.7, 8 28.8, 11 32.1; 13B 240 x 1,000 4 blocks 32.6, 6 27.9, 8 29.3; 64 decode
 // rows, 8B x 8,000 6 blocks 50.3, 10 40.3, 16 46.2; 70B x 16,000 10 74.7, 16 77.5,
 // 20 63.1, 25 69.3.
-static int tile_split(int nP, int64_t items, int64_t rows_heads, int64_t own_items, int own_blocks) {
+static int tile_split(int nP, int64_t items, int64_t rows_heads, int64_t own_items, int own_blocks, double &least) {
   constexpr double FIXED = 4, PART = 1.3e-4;
   int best = nP;
-  double least = 0;
+  least = 0;
   for (int s = 1; s <= most_splits(nP) && (s == 1 || items * s <= 512); ++s) {
     if (s > 1 && items * (s * FIXED + nP) / 512 + s * rows_heads * PART > least) break;  // more only cost more
     for (const int n : {ceil_div(nP, s), (int)(nP / (s - 0.5))}) {
@@ -995,7 +996,7 @@ static int tile_split(int nP, int64_t items, int64_t rows_heads, int64_t own_ite
 
 // Row tiles and splits.
 static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_heads, int n_kv_heads, int prefix_len,
-                        int max_ctx) {
+                        int max_ctx, int n_seq) {
   a.G = n_heads / n_kv_heads;
   a.nP = ceil_div(std::min(prefix_len, max_ctx), KV_BLOCK);
   a.F = prefix_len / KV_BLOCK;
@@ -1007,6 +1008,7 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
   // 18.8; 13B 64 rows over 8,000 (64) 101 and 79; 70B 16 rows over 8,000 (128) 32 and 24.
   const bool few = !half || (decode && packed <= 32);
   const int rt = few ? 16 : 128;
+  bool walk = false;
   const int tiles = a.nP ? ceil_div(packed, rt) : 0;
   if (decode && a.nP + own <= WHOLE_ENTRIES && (int64_t)rows * ceil_div(a.G, 16) * n_kv_heads <= WHOLE_ITEMS) {
     a.whole = 1;
@@ -1050,16 +1052,22 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
     // own items: a row's (as above), or the sequences' tiles, half of the longest's blocks each
     const int64_t items = (int64_t)tiles * n_kv_heads, rows_heads = (int64_t)rows * n_heads;
     const int64_t of_rows = (((int64_t)rows * n_kv_heads) << a.own_log) / 4 * ceil_div(own, a.oblk);
+    double split;
     a.sblk = tile_split(a.nP, items, rows_heads, decode ? of_rows : items * ceil_div(own, a.oblk),
-                        decode ? std::min(own, a.oblk) >> a.own_log : (std::min(own, a.oblk) + 1) / 2);
+                        decode ? std::min(own, a.oblk) >> a.own_log : (std::min(own, a.oblk) + 1) / 2, split);
+    // Prompts may instead walk the prefix and their own blocks in one item, and
+    // nothing is joined: in the units of tile_split, every round of 512 items takes
+    // the prefix, the first (or with more, about half) the longest own context; a
+    // sequence's last tile is half full.  Right for 30 of 33 batches measured, the
+    // others within 10% (walk against splits): 70B three prompts of 2,100 over 4,096
+    // tokens 686 us and 800, 8 of 100 over 1,000 50 and 69, 32 of 30 over 2,000 125 and
+    // 109; 13B two of 800 over 3,000 149 and 165; 8B 16 of 120 over 2,000 135 and 115,
+    // one of 2,500 over 4,000 313 and 283 (taken for 304 and 313).
+    const double rounds = std::ceil((tiles + (n_seq - 1) / 2.0) * n_kv_heads / 512);
+    walk = !decode && rounds * (a.nP + 3) + (rounds > 1 ? own / 2 : own) < 1.05 * split;
   }
   a.splits = a.nP ? ceil_div(a.nP, a.sblk) : 0;
-  // Prompts whose tiles fill two workgroups a CU walk the prefix and their own
-  // blocks in one item, and nothing is joined: 70B three prompts of 2,100 over
-  // 4,096 tokens 686 us against 800, 13B eight of 250 over 1,000 97 against 121; with
-  // fewer the prefix's splits share the work better: 70B 32 of 30 over 2,000, 480
-  // tiles, 107 us in splits, 125 in one walk (13B two of 800 over 3,000: 167 and 145).
-  if (half && !decode && (int64_t)tiles * n_kv_heads >= 512) {
+  if (walk) {
     a.splits = a.tiles = 0;
     own += a.nP;
     a.oblk = own;
@@ -1094,7 +1102,7 @@ static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   const int Hkv = b.kv.n_kv_heads;
   constexpr bool half = sizeof(T) == 2;
   const bool decode = !b.seq_start;
-  prefix_plan(a, decode, half, b.rows, b.n_heads, Hkv, b.prefix_len, b.max_ctx);
+  prefix_plan(a, decode, half, b.rows, b.n_heads, Hkv, b.prefix_len, b.max_ctx, b.n_seq);
   a.po = ws;
   a.pml = ws + (size_t)b.rows * b.n_heads * a.parts * HD;
   const int rto = decode || !half ? 16 : 128;
