@@ -827,6 +827,30 @@ def test_prefill_of_a_padded_batch(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("f16", 8, 2, 128), ("bf16", 2, 2, 64), ("f32", 4, 2, 64)])
+def test_infinite_values_inside_a_long_prefix(dtype, Hq, Hkv, hd):
+    """Few prompts over a prefix that is split: rows before an infinite value keep their results to the bit."""
+    rng = np.random.default_rng(77)
+    P, bad = 2000, 930
+    b = Batch(rng, dtype, Hkv, hd, P, [P + 30, 960, 5, P + 300])
+    seqs = [(0, P, 30), (1, 900, 60), (2, 0, 5), (3, P + 280, 20)]
+    q = values(rng, (115, Hq, hd), dtype)
+    clean = run_prefill(b, q, seqs, Hq)
+    b.vc[int(b.pre[bad // 64]), :, :, bad % 64] = float("inf")
+    got = run_prefill(b, q, seqs, Hq)
+    r = 0
+    for j, p, n in seqs:
+        ref, tol = b.reference(q[r:r + n], j, np.arange(p, p + n))
+        assert np.all(np.abs(clean[r:r + n] - ref) <= tol)
+        for i in range(n):
+            if p + i < bad:
+                assert np.array_equal(got[r + i], clean[r + i]), (j, i)
+            else:
+                assert not np.isfinite(got[r + i]).any(), (j, i)
+        r += n
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_rows_past_max_new(dtype):
     """Of a sequence with more rows than max_new the first max_new are right,
