@@ -1102,13 +1102,16 @@ static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   const int Hkv = b.kv.n_kv_heads;
   constexpr bool half = sizeof(T) == 2;
   const bool decode = !b.seq_start;
-  prefix_plan(a, decode, half, b.rows, b.n_heads, Hkv, b.prefix_len, b.max_ctx, b.n_seq);
+  // Sequences that can have rows: a batch of fixed size may hold many more places,
+  // and each that owned a tile would cost a search through all of seq_start.
+  const int live = std::min(b.n_seq, b.rows);
+  prefix_plan(a, decode, half, b.rows, b.n_heads, Hkv, b.prefix_len, b.max_ctx, live);
   a.po = ws;
   a.pml = ws + (size_t)b.rows * b.n_heads * a.parts * HD;
   const int rto = decode || !half ? 16 : 128;
   a.otiles = decode ? b.rows * ceil_div(a.G, rto)
-                    : (int)std::min((int64_t)b.n_seq * ceil_div((int64_t)std::min(b.max_new, b.rows) * a.G, rto),
-                                    (int64_t)b.rows * a.G / rto + b.n_seq);
+                    : (int)std::min((int64_t)live * ceil_div((int64_t)std::min(b.max_new, b.rows) * a.G, rto),
+                                    (int64_t)b.rows * a.G / rto + live);
   a.units = decode ? ceil_div((int64_t)a.otiles << a.own_log, 4) : a.otiles;
   a.by_g = divisor(a.G);
   a.by_hkv = divisor(Hkv);

@@ -827,6 +827,32 @@ def test_prefill_of_a_padded_batch(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_prefill_of_few_rows_among_many_empty_places(dtype):
+    """16 rows of five sequences among 2^20 places, as a step of fixed size may
+    hold: each place without rows is no work of its own."""
+    rng = np.random.default_rng(20)
+    P, Hq, Hkv, hd, places = 70, 32, 8, 128, 1 << 20
+    at, new, ctx = [0, 5, 64, 70000, places - 1], [1, 6, 1, 3, 5], [130, 76, 71, 73, 200]
+    b = Batch(rng, dtype, Hkv, hd, P, ctx)
+    q = values(rng, (16, Hq, hd), dtype)
+    n, slot, pos = np.zeros(places, int), np.full(places, -1), np.full(places, -1)
+    n[at], slot[at], pos[at] = new, b.slot, np.subtract(ctx, new)
+    start, qd = i32(np.concatenate([[0], np.cumsum(n)])), torch.from_numpy(q).to(TYPES[dtype]).to(DEV)
+    for max_new in (1, 6):                # one row a sequence, and all
+        out = torch.full_like(qd, 7.0)
+        ws = torch.empty(lp.prefix_prefill_attention_ws_bytes(16, Hq, Hkv, hd, P, 200), dtype=torch.uint8, device=DEV)
+        lp.op_prefix_prefill_attention(qd, out, b.kc, b.vc, b.pre_t, P, i32(b.table), start, i32(slot), i32(pos), max_new,
+                                       200, ws)
+        got, r = out.double().cpu().numpy(), 0
+        for j, (x, c) in enumerate(zip(new, ctx)):
+            rows = min(x, max_new)
+            ref, tol = b.reference(q[r:r + rows], j, np.arange(c - x, c - x + rows))
+            assert np.all(np.abs(got[r:r + rows] - ref) <= tol), j
+            r += x
+
+
+@gpu
 @pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("f16", 8, 2, 128), ("bf16", 2, 2, 64), ("f32", 4, 2, 64)])
 def test_infinite_values_inside_a_long_prefix(dtype, Hq, Hkv, hd):
     """Few prompts over a prefix that is split: rows before an infinite value keep their results to the bit."""
