@@ -695,6 +695,11 @@ __global__ __launch_bounds__(256) void prefill_attn_kernel(const T *__restrict__
 // Rows of a sequence that are computed: as many as its row of the block table
 // holds.  A tile of 128 rows can reach past max_len, by up to one block.
 __device__ __forceinline__ int prefill_len(int len, const KVCache &kv) { return min(len, kv.max_blocks * KV_BLOCK); }
+// Base-2 score past which the maximum is taken off before the scale: up to here
+// a rounded mc is within 2^-13, which moves a weight of 1 by 8.5e-5, less than
+// its rounding to 16 bits (2.4e-4 in f16).
+constexpr float PFA_LARGE = 4096.f;
+
 template <typename T, int HD, int QW, int KG>
 __global__ __launch_bounds__(QW *KG * 64, 2) void prefill_attn_mfma_kernel(const T *__restrict__ q,
                                                                           T *__restrict__ out,

@@ -255,11 +255,6 @@ __device__ __forceinline__ void store_o32(T *dst, const floatx16_t &o, float inv
   }
 }
 
-// Base-2 score past which the maximum is taken off before the scale: up to here
-// a rounded mc is within 2^-13, which moves a weight of 1 by 8.5e-5, less than
-// its rounding to 16 bits (2.4e-4 in f16).
-constexpr float PFA_LARGE = 4096.f;
-
 // Rotary embedding of one pair (x0, x1) = (dimension i, dimension i + hd/2)
 // at angle theta, cs = cos theta, sn = sin theta.  Every kernel that rotates
 // a pair rounds it the same way: the fused multiply-adds are explicit, and

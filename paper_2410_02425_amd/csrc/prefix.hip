@@ -183,6 +183,14 @@ struct Piece {
   }
 };
 
+// Base-2 score past which a tile takes the maximum off before the scale.  Up to
+// here its rounded mc is within 2^-19, which moves the sums of a block or part
+// by 1.3e-6 against those of the others, as they meet at the maximum itself: no
+// more than the rounding of fp32 scores does.  (Three prompts of 2,100 over 4,096
+// tokens, 70B heads: scores past it 703 us, under it 698; sums corrected for mc's
+// rounding at every new maximum 686 and 703.)
+constexpr float TILE_LARGE = 64.f;
+
 // Many rows of a 16-bit type over a range of entries, on 32x32x16 MFMAs: a
 // workgroup owns 128 packed rows, 32 to a wave, and walks its entries' blocks,
 // which are copied into LDS for all its waves (two stages: the next block lands while the
@@ -194,7 +202,8 @@ struct Piece {
 //   holds of each 16 keys are consecutive keys, the B operand of O^T += V^T P^T,
 //   and P never leaves the registers.
 //   The running maximum moves in every block that raises it for a row of the
-//   wave, so the largest weight is exactly 1 before it is rounded to 16 bits.
+//   wave, so the largest weight is 1 (within TILE_LARGE's 1.3e-6) before it is
+//   rounded to 16 bits.
 // V at places that no row of the tile sees is cleared in LDS (stale entries may
 // hold anything, and 0 * NaN is not 0).  Places that only some of its rows see
 // are not: their weight is 0 for the others, which is enough unless V is
@@ -330,7 +339,7 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
     float mc = 0.f;
     mref = -INFINITY;
     lsum = 0.f;
-    bool large = false;   // wave-uniform: a row's |mc| is past PFA_LARGE
+    bool large = false;   // wave-uniform: a row's |mc| is past TILE_LARGE
     bool masked = false;  // wave-uniform: a block that only some rows see whole
     for (int e = e0; e < e1; ++e) {
       const bool mine = e < a.nP;
@@ -399,7 +408,7 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
         const float corr = nm == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mref - nm) * c2);
         mref = nm;
         mc = nm == -INFINITY ? 0.f : nm * c2;  // a row that has seen no key yet
-        large = __any(fabsf(mc) > PFA_LARGE);
+        large = __any(fabsf(mc) > TILE_LARGE);
         lsum *= corr;
 #pragma unroll
         for (int t = 0; t < NT; ++t)

@@ -480,6 +480,48 @@ def test_scores_of_any_size(dtype, lo, hi):
         assert np.all(np.abs(got[j:j + 1] - ref) <= tol + 2.0 ** -15 * mag), j
 
 
+@gpu
+@pytest.mark.parametrize("P,rows,Hq", [(8192, 3, 1), (0, 260, 64)])
+def test_sums_over_many_large_scores_meet_at_one_maximum(P, rows, Hq):
+    """Scores of 4,000 in base 2, with values of 1 at the first 8,192 positions
+    and -1 at the others: an error of one part's (or, in a walk of one part, of
+    one block's) sums against another's is the result's.  Every block holds its
+    half's largest score, and the halves' largest are such that score times
+    log2(e) / sqrt(64), rounded in fp32, is off by 2^-13 up in one, down in the other."""
+    rng = np.random.default_rng(1)
+    hd, n, top = 64, 16384, (31.671875, 31.875)
+    x = [np.minimum(rng.integers(0, 2048, 8192) / 64, t) for t in top]
+    for half, t in zip(x, top):
+        half[rng.integers(0, 64, 128) + 64 * np.arange(128)] = t
+    score = 22144 + np.concatenate(x)                # 128 * 173 + ..: exact in f16 as two products, and in fp32
+    kc = torch.zeros(256, 1, 64, hd, dtype=torch.float16, device=DEV)
+    kc[..., 0] = 173
+    kc[:, 0, :, 1] = torch.from_numpy(score - 22144).half().view(256, 64).to(DEV)
+    assert torch.equal(kc[:, 0, :, 1].double().cpu().flatten(), torch.from_numpy(score - 22144))
+    v = np.where(np.arange(n) < 8192, 1.0, -1.0)
+    vc = torch.from_numpy(v).half().view(256, 1, 1, 64).expand(256, 1, hd, 64).contiguous().to(DEV)
+    q = torch.zeros(rows, Hq, hd, dtype=torch.float16, device=DEV)
+    q[..., 0], q[..., 1] = 128, 1
+    out = torch.empty_like(q)
+    table = i32([np.arange(256)])
+    ws = torch.empty(lp.prefix_prefill_attention_ws_bytes(rows, Hq, 1, hd, P, n) + 16, dtype=torch.uint8, device=DEV)
+    lp.op_prefix_prefill_attention(q, out, kc, vc, table[0, :P // 64].contiguous(), P, table, i32([0, rows]), i32([0]),
+                                   i32([n - rows]), rows, n, ws)
+    got = out.double().cpu().numpy()
+    # weights are rounded to f16 against the largest of their own half, and the sums scaled to the row's
+    weight = [np.exp((22144 + a - 22144 - t) / 8) for a, t in zip(x, top)]
+    scale = np.repeat([np.exp((top[0] - top[1]) / 8), 1.0], 8192)
+    held = torch.from_numpy(np.concatenate(weight)).half().double().numpy() * scale
+    weight = np.concatenate(weight) * scale
+    for r in range(rows):
+        c = n - rows + r + 1
+        ref = (held[:c] * v[:c]).sum() / weight[:c].sum()
+        # two fp32 sums over n terms in random order: 2^-24 of each partial sum, in all 2^-24 sqrt(n / 3) = 4.4e-6
+        # of the whole as a standard deviation, four of them; a weight next to a tie (6e-4 of them) may round the
+        # other way: 6e-4 * 2^-11; the result's own rounding
+        assert np.all(np.abs(got[r] - ref) <= 2.0 ** -11 * abs(ref) + 1.8e-5 + 3e-7), (r, got[r, 0, 0] - ref)
+
+
 # ------------------------------------------------------------------ a step of all four
 
 class Service:
