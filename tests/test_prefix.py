@@ -977,6 +977,93 @@ def test_caches_past_4_gib(dtype):
         assert small_k[s][:, lo:hi].any()
 
 
+def counted_prefill(monkeypatch, b, q, seqs, Hq, **how):
+    """run_prefill, and the parts that its rows were computed in, from what was
+    written of the workspace: rows x heads x parts x (head_dim + 2) fp32 numbers,
+    none for one part that goes straight to the output."""
+    used, call = [], lp.op_prefix_prefill_attention
+    monkeypatch.setattr(lp, "op_prefix_prefill_attention", lambda *args: (used.append(args[-1]), call(*args)))
+    got = run_prefill(b, q, seqs, Hq, **how)
+    monkeypatch.undo()
+    written = (used[0].view(torch.int32) != -1).nonzero()
+    return got, (int(written.max()) + 1) / (q.shape[0] * Hq * (b.hd + 2)) if len(written) else 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype,Hq,hd,P", [("f16", 32, 64, 8300), ("bf16", 16, 128, 0)])
+def test_one_walk_over_more_than_128_blocks(monkeypatch, dtype, Hq, hd, P):
+    """More blocks than a wave holds the places of at a time, three times over:
+    prompts in one walk of prefix and own blocks, one inside the prefix, a block
+    missing in the middle, and infinite values that the earlier rows' second
+    walk has to pass."""
+    rng = np.random.default_rng(hd)
+    Hkv, first, new = 2, 8300 + 100, 1000
+    b = Batch(rng, dtype, Hkv, hd, P, [first + new, 6900])
+    q = values(rng, (1100, Hq, hd), dtype)
+    gone = 90                                           # an entry of both sequences
+    b.table[b.slot[0], gone], b.table[b.slot[1], gone] = -1, -1
+    if P:
+        b.pre[gone] = -1
+        b.pre_t = i32(b.pre)
+    seqs = [(0, first, new), (1, 6800, 100)]
+    clean, parts = counted_prefill(monkeypatch, b, q, seqs, Hq)
+    assert parts == 0 and (first + new) // 64 > 128     # one walk
+    r = 0
+    for j, p, n in seqs:
+        some = np.unique(np.concatenate([np.arange(0, n, 97), [n - 1]]))
+        K, V = b.K[j], b.V[j]
+        keep = np.setdiff1d(np.arange(len(K)), np.arange(64 * gone, 64 * gone + 64))
+        ref, mag = (T.attention(q[r:r + n][some], K[keep], v[keep], p + some, keep, Hkv) for v in (V, np.abs(V)))
+        tol = bound(dtype, q[r:r + n][some], K[keep], V[keep], ref, mag)
+        assert np.all(np.abs(clean[r:r + n][some] - ref) <= tol), j
+        r += n
+    # rows before an infinite value keep their results to the bit, others are not finite
+    for j, bad, r0, r1 in ((0, first + 517, 517, 1000), (1, 6850, 1050, 1100)):
+        blk = int(b.pre[bad // 64] if bad < P else b.table[b.slot[j], bad // 64])
+        old = b.vc[blk, :, :, bad % 64].clone()
+        b.vc[blk, :, :, bad % 64] = float("inf")
+        got, parts = counted_prefill(monkeypatch, b, q, seqs, Hq)
+        b.vc[blk, :, :, bad % 64] = old
+        behind = np.arange(r0, r1)
+        if bad < P:
+            behind = np.concatenate([np.arange(1000), behind])      # the other sequence reads it too
+        before = np.setdiff1d(np.arange(1100), behind)
+        assert parts == 0 and not np.isfinite(got[behind]).any()
+        assert np.array_equal(got[before], clean[before])
+
+
+@gpu
+@pytest.mark.parametrize("dtype,Hq,P", [("f16", 8, 100), ("f16", 8, 0), ("f32", 1, 0), ("f32", 1, 100)])
+def test_join_of_more_than_64_parts(monkeypatch, dtype, Hq, P):
+    """Few new tokens after a long context of their own: the parts after the
+    64th, with larger scores than those before; short contexts below the same
+    max_ctx, whose later parts are empty; and rows whose first 64 parts are."""
+    rng = np.random.default_rng(P + Hq)
+    Hkv, hd, top, new = 1, 64, 60000, 30
+    b = Batch(rng, dtype, Hkv, hd, P, [top, P + 300])
+    b.kc[b.table[b.slot[0], 600:938]] *= 2              # exact
+    b.K[0][600 * 64:] *= 2
+    q = values(rng, (new, Hq, hd), dtype)
+
+    def check(got, q, j, positions, keep):
+        K, V = b.K[j][keep], b.V[j][keep]
+        ref, mag = (T.attention(q, K, v, positions, keep, Hkv) for v in (V, np.abs(V)))
+        assert np.all(np.abs(got - ref) <= bound(dtype, q, K, V, ref, mag)), j
+
+    got, parts = counted_prefill(monkeypatch, b, q, [(0, top - new, new)], Hq)
+    assert parts > 64
+    check(got, q, 0, np.arange(top - new, top), np.arange(top))
+    got, parts = counted_prefill(monkeypatch, b, q, [(1, P + 270, new)], Hq, max_ctx=top)
+    assert parts > 64
+    check(got, q, 1, np.arange(P + 270, P + 300), np.arange(P + 300))
+    b.table[b.slot[0], :650] = -1
+    if P:
+        b.pre_t = i32(np.full(len(b.pre), -1))
+    got, parts = counted_prefill(monkeypatch, b, q, [(0, top - new, new)], Hq)
+    assert parts > 64 and 650 / (938 / parts) > 64 + 4  # the prefix's parts and own ones before the first kept
+    check(got, q, 0, np.arange(top - new, top), np.arange(650 * 64, top))
+
+
 @gpu
 def test_graphs_that_share_a_workspace():
     """A prefill and a decode step captured with the same workspace, replayed in
