@@ -240,14 +240,16 @@ int lp_op_qkv_append(int32_t dtype, const float *qkv, int64_t ld, const float *r
 
 /* Decode attention with a shared prefix: row m of q, out [M][Hq][hd] reads
  * positions 0 .. row_pos[m] of slot row_slot[m], those below P from the
- * prefix's blocks, which are read once for the whole batch.  Contexts longer
- * than max_ctx are clamped to it (max_ctx, prefix_len and M Hq at most 2^30;
- * sizes whose work fills 2^23 workgroups, from M Hq = 2^25 on, are refused).
- * A row that reads nothing (position -1, no such slot, all its blocks missing)
- * gets zeros.  Any group Hq / Hkv; head_dim 64 or 128 in every dtype;
- * 64 * max_blocks >= max_ctx where max_ctx > P.
- * ws: at least lp_op_prefix_decode_attention_ws_bytes of the same sizes (0
- * for sizes that are refused). */
+ * prefix's blocks.  Contexts longer than max_ctx are clamped to it.  A row that
+ * reads nothing (position -1, no such slot, all its blocks missing) gets zeros.
+ * Any group Hq / Hkv; head_dim 64 or 128 in every dtype; 64 * max_blocks >=
+ * max_ctx where max_ctx > P.
+ * max_ctx, prefix_len and M Hq are at most 2^30.  A call that would launch 2^23
+ * workgroups or more is refused as well: none is with M Hq (16 + max_ctx / 4096)
+ * up to 2^22, all are from M Hq = 2^25 on.
+ * ws: at least lp_op_prefix_decode_attention_ws_bytes of the same sizes, which is
+ * 0 for sizes out of the limits above.  It does not look at the workgroups,
+ * which depend on dtype and sequences too: those show at the call. */
 size_t lp_op_prefix_decode_attention_ws_bytes(int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                               int32_t prefix_len, int32_t max_ctx);
 int lp_op_prefix_decode_attention(int32_t dtype, const void *q, void *out, const void *k_cache, const void *v_cache,
@@ -263,9 +265,11 @@ int lp_op_prefix_decode_attention(int32_t dtype, const void *q, void *out, const
  * positions 0 up to its own.  K and V of the new positions are in the cache
  * already, as are those before them (a sequence may go on from any context:
  * the prefix, one longer than it, or none of it).  Contexts and rows that read
- * nothing as for decode.  max_new bounds the rows of every sequence (rows of a
- * longer one from max_new on hold no result); rows of no sequence stay as they
- * are.  Sizes as for decode.  seq_start ascends; what of it lies outside 0 .. rows is left out. */
+ * nothing as for decode.  max_new bounds the rows of every sequence (rows of a longer one from
+ * max_new on hold no result); rows of no sequence stay as they are.  seq_start
+ * ascends; what of it lies outside 0 .. rows is left out.  Sequences
+ * without rows take no workgroups.  Limits and ws as for decode, with `rows`
+ * for M. */
 size_t lp_op_prefix_prefill_attention_ws_bytes(int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                                int32_t prefix_len, int32_t max_ctx);
 int lp_op_prefix_prefill_attention(int32_t dtype, const void *q, void *out, const void *k_cache, const void *v_cache,

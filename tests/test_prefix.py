@@ -936,6 +936,29 @@ def test_rows_past_max_new(dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_the_largest_batches_that_always_fit(dtype):
+    """Rows times heads times (16 + max_ctx / 4,096) just under 2^22, of which some rows are looked at."""
+    rng = np.random.default_rng(22)
+    M, Hq, Hkv, hd, P, ctx = 4070, 64, 8, 64, 100, [101, 228, 300]
+    assert M * Hq * (16 + 300 / 4096) <= 1 << 22 < (M + 10) * Hq * (16 + 300 / 4096)
+    b = Batch(rng, dtype, Hkv, hd, P, ctx)
+    q = values(rng, (M, Hq, hd), dtype)
+    rows = [(m % 3, ctx[m % 3] - 1) for m in range(M)]
+    got = run_decode(b, q, rows, Hq)
+    some = [0, 1, 2, 2047, 2048, 3001, M - 2, M - 1]
+    for m in some:
+        j, p = rows[m]
+        ref, tol = b.reference(q[m:m + 1], j, [p])
+        assert np.all(np.abs(got[m:m + 1] - ref) <= tol), m
+    got = run_prefill(b, q, [(j, p, 1) for j, p in rows], Hq)
+    for m in some:
+        j, p = rows[m]
+        ref, tol = b.reference(q[m:m + 1], j, [p])
+        assert np.all(np.abs(got[m:m + 1] - ref) <= tol), m
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_caches_past_4_gib(dtype):
     """Blocks whose byte (f32: also element) offsets pass 32 bits: what a small cache gives, to the bit."""
     rng = np.random.default_rng(21)
@@ -1232,6 +1255,22 @@ def test_work_past_one_launch_is_refused(decode):
         args = [dtype, A, A, A, A, 50, A, P, A, 4, 1 << 24, *seqs, Hq, Hkv, 64, ctx, A, 1 << 60, None]
         assert f(*args) == EINVAL, (dtype, rows)
         assert "launch" in L.lp_last_error(None).decode()
+
+
+@pytest.mark.parametrize("decode", [True, False])
+@pytest.mark.parametrize("dtype", [F16, lp.LP_BF16, F32])
+def test_row_and_head_pairs_past_one_launch_are_refused(decode, dtype):
+    """From 2^25 pairs on, whatever the contexts; the workspace's size, which
+    depends on neither dtype nor sequences, is that of the limits alone."""
+    L = lp.lib()
+    f = L.lp_op_prefix_decode_attention if decode else L.lp_op_prefix_prefill_attention
+    size = L.lp_op_prefix_decode_attention_ws_bytes if decode else L.lp_op_prefix_prefill_attention_ws_bytes
+    for rows, Hq, Hkv, P, ctx in ((1 << 20, 32, 8, 0, 1), (1 << 20, 32, 8, 64, 50), (1 << 22, 8, 8, 5000, 5100), (1 << 29, 1, 1, 64, 70)):
+        seqs = [A, A, rows] if decode else [A, A, A, 1, rows, rows]
+        assert f(dtype, A, A, A, A, 50, A, P, A, 4, 1000, *seqs, Hq, Hkv, 64, ctx, A, 1 << 60, None) == EINVAL, (rows, Hq)
+        assert "launch" in L.lp_last_error(None).decode()
+        assert size(rows, Hq, Hkv, 64, P, ctx) > 0
+    assert size((1 << 25) + 1, 32, 8, 64, 64, 70) == size(1, 8, 8, 64, 0, (1 << 30) + 1) == size(1, 8, 8, 64, (1 << 30) + 1, 9) == 0
 
 
 def test_loads_into_lds_keep_their_wait_states(tmp_path):
