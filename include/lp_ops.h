@@ -241,9 +241,9 @@ int lp_op_qkv_append(int32_t dtype, const float *qkv, int64_t ld, const float *r
 /* Decode attention with a shared prefix: row m of q, out [M][Hq][hd] reads
  * positions 0 .. row_pos[m] of slot row_slot[m], those below P from the
  * prefix's blocks.  Contexts longer than max_ctx are clamped to it.  A row that
- * reads nothing (position -1, no such slot, all its blocks missing) gets zeros.
- * Any group Hq / Hkv; head_dim 64 or 128 in every dtype; 64 * max_blocks >=
- * max_ctx where max_ctx > P.
+ * reads nothing (position -1, no such slot, all its blocks missing), or whose
+ * every score is minus infinity, gets zeros.  Any group Hq / Hkv; head_dim 64
+ * or 128 in every dtype; 64 * max_blocks >= max_ctx where max_ctx > P.
  * max_ctx, prefix_len and M Hq are at most 2^30.  A call that would launch 2^23
  * workgroups or more is refused as well: none is with M Hq (16 + max_ctx / 4096)
  * up to 2^22, all are from M Hq = 2^25 on.
@@ -265,9 +265,10 @@ int lp_op_prefix_decode_attention(int32_t dtype, const void *q, void *out, const
  * positions 0 up to its own.  K and V of the new positions are in the cache
  * already, as are those before them (a sequence may go on from any context:
  * the prefix, one longer than it, or none of it).  Contexts and rows that read
- * nothing as for decode.  max_new bounds the rows of every sequence (rows of a longer one from
+ * nothing as for decode; all rows of a sequence whose seq_pos is negative are
+ * such.  max_new bounds the rows of every sequence (rows of a longer one from
  * max_new on hold no result); rows of no sequence stay as they are.  seq_start
- * ascends; what of it lies outside 0 .. rows is left out.  Sequences
+ * ascends; entries below 0 count as 0, those above `rows` as `rows`.  Sequences
  * without rows take no workgroups.  Limits and ws as for decode, with `rows`
  * for M. */
 size_t lp_op_prefix_prefill_attention_ws_bytes(int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,

@@ -935,6 +935,77 @@ def test_rows_past_max_new(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("f16", 8, 2, 128), ("bf16", 4, 4, 64), ("f32", 4, 2, 64)])
+def test_scores_of_minus_infinity(dtype, Hq, Hkv, hd):
+    """Infinite keys: rows that they score minus infinity leave them out, get
+    zeros where every key is such a one, and NaN where a score is plus infinity."""
+    rng = np.random.default_rng(hd + Hq)
+    P, ctx = 300, [301, 420, 300, 1200]
+    b = Batch(rng, dtype, Hkv, hd, P, ctx)
+
+    def rows_of(n):             # the first dimension's sign decides
+        q = values(rng, (n, Hq, hd), dtype)
+        q[..., 0] = np.where(np.arange(n) % 4 == 3, 1.0, -1.0)[:, None]
+        return q
+
+    def infinite(j, lo, hi):
+        for p in range(lo, hi):
+            b.kc[int(b.pre[p // 64] if p < P else b.table[b.slot[j], p // 64]), :, p % 64, 0] = float("inf")
+
+    def check(got, q, j, p, gone):
+        keep = np.array([i for i in range(p + 1) if not any(lo <= i < hi for k, lo, hi in gone if k in (j, None))], int)
+        if (q[0, 0, 0] > 0 and len(keep) <= p):
+            assert np.isnan(got).all(), (j, p)
+        elif not len(keep):
+            assert np.all(got == 0), (j, p)
+        else:
+            K, V = b.K[j][keep], b.V[j][keep]
+            ref, mag = (T.attention(q, K, v, [p], keep, Hkv) for v in (V, np.abs(V)))
+            assert np.all(np.abs(got - ref) <= bound(dtype, q, K, V, ref, mag)), (j, p)
+
+    # a few keys in both; then the whole prefix and the first own keys
+    gone = [(None, 100, 140), (3, 301, 310), (3, 700, 900)]
+    for step in range(2):
+        for j, lo, hi in gone:
+            infinite(j, lo, hi)
+        for n in (4, 44):       # few rows, and a batch that fills a tile
+            rows = [(m % 4, [ctx[m % 4] - 1, 130, 99, 299, 311 if m % 4 == 1 else 250][m % 5]) for m in range(n)]
+            q = rows_of(n)
+            got = run_decode(b, q, rows, Hq)
+            for m, (j, p) in enumerate(rows):
+                check(got[m:m + 1], q[m:m + 1], j, p, gone)
+        seqs = [(1, 290, 130), (2, 90, 60), (3, 1150, 50)]
+        q, r = rows_of(240), 0
+        got = run_prefill(b, q, seqs, Hq)
+        for j, p, n in seqs:
+            for i in range(n):
+                check(got[r + i:r + i + 1], q[r + i:r + i + 1], j, p + i, gone)
+            r += n
+        gone = [(None, 0, 300), (3, 300, 310), (3, 700, 900)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_sequences_that_leave_the_rows(dtype):
+    """Entries of seq_start below 0 and above the rows count as these; a negative seq_pos is no row with keys."""
+    rng = np.random.default_rng(4)
+    P, Hq, Hkv, hd, n = 100, 4, 2, 64, 50
+    b = Batch(rng, dtype, Hkv, hd, P, [P + 60] * 3)
+    q = values(rng, (n, Hq, hd), dtype)
+    for max_new in (n, 100):
+        out = torch.full((n, Hq, hd), 7.0, dtype=TYPES[dtype], device=DEV)
+        ws = torch.empty(lp.prefix_prefill_attention_ws_bytes(n, Hq, Hkv, hd, P, P + 60), dtype=torch.uint8, device=DEV)
+        lp.op_prefix_prefill_attention(torch.from_numpy(q).to(TYPES[dtype]).to(DEV), out, b.kc, b.vc, b.pre_t, P, i32(b.table),
+                                       i32([-9, 12, 30, 70, 90]), i32([b.slot[0], b.slot[1], b.slot[2], b.slot[0]]),
+                                       i32([P, -3, P + 20, 5]), max_new, P + 60, ws)
+        got = out.double().cpu().numpy()
+        for j, r0, r1, p in ((0, 0, 12, P), (2, 30, 50, P + 20)):
+            ref, tol = b.reference(q[r0:r1], j, np.arange(p, p + r1 - r0))
+            assert np.all(np.abs(got[r0:r1] - ref) <= tol), j
+        assert np.all(got[12:30] == 0)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_the_largest_batches_that_always_fit(dtype):
     """Rows times heads times (16 + max_ctx / 4,096) just under 2^22, of which some rows are looked at."""
