@@ -437,6 +437,8 @@ __device__ __forceinline__ void tile_item(const T *__restrict__ q, T *__restrict
             p[r] = __builtin_amdgcn_exp2f(fmaf(s[t][u * 8 + r], c2, -mo));
             lsum += p[r];
           }
+          // the one rounding below 32 bits before the result's: the matrix instruction
+          // of 16-bit V takes 16-bit weights (their sum stays fp32 and unrounded)
           pb[t * 2 + u] = pack8<T>(p);
         }
       if (careful && partly) {
@@ -731,7 +733,7 @@ __device__ __forceinline__ void rows_item(const T *__restrict__ q, T *__restrict
         for (int nt = 0; nt < 2; ++nt) {
           const float p = __builtin_amdgcn_exp2f((s[nt][y] - m0) * c2);
           sm[y] += p;
-          pls[4 * quad + y][nt * 16 + r16] = round_to<T>(p);
+          pls[4 * quad + y][nt * 16 + r16] = round_to<T>(p);  // as in tile_item; fp32 keeps all bits
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) o[nt][y] *= corr;
@@ -975,7 +977,8 @@ static int most_splits(int nP) { return nP <= 32 ? ceil_div(nP, 2) : std::max(16
 // Blocks of a split of the prefix for `items` tiles and KV heads.  In units of a
 // block's time where two workgroups share a CU (about 2 us), an item of n blocks
 // takes n + 4, 512 run at once, the work spread over them ends half the shortest
-// item after its mean, and a split costs its partials' way to memory and back.
+// item after its mean, and a split costs its partials' way to memory and back (the
+// 4 and PART, per row and head, are fitted to the batches below).
 // Splits are even, or the last one is half as long, so that other items begin
 // where it ends.  Measured (graphs of calls; prompts' rows x tokens of prefix,
 // blocks of a split): 8B 640 x 1,500 6 blocks 53.4 us, 8 46.7, 12 44.0, 24 55.5;
@@ -1067,8 +1070,8 @@ static void prefix_plan(PrefixArgs &a, bool decode, bool half, int rows, int n_h
     // Prompts may instead walk the prefix and their own blocks in one item, and
     // nothing is joined: in the units of tile_split, every round of 512 items takes
     // the prefix, the first (or with more, about half) the longest own context; a
-    // sequence's last tile is half full.  Right for 30 of 33 batches measured, the
-    // others within 10% (walk against splits): 70B three prompts of 2,100 over 4,096
+    // sequence's last tile is half full.  The 3 and 1.05 are fitted: right for 30 of
+    // 33 batches measured, the others within 11% (walk against splits): 70B three prompts of 2,100 over 4,096
     // tokens 686 us and 800, 8 of 100 over 1,000 50 and 69, 32 of 30 over 2,000 125 and
     // 109; 13B two of 800 over 3,000 149 and 165; 8B 16 of 120 over 2,000 135 and 115,
     // one of 2,500 over 4,000 313 and 283 (taken for 304 and 313).
@@ -1112,7 +1115,9 @@ static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   constexpr bool half = sizeof(T) == 2;
   const bool decode = !b.seq_start;
   // Sequences that can have rows: a batch of fixed size may hold many more places,
-  // and each that owned a tile would cost a search through all of seq_start.
+  // and each that owned a tile would cost a search through all of seq_start (8B
+  // heads, five prompts of 40 over 1,500 tokens: in 5 places 22 us, in 8,192 124;
+  // with a tile for every place 4,221).
   const int live = std::min(b.n_seq, b.rows);
   prefix_plan(a, decode, half, b.rows, b.n_heads, Hkv, b.prefix_len, b.max_ctx, live);
   a.po = ws;
