@@ -1,7 +1,7 @@
 /* lp_ops.h -- single-kernel entry points of the serving step, for parity
  * checks and kernel timing.  They launch exactly the kernels the engine runs
- * (those of the last section, a batch that shares a prefix, are for callers
- * that plan their own steps), on caller-provided device buffers,
+ * (those of the last two sections, a batch that shares a prefix and a cache
+ * held in 4 bits, are for callers that plan their own steps), on caller-provided device buffers,
  * asynchronously on `hip_stream` (a hipStream_t, NULL for the null stream).
  * All pointers are device pointers unless stated otherwise; the caller owns
  * every buffer.  Each returns LP_OK or
@@ -279,6 +279,89 @@ int lp_op_prefix_prefill_attention(int32_t dtype, const void *q, void *out, cons
                                    const int32_t *seq_start, const int32_t *seq_slot, const int32_t *seq_pos,
                                    int32_t n_seq, int32_t rows, int32_t max_new, int32_t n_heads, int32_t n_kv_heads,
                                    int32_t head_dim, int32_t max_ctx, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* ---- a K/V cache held in 4 bits ----
+ *
+ * The contexts of decode are read at the rate of the memory, and they fill it: a
+ * cache of 4.5 bits a value holds 3.6 times the positions of a 16-bit one and is
+ * read 3.6 times as fast.  The calls below write it, attend over it and bring
+ * entries back; block ids, entries (64 * block + place), slots and positions are
+ * those of the calls above (lp_op_block_tables makes them, with prefix_len 0 or
+ * a multiple of 64), and so are the rules for what does not fit: it is left out,
+ * never read or written through.  q, out, the caches and ws start on 16 bytes
+ * (LP_EINVAL otherwise); ws needs no clearing, and calls that overlap in time
+ * need one each.
+ *
+ * 32 consecutive dims of a head at one position are a group, with one scale s:
+ * the least number that is not below a sixth of the group's largest magnitude
+ * and is a multiple of 2^-23 of at most 6 significant bits; at most 10,752; NaN
+ * if the group holds an infinity or NaN (all its values are then NaN).  A value
+ * is held as its sign and the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (codes 0 ..
+ * 7) times s, of two equally near ones the even code; past 6 s, 6.  The values
+ * held have 8 significant bits and are exact in every dtype.
+ *
+ * cache: for each block and KV head 72 head_dim bytes, [n_blocks][Hkv][72 hd],
+ * that do not depend on dtype.  With J = hd / 32, a byte two codes (sign above
+ * the three bits), the lower dim in the low half:
+ *   K codes   [64][hd / 2]       byte 4 J i + 4 j + b: dims 32 j + 8 i + 2 b and
+ *                                the next (i, b < 4, j < J)
+ *   K scales  [64][J] fp16
+ *   V codes   [16][hd / 8][4][4] word w of positions 4 n .. 4 n + 3 side by side;
+ *                                byte J r + j of a position's hd / 2 bytes: dims
+ *                                32 j + 2 r and the next (r < 16)
+ *   V scales  [J][64] fp16
+ * Any bytes are a cache: places that no row may read need not be cleared. */
+
+/* Bytes of a cache; 0 for sizes that no call takes. */
+size_t lp_op_kv4_cache_bytes(int64_t n_blocks, int32_t n_kv_heads, int32_t head_dim);
+
+/* lp_op_qkv_append into a cache held in 4 bits: the same arguments, rotation,
+ * rules and limits, with K (rotated) and V quantised from fp32 at row_entry;
+ * dtype is q's. */
+int lp_op_kv4_append(int32_t dtype, const float *qkv, int64_t ld, const float *rope_cos, const float *rope_sin,
+                     int32_t n_pos, const int32_t *row_pos, const int64_t *row_entry, int32_t rows, void *q,
+                     void *cache, int64_t n_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                     void *hip_stream);
+
+/* Entries of a 4-bit cache back into an ordinary cache of dtype (k_cache
+ * [n_dst_blocks][Hkv][64][hd], v_cache [n_dst_blocks][Hkv][hd][64]): K and V of
+ * src_entry[i] go to dst_entry[i], i < rows, exactly.  Rows with either entry
+ * outside its cache are left out.  No two rows may have the same dst_entry.
+ * rows Hkv at most 2^26. */
+int lp_op_kv4_read(int32_t dtype, const void *cache, int64_t n_blocks, const int64_t *src_entry,
+                   const int64_t *dst_entry, int32_t rows, void *k_cache, void *v_cache, int64_t n_dst_blocks,
+                   int32_t n_kv_heads, int32_t head_dim, void *hip_stream);
+
+/* Decode attention over a 4-bit cache: row m of q, out [M][Hq][hd] reads
+ * positions 0 .. row_pos[m] of slot row_slot[m].  Contexts longer than max_ctx
+ * are clamped to it; 64 * max_blocks >= max_ctx.  A row that reads nothing
+ * (position -1, no such slot, all its blocks missing) gets zeros.  Any group Hq
+ * / Hkv; head_dim 64 or 128.  max_ctx and M Hq are at most 2^30, and a call that
+ * would launch 2^23 workgroups or more is refused as well.
+ * ws: at least lp_op_kv4_decode_attention_ws_bytes of the same sizes (0 for
+ * sizes out of these limits). */
+size_t lp_op_kv4_decode_attention_ws_bytes(int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                           int32_t max_ctx);
+int lp_op_kv4_decode_attention(int32_t dtype, const void *q, void *out, const void *cache, int64_t n_blocks,
+                               const int32_t *block_table, int32_t n_slots, int32_t max_blocks,
+                               const int32_t *row_slot, const int32_t *row_pos, int32_t M, int32_t n_heads,
+                               int32_t n_kv_heads, int32_t head_dim, int32_t max_ctx, void *ws, size_t ws_bytes,
+                               void *hip_stream);
+
+/* Causal attention of packed new tokens over a 4-bit cache: sequence j owns rows
+ * [seq_start[j], seq_start[j + 1]) of q, out [rows][Hq][hd], at positions
+ * seq_pos[j], seq_pos[j] + 1, ... of slot seq_slot[j]; each row reads positions
+ * 0 up to its own, the new ones among them as the cache holds them.  Rows,
+ * offsets, max_new and rows of no sequence as for
+ * lp_op_prefix_prefill_attention; limits and ws as for decode, with `rows` for
+ * M. */
+size_t lp_op_kv4_prefill_attention_ws_bytes(int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                            int32_t max_ctx);
+int lp_op_kv4_prefill_attention(int32_t dtype, const void *q, void *out, const void *cache, int64_t n_blocks,
+                                const int32_t *block_table, int32_t n_slots, int32_t max_blocks,
+                                const int32_t *seq_start, const int32_t *seq_slot, const int32_t *seq_pos,
+                                int32_t n_seq, int32_t rows, int32_t max_new, int32_t n_heads, int32_t n_kv_heads,
+                                int32_t head_dim, int32_t max_ctx, void *ws, size_t ws_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -195,6 +195,25 @@ struct QkvAppend {
 template <typename T>
 void launch_qkv_append(const QkvAppend &a, T *q, T *k, T *v, hipStream_t s);
 
+// A cache held in 4 bits (kv4.hpp): QKV append into it (`cache` in the place of
+// both caches), entries of it back into an ordinary cache, and attention over it.
+// For attention kv.k of the batch is the 4-bit cache, and there is no prefix.
+template <typename T>
+void launch_kv4_append(const QkvAppend &a, T *q, uint8_t *cache, hipStream_t s);
+struct Kv4Read {
+  const uint8_t *cache;
+  int64_t n_blocks;
+  const int64_t *src_entry, *dst_entry;
+  int64_t n_dst_blocks;
+  int32_t rows, n_kv_heads, head_dim;
+};
+template <typename T>
+void launch_kv4_read(const Kv4Read &a, T *k, T *v, hipStream_t s);
+size_t kv4_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_heads, int head_dim, int max_ctx);
+// False, with nothing launched, where the sizes need more workgroups than a launch may have.
+template <typename T>
+bool launch_kv4_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s);
+
 // Greedy token per row (lowest index on ties): tok -> slot_tok[out_slot[m]]
 // and tok_log[m].
 void launch_argmax(const float *logits, int64_t ld, int M, int V, const int32_t *out_slot,

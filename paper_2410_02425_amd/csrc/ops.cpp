@@ -232,24 +232,32 @@ extern "C" int lp_op_block_tables(const int32_t *seq_slot, const int32_t *cached
   return op_status();
 }
 
+// The checks that both appends share (into a 4-bit cache: it is both of the caches).
+static int append_args(const QkvAppend &a, int32_t dtype, const void *q, const void *k_cache, const void *v_cache) {
+  OPCHK(a.n_heads > 0 && a.n_kv_heads > 0 && a.n_heads % a.n_kv_heads == 0, "qkv append: heads");
+  OPCHK(a.head_dim == 64 || a.head_dim == 128, "qkv append: head_dim must be 64 or 128");
+  OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "qkv append: dtype");
+  OPCHK(a.rows >= 0 && a.n_pos > 0 && a.n_blocks > 0 && a.ld % 2 == 0 &&
+            a.ld >= ((int64_t)a.n_heads + 2 * (int64_t)a.n_kv_heads) * a.head_dim &&
+            a.rows * ((int64_t)a.n_heads + 2 * (int64_t)a.n_kv_heads) <= 1 << 23,
+        "qkv append: sizes");
+  if (a.rows == 0) return LP_OK;  // no rows: nothing is read or written
+  OPCHK(a.qkv && a.rope_cos && a.rope_sin && a.row_pos && a.row_entry && q && k_cache && v_cache,
+        "qkv append: pointers");
+  OPCHK((((uintptr_t)a.qkv | (uintptr_t)a.rope_cos | (uintptr_t)a.rope_sin) & 7) == 0,
+        "qkv append: qkv and the rotary tables start on 8 bytes");
+  OPCHK(aligned16(q) && aligned16(k_cache) && aligned16(v_cache), "qkv append: q and the caches start on 16 bytes");
+  return LP_OK;
+}
+
 extern "C" int lp_op_qkv_append(int32_t dtype, const float *qkv, int64_t ld, const float *rope_cos,
                                 const float *rope_sin, int32_t n_pos, const int32_t *row_pos,
                                 const int64_t *row_entry, int32_t rows, void *q, void *k_cache, void *v_cache,
                                 int64_t n_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                 void *stream) {
-  OPCHK(n_heads > 0 && n_kv_heads > 0 && n_heads % n_kv_heads == 0, "qkv append: heads");
-  OPCHK(head_dim == 64 || head_dim == 128, "qkv append: head_dim must be 64 or 128");
-  OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "qkv append: dtype");
-  OPCHK(rows >= 0 && n_pos > 0 && n_blocks > 0 && ld % 2 == 0 &&
-            ld >= ((int64_t)n_heads + 2 * (int64_t)n_kv_heads) * head_dim &&
-            rows * ((int64_t)n_heads + 2 * (int64_t)n_kv_heads) <= 1 << 23,
-        "qkv append: sizes");
-  if (rows == 0) return LP_OK;  // no rows: nothing is read or written
-  OPCHK(qkv && rope_cos && rope_sin && row_pos && row_entry && q && k_cache && v_cache, "qkv append: pointers");
-  OPCHK((((uintptr_t)qkv | (uintptr_t)rope_cos | (uintptr_t)rope_sin) & 7) == 0,
-        "qkv append: qkv and the rotary tables start on 8 bytes");
-  OPCHK(aligned16(q) && aligned16(k_cache) && aligned16(v_cache), "qkv append: q and the caches start on 16 bytes");
   QkvAppend a{qkv, ld, rope_cos, rope_sin, row_pos, row_entry, n_blocks, n_pos, rows, n_heads, n_kv_heads, head_dim};
+  const int rc = append_args(a, dtype, q, k_cache, v_cache);
+  if (rc || rows == 0) return rc;
   hipStream_t s = (hipStream_t)stream;
   if (dtype == LP_BF16)
     launch_qkv_append<bf16_t>(a, (bf16_t *)q, (bf16_t *)k_cache, (bf16_t *)v_cache, s);
@@ -332,4 +340,111 @@ extern "C" int lp_op_prefix_prefill_attention(int32_t dtype, const void *q, void
                 prefix_blocks, prefix_len, n_slots, seq_start, seq_slot, seq_pos, n_seq, rows, max_new, max_ctx,
                 n_heads};
   return prefix_attention(dtype, q, out, b, false, ws, ws_bytes, stream);
+}
+
+// ------------------------------------------------------------------ a cache held in 4 bits
+
+extern "C" size_t lp_op_kv4_cache_bytes(int64_t n_blocks, int32_t n_kv_heads, int32_t head_dim) {
+  if (n_blocks <= 0 || n_kv_heads <= 0 || (head_dim != 64 && head_dim != 128)) return 0;
+  return (size_t)n_blocks * n_kv_heads * 72 * head_dim;
+}
+
+extern "C" int lp_op_kv4_append(int32_t dtype, const float *qkv, int64_t ld, const float *rope_cos,
+                                const float *rope_sin, int32_t n_pos, const int32_t *row_pos,
+                                const int64_t *row_entry, int32_t rows, void *q, void *cache, int64_t n_blocks,
+                                int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, void *stream) {
+  QkvAppend a{qkv, ld, rope_cos, rope_sin, row_pos, row_entry, n_blocks, n_pos, rows, n_heads, n_kv_heads, head_dim};
+  const int rc = append_args(a, dtype, q, cache, cache);
+  if (rc || rows == 0) return rc;
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == LP_BF16)
+    launch_kv4_append<bf16_t>(a, (bf16_t *)q, (uint8_t *)cache, s);
+  else if (dtype == LP_F16)
+    launch_kv4_append<f16_t>(a, (f16_t *)q, (uint8_t *)cache, s);
+  else
+    launch_kv4_append<float>(a, (float *)q, (uint8_t *)cache, s);
+  return op_status();
+}
+
+extern "C" int lp_op_kv4_read(int32_t dtype, const void *cache, int64_t n_blocks, const int64_t *src_entry,
+                              const int64_t *dst_entry, int32_t rows, void *k_cache, void *v_cache,
+                              int64_t n_dst_blocks, int32_t n_kv_heads, int32_t head_dim, void *stream) {
+  OPCHK(n_kv_heads > 0 && (head_dim == 64 || head_dim == 128), "kv4 read: heads, head_dim 64 or 128");
+  OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "kv4 read: dtype");
+  OPCHK(rows >= 0 && n_blocks > 0 && n_dst_blocks > 0 && (int64_t)rows * n_kv_heads <= 1 << 26, "kv4 read: sizes");
+  if (rows == 0) return LP_OK;  // no rows: nothing is read or written
+  OPCHK(cache && src_entry && dst_entry && k_cache && v_cache, "kv4 read: pointers");
+  OPCHK(aligned16(cache) && aligned16(k_cache) && aligned16(v_cache), "kv4 read: the caches start on 16 bytes");
+  Kv4Read a{(const uint8_t *)cache, n_blocks, src_entry, dst_entry, n_dst_blocks, rows, n_kv_heads, head_dim};
+  hipStream_t s = (hipStream_t)stream;
+  if (dtype == LP_BF16)
+    launch_kv4_read<bf16_t>(a, (bf16_t *)k_cache, (bf16_t *)v_cache, s);
+  else if (dtype == LP_F16)
+    launch_kv4_read<f16_t>(a, (f16_t *)k_cache, (f16_t *)v_cache, s);
+  else
+    launch_kv4_read<float>(a, (float *)k_cache, (float *)v_cache, s);
+  return op_status();
+}
+
+extern "C" size_t lp_op_kv4_decode_attention_ws_bytes(int32_t M, int32_t n_heads, int32_t n_kv_heads,
+                                                      int32_t head_dim, int32_t max_ctx) {
+  if (!prefix_sizes(M, n_heads, n_kv_heads, head_dim, 0, max_ctx)) return 0;
+  return kv4_attention_ws_bytes(true, M, n_heads, n_kv_heads, head_dim, max_ctx);
+}
+
+extern "C" size_t lp_op_kv4_prefill_attention_ws_bytes(int32_t rows, int32_t n_heads, int32_t n_kv_heads,
+                                                       int32_t head_dim, int32_t max_ctx) {
+  if (!prefix_sizes(rows, n_heads, n_kv_heads, head_dim, 0, max_ctx)) return 0;
+  return kv4_attention_ws_bytes(false, rows, n_heads, n_kv_heads, head_dim, max_ctx);
+}
+
+// The checks that both phases share; `b` is complete but for them.
+static int kv4_attention(int32_t dtype, const void *q, void *out, const PrefixBatch &b, bool decode, void *ws,
+                         size_t ws_bytes, void *stream) {
+  OPCHK(prefix_sizes(b.rows, b.n_heads, b.kv.n_kv_heads, b.kv.head_dim, 0, b.max_ctx),
+        "kv4 attention: sizes (rows, heads, head_dim 64 or 128, max_ctx)");
+  OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "kv4 attention: dtype");
+  OPCHK(b.n_seq >= 0 && b.n_seq <= PREFIX_MAX_POS && b.kv.n_blocks > 0 && b.n_slots > 0 && b.max_new > 0,
+        "kv4 attention: sizes");
+  OPCHK(b.kv.max_blocks > 0 && (int64_t)b.kv.max_blocks * KV_BLOCK >= b.max_ctx,
+        "kv4 attention: max_blocks too small for max_ctx");
+  if (b.rows == 0 || b.n_seq == 0) return LP_OK;  // no rows: nothing is read or written
+  OPCHK(q && out && b.kv.k && b.kv.block_table && b.seq_slot && b.seq_pos && (decode || b.seq_start),
+        "kv4 attention: pointers");
+  OPCHK(aligned16(q) && aligned16(out) && aligned16(b.kv.k) && aligned16(ws),
+        "kv4 attention: q, out, the cache and ws start on 16 bytes");
+  const size_t need =
+      kv4_attention_ws_bytes(decode, b.rows, b.n_heads, b.kv.n_kv_heads, b.kv.head_dim, b.max_ctx);
+  OPCHK(need == 0 || (ws && ws_bytes >= need), "kv4 attention: ws");
+  hipStream_t s = (hipStream_t)stream;
+  bool fits;
+  if (dtype == LP_BF16)
+    fits = launch_kv4_attention<bf16_t>((const bf16_t *)q, (bf16_t *)out, b, (float *)ws, s);
+  else if (dtype == LP_F16)
+    fits = launch_kv4_attention<f16_t>((const f16_t *)q, (f16_t *)out, b, (float *)ws, s);
+  else
+    fits = launch_kv4_attention<float>((const float *)q, (float *)out, b, (float *)ws, s);
+  OPCHK(fits, "kv4 attention: more rows, heads and blocks than one launch takes");
+  return op_status();
+}
+
+extern "C" int lp_op_kv4_decode_attention(int32_t dtype, const void *q, void *out, const void *cache,
+                                          int64_t n_blocks, const int32_t *block_table, int32_t n_slots,
+                                          int32_t max_blocks, const int32_t *row_slot, const int32_t *row_pos,
+                                          int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                          int32_t max_ctx, void *ws, size_t ws_bytes, void *stream) {
+  PrefixBatch b{{(void *)cache, nullptr, block_table, max_blocks, n_blocks, n_kv_heads, head_dim},
+                nullptr, 0, n_slots, nullptr, row_slot, row_pos, M, M, 1, max_ctx, n_heads};
+  return kv4_attention(dtype, q, out, b, true, ws, ws_bytes, stream);
+}
+
+extern "C" int lp_op_kv4_prefill_attention(int32_t dtype, const void *q, void *out, const void *cache,
+                                           int64_t n_blocks, const int32_t *block_table, int32_t n_slots,
+                                           int32_t max_blocks, const int32_t *seq_start, const int32_t *seq_slot,
+                                           const int32_t *seq_pos, int32_t n_seq, int32_t rows, int32_t max_new,
+                                           int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_ctx,
+                                           void *ws, size_t ws_bytes, void *stream) {
+  PrefixBatch b{{(void *)cache, nullptr, block_table, max_blocks, n_blocks, n_kv_heads, head_dim},
+                nullptr, 0, n_slots, seq_start, seq_slot, seq_pos, n_seq, rows, max_new, max_ctx, n_heads};
+  return kv4_attention(dtype, q, out, b, false, ws, ws_bytes, stream);
 }

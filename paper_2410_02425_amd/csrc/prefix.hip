@@ -16,23 +16,10 @@
 #include <cmath>
 #include <type_traits>
 
+#include "batch.hpp"
 #include "device.hpp"
 
 namespace lp {
-
-// n / d for n >= 0 with m = floor(2^32 / d) (all ones for d = 1): n m / 2^32 is
-// at most one short, which the remainder shows.
-struct Divisor {
-  uint32_t d, m;
-};
-__device__ __forceinline__ int div_by(int n, Divisor x) {
-  const uint32_t k = __umulhi((uint32_t)n, x.m);
-  return (int)(k + ((uint32_t)n - k * x.d >= x.d ? 1 : 0));
-}
-static Divisor divisor(int d) {
-  const uint32_t u = (uint32_t)std::max(d, 1);
-  return {u, u > 1 ? (uint32_t)((1ull << 32) / u) : 0xFFFFFFFFu};
-}
 
 struct PrefixArgs {
   PrefixBatch b;
@@ -62,25 +49,6 @@ struct PrefixRow {
 __device__ __forceinline__ PrefixRow packed_row(const PrefixArgs &a, int start, int r0, int l, int g) {
   const int t0 = div_by(r0, a.by_g), x = r0 - t0 * a.G + l, dt = div_by(x, a.by_g);
   return PrefixRow{start + t0 + dt, g * a.G + x - dt * a.G, t0 + dt};
-}
-
-// Sequence j's first row and row count, inside the batch's rows.
-__device__ __forceinline__ void seq_rows(const PrefixBatch &b, int j, int &start, int &n) {
-  if (!b.seq_start) {
-    start = j;
-    n = 1;
-    return;
-  }
-  start = min(max(b.seq_start[j], 0), b.rows);
-  n = min(max(b.seq_start[j + 1], start), b.rows) - start;
-}
-
-// Keys that row i of sequence j sees.
-__device__ __forceinline__ int row_ctx(const PrefixBatch &b, int j, int i) {
-  const int slot = b.seq_slot[j], p0 = b.seq_pos[j];
-  if (slot < 0 || slot >= b.n_slots) return 0;
-  const int64_t ctx = (int64_t)p0 + i + 1;
-  return p0 < 0 ? 0 : (int)min(ctx, (int64_t)b.max_ctx);
 }
 
 // Keys that a packed row sees, -1 if the row does not exist: token t of sequence
@@ -956,8 +924,6 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
 }
 
 // ------------------------------------------------------------------ plan
-
-static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // A decode batch whose rows each see at most WHOLE_ENTRIES blocks, and whose rows
 // and KV heads are at most WHOLE_ITEMS, takes a workgroup per row and KV head

@@ -29,6 +29,8 @@ EXPORTED = [
     "lp_op_prefill_attention", "lp_op_argmax", "lp_op_init_weight", "lp_op_sample",
     "lp_op_block_tables", "lp_op_qkv_append", "lp_op_prefix_decode_attention_ws_bytes",
     "lp_op_prefix_decode_attention", "lp_op_prefix_prefill_attention_ws_bytes", "lp_op_prefix_prefill_attention",
+    "lp_op_kv4_cache_bytes", "lp_op_kv4_append", "lp_op_kv4_read", "lp_op_kv4_decode_attention_ws_bytes",
+    "lp_op_kv4_decode_attention", "lp_op_kv4_prefill_attention_ws_bytes", "lp_op_kv4_prefill_attention",
 ]
 
 
@@ -135,6 +137,12 @@ def lib():
                                               i32, i32, vp, sz, vp],
             "lp_op_prefix_prefill_attention": [i32, vp, vp, vp, vp, i64, vp, i32, vp, i32, i32, vp, vp, vp, i32, i32,
                                                i32, i32, i32, i32, i32, vp, sz, vp],
+            "lp_op_kv4_append": [i32, vp, i64, vp, vp, i32, vp, vp, i32, vp, vp, i64, i32, i32, i32, vp],
+            "lp_op_kv4_read": [i32, vp, i64, vp, vp, i32, vp, vp, i64, i32, i32, vp],
+            "lp_op_kv4_decode_attention": [i32, vp, vp, vp, i64, vp, i32, i32, vp, vp, i32, i32, i32, i32, i32, vp, sz,
+                                           vp],
+            "lp_op_kv4_prefill_attention": [i32, vp, vp, vp, i64, vp, i32, i32, vp, vp, vp, i32, i32, i32, i32, i32,
+                                            i32, i32, vp, sz, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -147,6 +155,11 @@ def lib():
         for name in ("lp_op_prefix_decode_attention_ws_bytes", "lp_op_prefix_prefill_attention_ws_bytes"):
             getattr(L, name).argtypes = [i32] * 6
             getattr(L, name).restype = sz
+        for name in ("lp_op_kv4_decode_attention_ws_bytes", "lp_op_kv4_prefill_attention_ws_bytes"):
+            getattr(L, name).argtypes = [i32] * 5
+            getattr(L, name).restype = sz
+        L.lp_op_kv4_cache_bytes.argtypes = [i64, i32, i32]
+        L.lp_op_kv4_cache_bytes.restype = sz
         L.lp_op_packed_weight_bytes.argtypes = [i32, i32, i32]
         L.lp_op_packed_weight_bytes.restype = sz
         L.lp_engine_destroy.restype = None
@@ -614,15 +627,11 @@ def op_block_tables(seq_slot, cached, lengths, prefix_blocks, prefix_len, free_b
            taken, rslot, rpos, entry, max_rows))
 
 
-def op_qkv_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, kc, vc):
-    """Rotates q and k of the fp32 projection qkv [rows, (Hq + 2 Hkv) hd] (rows
-    may be strided), rounds q to q [rows, Hq, hd] and stores k and v in the
-    cache at row_entry (lp_op_qkv_append)."""
+def _append_args(qkv, rope_cos, rope_sin, row_pos, row_entry, q, hkv):
+    """What both appends hand over alike: the GPU, the arguments before q, heads and head_dim."""
     import torch
     dt, dev = _dt3(q), _gpu(q)
     rows, hq, hd = q.shape
-    n_blocks, hkv = _cache_shape(kc, vc, hd)
-    acts = _pointers(dev, q.dtype, "q kc vc", q, kc, vc)
     cos, sin = _pointers(dev, torch.float32, "rope_cos rope_sin", rope_cos, rope_sin)
     pos, = _pointers(dev, torch.int32, "row_pos", row_pos)
     entry, = _pointers(dev, torch.int64, "row_entry", row_entry)
@@ -632,9 +641,18 @@ def op_qkv_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, kc, vc):
     _need(row_pos.numel() == row_entry.numel() == rows, "row_pos and row_entry [rows]")
     _need(rope_cos.shape == rope_sin.shape and rope_cos.dim() == 2 and rope_cos.shape[1] == hd // 2,
           "rope_cos, rope_sin [positions, hd / 2]")
-    _call(lib().lp_op_qkv_append, dev,
-          (dt, qkv.data_ptr(), qkv.stride(0) if rows > 1 else width, cos, sin, rope_cos.shape[0], pos, entry, rows,
-           *acts, n_blocks, hq, hkv, hd))
+    return dev, (dt, qkv.data_ptr(), qkv.stride(0) if rows > 1 else width, cos, sin, rope_cos.shape[0], pos, entry,
+                 rows), (hq, hkv, hd)
+
+
+def op_qkv_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, kc, vc):
+    """Rotates q and k of the fp32 projection qkv [rows, (Hq + 2 Hkv) hd] (rows
+    may be strided), rounds q to q [rows, Hq, hd] and stores k and v in the
+    cache at row_entry (lp_op_qkv_append)."""
+    n_blocks, hkv = _cache_shape(kc, vc, q.shape[2])
+    dev, args, heads = _append_args(qkv, rope_cos, rope_sin, row_pos, row_entry, q, hkv)
+    acts = _pointers(dev, q.dtype, "q kc vc", q, kc, vc)
+    _call(lib().lp_op_qkv_append, dev, (*args, *acts, n_blocks, *heads))
 
 
 def prefix_decode_attention_ws_bytes(M, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx):
@@ -688,3 +706,91 @@ def op_prefix_prefill_attention(q, out, kc, vc, prefix_blocks, prefix_len, block
         "prefix_blocks block_table seq_start seq_slot seq_pos")
     _need(seq_start.numel() == n + 1 and seq_pos.numel() == n, "seq_start [n + 1], seq_slot and seq_pos [n]")
     _call(lib().lp_op_prefix_prefill_attention, dev, (*cache, *idx, n, rows, max_new, *heads, max_ctx, *space))
+
+
+# ------------------------------------------------------------------ a cache held in 4 bits
+
+def kv4_cache_bytes(n_blocks, n_kv_heads, head_dim):
+    return lib().lp_op_kv4_cache_bytes(n_blocks, n_kv_heads, head_dim)
+
+
+def _kv4_shape(cache, hd):
+    n_blocks, hkv, size = cache.shape
+    _need(hd in (64, 128) and size == 72 * hd, "cache: uint8 [n_blocks, Hkv, 72 hd], hd 64 or 128")
+    return n_blocks, hkv
+
+
+def op_kv4_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, cache):
+    """op_qkv_append into a cache held in 4 bits (lp_op_kv4_append): uint8
+    cache [n_blocks, Hkv, 72 hd]."""
+    import torch
+    n_blocks, hkv = _kv4_shape(cache, q.shape[2])
+    dev, args, heads = _append_args(qkv, rope_cos, rope_sin, row_pos, row_entry, q, hkv)
+    qp, = _pointers(dev, q.dtype, "q", q)
+    cp, = _pointers(dev, torch.uint8, "cache", cache)
+    _call(lib().lp_op_kv4_append, dev, (*args, qp, cp, n_blocks, *heads))
+
+
+def op_kv4_read(cache, src_entry, dst_entry, kc, vc):
+    """Entries src_entry of a 4-bit cache to the entries dst_entry of an
+    ordinary one (lp_op_kv4_read): uint8 cache [n_blocks, Hkv, 72 hd]; int64
+    src_entry and dst_entry of one length; kc [n, Hkv, 64, hd], vc [n, Hkv, hd, 64]."""
+    import torch
+    dt, dev, hd = _dt3(kc), _gpu(kc), kc.shape[3]
+    n_dst, hkv = _cache_shape(kc, vc, hd)
+    n_blocks, held = _kv4_shape(cache, hd)
+    _need(held == hkv, "cache, kc and vc: one number of heads")
+    k, v = _pointers(dev, kc.dtype, "kc vc", kc, vc)
+    cp, = _pointers(dev, torch.uint8, "cache", cache)
+    src, dst = _pointers(dev, torch.int64, "src_entry dst_entry", src_entry, dst_entry)
+    _need(src_entry.numel() == dst_entry.numel(), "src_entry and dst_entry: one length")
+    _call(lib().lp_op_kv4_read, dev, (dt, cp, n_blocks, src, dst, src_entry.numel(), k, v, n_dst, hkv, hd))
+
+
+def kv4_decode_attention_ws_bytes(M, n_heads, n_kv_heads, head_dim, max_ctx):
+    return lib().lp_op_kv4_decode_attention_ws_bytes(M, n_heads, n_kv_heads, head_dim, max_ctx)
+
+
+def kv4_prefill_attention_ws_bytes(rows, n_heads, n_kv_heads, head_dim, max_ctx):
+    return lib().lp_op_kv4_prefill_attention_ws_bytes(rows, n_heads, n_kv_heads, head_dim, max_ctx)
+
+
+def _kv4_args(q, out, cache, block_table, ws, index, names):
+    """What both phases hand over alike: the GPU, dtype and cache arguments, the
+    index tensors' pointers, heads and head_dim, the workspace's pointer and bytes."""
+    import torch
+    dt, dev = _dt3(q), _gpu(q)
+    hq, hd = q.shape[1:]
+    n_blocks, hkv = _kv4_shape(cache, hd)
+    acts = _pointers(dev, q.dtype, "q out", q, out)
+    cp, = _pointers(dev, torch.uint8, "cache", cache)
+    table, *idx = _pointers(dev, torch.int32, names, block_table, *index)
+    n_slots, max_blocks = block_table.shape
+    _need(out.shape == q.shape, "out: shape of q")
+    _need(ws is None or (ws.get_device() == dev and ws.is_contiguous()), "ws: contiguous, on the GPU of q")
+    space = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+    return dev, (dt, *acts, cp, n_blocks, table, n_slots, max_blocks), idx, (hq, hkv, hd), space
+
+
+def op_kv4_decode_attention(q, out, cache, block_table, row_slot, row_pos, max_ctx, ws):
+    """One token a row over a cache held in 4 bits (lp_op_kv4_decode_attention):
+    q, out [M, Hq, hd], uint8 cache [n_blocks, Hkv, 72 hd]; int32 block_table
+    [n_slots, max_blocks], row_slot and row_pos [M]; ws of
+    kv4_decode_attention_ws_bytes."""
+    M = q.shape[0]
+    dev, cache_args, idx, heads, space = _kv4_args(q, out, cache, block_table, ws, (row_slot, row_pos),
+                                                   "block_table row_slot row_pos")
+    _need(row_slot.numel() == row_pos.numel() == M, "row_slot, row_pos [M]")
+    _call(lib().lp_op_kv4_decode_attention, dev, (*cache_args, *idx, M, *heads, max_ctx, *space))
+
+
+def op_kv4_prefill_attention(q, out, cache, block_table, seq_start, seq_slot, seq_pos, max_new, max_ctx, ws):
+    """Packed new tokens, causal, over a cache held in 4 bits
+    (lp_op_kv4_prefill_attention): q, out [rows, Hq, hd]; int32 seq_start [n +
+    1], seq_slot and seq_pos [n] (position of each sequence's first row); the
+    others as for decode, ws of kv4_prefill_attention_ws_bytes."""
+    rows, n = q.shape[0], seq_slot.numel()
+    dev, cache_args, idx, heads, space = _kv4_args(q, out, cache, block_table, ws, (seq_start, seq_slot, seq_pos),
+                                                   "block_table seq_start seq_slot seq_pos")
+    _need(seq_start.numel() == n + 1 and seq_pos.numel() == n, "seq_start [n + 1], seq_slot and seq_pos [n]")
+    _call(lib().lp_op_kv4_prefill_attention, dev, (*cache_args, *idx, n, rows, max_new, *heads, max_ctx, *space))
