@@ -7,6 +7,7 @@
 
 #include <algorithm>
 
+#include "device.hpp"
 #include "kernels.hpp"
 
 namespace lp {
@@ -42,6 +43,50 @@ __device__ __forceinline__ int row_ctx(const PrefixBatch &b, int j, int i) {
   if (slot < 0 || slot >= b.n_slots) return 0;
   const int64_t ctx = (int64_t)p0 + i + 1;
   return p0 < 0 ? 0 : (int)min(ctx, (int64_t)b.max_ctx);
+}
+
+// Rows are packed: a sequence's tokens, each with the G query heads of a KV head.
+// The arguments A of a kernel hold the batch b, G, and divisors by G (by_g) and by
+// the tiles of a decode row's G heads (by_per).
+
+struct PrefixRow {
+  int token, head, t;  // t: the token's place in its sequence, or in the batch
+};
+
+// Row l of the packed rows from r0 (uniform) on: of all tokens, or of a sequence
+// whose first token is `start`.
+template <typename A>
+__device__ __forceinline__ PrefixRow packed_row(const A &a, int start, int r0, int l, int g) {
+  const int t0 = div_by(r0, a.by_g), x = r0 - t0 * a.G + l, dt = div_by(x, a.by_g);
+  return PrefixRow{start + t0 + dt, g * a.G + x - dt * a.G, t0 + dt};
+}
+
+// Own tile u of RT packed rows: sequence by sequence, each with as many tiles as
+// its rows need.  Each wave finds it on its own: an inclusive sum over 64
+// sequences at a time, the first whose sum exceeds u.  False past the last.
+template <int RT, typename A>
+__device__ __forceinline__ bool own_tile(const A &a, int u, int &j, int &r0) {
+  const int lane = threadIdx.x & 63;
+  if (!a.b.seq_start) {  // one row a sequence
+    j = div_by(u, a.by_per);
+    r0 = (u - j * (int)a.by_per.d) * RT;
+    return j < a.b.n_seq;
+  }
+  for (int base = 0; base < a.b.n_seq; base += 64) {
+    int start, n = 0;
+    if (base + lane < a.b.n_seq) seq_rows(a.b, base + lane, start, n);
+    const int tiles = (int)(((int64_t)min(n, a.b.max_new) * a.G + RT - 1) / RT);
+    const int incl = (int)wave_scan((uint64_t)tiles);
+    const int total = __builtin_amdgcn_readlane(incl, 63);
+    if (u < total) {
+      const int k = __popcll(__ballot(incl <= u));  // sequences wholly before the tile
+      j = base + k;
+      r0 = (__shfl(incl, k, 64) - 1 - u) * RT;  // from the last, whose rows see most
+      return true;
+    }
+    u -= total;
+  }
+  return false;
 }
 
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }

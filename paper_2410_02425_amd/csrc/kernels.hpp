@@ -171,6 +171,14 @@ size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_he
 template <typename T>
 bool launch_prefix_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s);
 
+// Joins the parts of each (row, head) of a batch without a prefix, of part_blocks
+// blocks each: o [rows][n_heads][parts][hd], unscaled largest score and sum
+// [rows][n_heads][parts][2].
+template <typename T>
+void launch_attention_join(T *out, const PrefixBatch &b, int parts, int part_blocks, float *po, float *pml,
+                           hipStream_t s);
+int64_t attention_join_wgs(const PrefixBatch &b, int parts);
+
 // Block tables, row offsets and cache entries of a step (see lp_op_block_tables).
 struct TableStep {
   const int32_t *seq_slot, *cached, *lengths;

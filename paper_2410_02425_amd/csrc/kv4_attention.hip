@@ -1,88 +1,420 @@
 // Attention over the cache held in 4 bits.
+//
+// Codes go to the matrix cores without their scales, exact in 16 bits:
+//   score(t) = sum over groups j of sk[t][j] (q_j . c_tj): one MFMA over 32 dims is
+//   a group's product, the scale multiplies its fp32 result;
+//   out[d] = sum over t of (p_t sv[t][j]) c[t][d], d in group j: the scale goes into
+//   the weight before that is rounded for the MFMA.
+// So no value is dequantised, codes are finite whatever a stale place holds, and a
+// row's mask clears its own weights alone.
+// fp32: q and the weights as three bf16 parts each (8 bits and 8 and 8), products
+// with codes exact, all sums fp32.
 #include <algorithm>
+#include <type_traits>
 
 #include "batch.hpp"
 #include "kv4.hpp"
 
 namespace lp {
 
-// A wave per (row, query head): its lanes are the keys of a block for the scores,
-// the dims for the values.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) void kv4_attention_kernel(const T *__restrict__ q, T *__restrict__ out,
-                                                            PrefixBatch b) {
+struct Kv4Args {
+  PrefixBatch b;
+  int G;                // query heads of a KV head
+  int units;            // row tiles
+  int splits, sblk;     // splits of a tile's blocks, blocks of a split
+  Divisor by_g, by_hkv, by_units, by_per;
+  float *po, *pml;      // partial o [rows][n_heads][splits][hd], (m, l) [rows][n_heads][splits][2]
+};
+// A part's m is the largest score before the scale 1/sqrt(hd), its weights are
+// 2^((score - m) c2).
+template <int HD>
+constexpr float KV4_C2 = (HD == 64 ? 0.125f : 0.08838834764831845f) * 1.44269504088896341f;
+
+typedef unsigned int u32x2_tt __attribute__((ext_vector_type(2)));
+typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+
+// Eight codes (a word, the low half first) as an MFMA operand.
+template <typename T>
+__device__ __forceinline__ typename Mfma<T>::v8 codes8(uint32_t w) {
+  const u32x4_tt v = {kv4_pair16<T, 0>(w), kv4_pair16<T, 1>(w), kv4_pair16<T, 2>(w), kv4_pair16<T, 3>(w)};
+  return __builtin_bit_cast(typename Mfma<T>::v8, v);
+}
+
+// Maximum / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float quads_max(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return half_swap_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float quads_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return half_swap_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// Up to 16 packed rows of a KV head over a range of blocks, on 16x16x32 MFMAs; the
+// workgroup's waves take blocks in turn, each with LDS of its own for one block:
+// its K half is copied there while the softmax and the values of the block before
+// are worked on, its V half while the scores are.  S^T = K Q^T: a lane holds one
+// row's scores of 8 consecutive keys of each 32, which is the operand of O^T +=
+// V^T P^T as it lies; V's pairs of keys are made from its words of one key by
+// exchanging halves of bytes.
+template <typename T, int HD, int NW>
+__global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef Kv4<HD> F;
-  constexpr int J = F::J, DPL = HD / 64;
+  constexpr bool WIDE = sizeof(T) == 4;
+  typedef std::conditional_t<WIDE, bf16_t, T> QT;      // operands of the scores
+  typedef std::conditional_t<WIDE, bf16_t, f16_t> PT;  // of the values: fp16 has the finer weights
+  typedef typename Mfma<QT>::v8 qv8;
+  typedef typename Mfma<PT>::v8 pv8;
+  constexpr int J = F::J, NP = WIDE ? 3 : 1;
+  constexpr float c2 = KV4_C2<HD>;
+  constexpr int PART = 36 * HD, FULL = 32 * HD / 1024, TAIL = 4 * HD / 16;  // a half's bytes, copies, lanes of the last
+  constexpr int ND = FULL + 1;
+  __shared__ __attribute__((aligned(1024))) char lds[NW * F::BYTES];
+  __shared__ float wm[NW * 16], wl[NW * 16];
+  const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int64_t rh = (int64_t)blockIdx.x * 4 + wave;
-  const int t = (int)(rh / b.n_heads), h = (int)(rh - (int64_t)t * b.n_heads);
-  if (t >= b.rows) return;
-  int seq = -1, i = 0;
-  if (!b.seq_start) {
-    seq = t;
-  } else {
-    for (int j = 0; j < b.n_seq; ++j) {
-      int start, n;
-      seq_rows(b, j, start, n);
-      if (t >= start && t < start + n) seq = j, i = t - start;
-    }
-    if (seq < 0) return;
+  const int r16 = lane & 15, quad = lane >> 4;
+  const int i0 = div_by(blockIdx.x, a.by_hkv), g = blockIdx.x - i0 * Hkv;
+  const int part = div_by(i0, a.by_units);  // all rows' first splits, then their second ones
+  int j_, r0;
+  if (!own_tile<16>(a, i0 - part * a.units, j_, r0)) return;
+  const int seq = __builtin_amdgcn_readfirstlane(j_);
+  r0 = __builtin_amdgcn_readfirstlane(r0);
+  int start, n;
+  seq_rows(a.b, seq, start, n);
+  const int slot = a.b.seq_slot[seq];
+  const int top = row_ctx(a.b, seq, min(div_by(r0 + 15, a.by_g), n - 1));  // the last row sees most
+  const int e0 = part * a.sblk, e1 = min(e0 + a.sblk, (top + KV_BLOCK - 1) / KV_BLOCK);
+  const bool direct = a.splits == 1;
+  if (!direct && !a.b.seq_start && e0 >= e1) return;  // decode's join reads no such part
+  const PrefixRow w = packed_row(a, start, r0, r16, g);
+  const bool live = w.t < n && w.t < a.b.max_new;
+  const int ctx = live ? row_ctx(a.b, seq, w.t) : 0;
+  // keys that every row of the tile sees; rows that see nothing get zeros at the end
+  const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
+  // lane i: block id of entry e0 + i (an item has at most 64), -1 for none
+  int id = -1;
+  if (e0 + lane < e1 && e0 + lane < a.b.kv.max_blocks) {
+    id = a.b.kv.block_table[(int64_t)slot * a.b.kv.max_blocks + e0 + lane];
+    if (id >= a.b.kv.n_blocks) id = -1;
   }
-  const int ctx = i < b.max_new ? row_ctx(b, seq, i) : 0;
-  const int slot = b.seq_slot[seq];
-  const uint8_t *cache = (const uint8_t *)b.kv.k;
-  const float scale = rsqrtf((float)HD);
-  const T *qr = q + rh * HD;
-  float m = -INFINITY, sum = 0.f, o[DPL];
+  constexpr uint64_t every = NW == 1 ? ~0ull : ~0ull / ((1ull << NW) - 1);  // every NW-th
+  uint64_t left = __ballot(id >= 0) & (every << wave);
+
+  char *ks = lds + wave * F::BYTES, *vs = ks + PART;
+  const uint32_t kl = lds_addr(ks), vl = kl + PART;
+  // Copies of 1 KB; 16-byte pieces of K rows are XOR-swizzled by the row against
+  // bank conflicts.  Pieces past the last key repeat the last one before it.
+  constexpr int KP = HD / 32;  // 16-byte pieces of a K row
+  auto swz = [](int key) __attribute__((always_inline)) { return (key >> 3) & (KP - 1); };
+  auto copy = [&](int i, bool is_k) __attribute__((always_inline)) {
+    const int keys = min(KV_BLOCK, top - (e0 + i) * KV_BLOCK);
+    const char *src = (const char *)a.b.kv.k +
+                      ((int64_t)__builtin_amdgcn_readlane(id, i) * Hkv + g) * F::BYTES + (is_k ? 0 : PART);
+    const uint32_t dst = is_k ? kl : vl;
+    const uint32_t last = (is_k ? keys * (HD / 2) : (keys + 3) / 4 * 2 * HD) - 16;
 #pragma unroll
-  for (int d = 0; d < DPL; ++d) o[d] = 0.f;
-  for (int e = 0; e * KV_BLOCK < ctx; ++e) {
-    const int id = e < b.kv.max_blocks ? b.kv.block_table[(int64_t)slot * b.kv.max_blocks + e] : -1;
-    if (id < 0 || id >= b.kv.n_blocks) continue;
-    const uint8_t *blk = cache + ((int64_t)id * b.kv.n_kv_heads + h / (b.n_heads / b.kv.n_kv_heads)) * F::BYTES;
-    const int keys = min(ctx - e * KV_BLOCK, KV_BLOCK);
-    float s = 0.f;
-    for (int w = 0; w < HD / 8; ++w) {
-      const int o8 = w / J, j = w % J;
-      const uint32_t c = *(const uint32_t *)(blk + F::k_row(lane) + 4 * w);
-      const f32x2_t x[4] = {kv4_pair32<0>(c), kv4_pair32<1>(c), kv4_pair32<2>(c), kv4_pair32<3>(c)};
-      float part = 0.f;
-      for (int d = 0; d < 8; ++d) part = fmaf(Act<T>::ld(qr[32 * j + 8 * o8 + d]), x[d / 2][d % 2], part);
-      s = fmaf(part, (float)*(const _Float16 *)(blk + F::k_scale(lane, j)), s);
+    for (int c = 0; c < FULL; ++c) {
+      uint32_t off = c * 1024 + lane * 16;
+      if (is_k) off ^= swz(off / (HD / 2)) * 16;
+      dma16s(src, min(off, last), dst + c * 1024);
     }
-    s = lane < keys ? s * scale : -INFINITY;
-    const float nm = fmaxf(m, wave_max(s)), m0 = nm == -INFINITY ? 0.f : nm;
-    const float corr = m == nm ? 1.f : expf(m - nm), p = expf(s - m0);
-    m = nm;
-    sum = sum * corr + wave_sum(p);
+    const uint32_t tail = __builtin_amdgcn_readfirstlane(dst + 32 * HD);  // kept scalar where lanes part
+    if (lane < TAIL) dma16s(src, 32 * HD + lane * 16, tail);
+  };
+
+  qv8 qa[NP][J];  // Q^T as the B operand: this lane's row, dims 32 j + 8 quad ..
+  {
+    const T *qr = q + ((int64_t)(live ? w.token : start) * Hq + w.head) * HD + quad * 8;
 #pragma unroll
-    for (int d = 0; d < DPL; ++d) o[d] *= corr;
-    for (int k = 0; k < keys; ++k) {
-      const float pk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(p), k));
+    for (int j = 0; j < J; ++j) {
+      if constexpr (!WIDE) {
+        qa[0][j] = load8<T>(qr + 32 * j);
+      } else {
+        const float4 x = *(const float4 *)(qr + 32 * j), y = *(const float4 *)(qr + 32 * j + 4);
+        float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-      for (int d = 0; d < DPL; ++d) {
-        const int dim = d * 64 + lane, j = dim / 32, r = dim % 32 / 2, byte = J * r + j;
-        const uint32_t c = *(const uint8_t *)(blk + F::v_word(k, byte / 4) + byte % 4);
-        const float x = kv4_pair32<0>(c >> (dim % 2 * 4))[0];
-        o[d] = fmaf(pk, x * (float)*(const _Float16 *)(blk + F::v_scale(k, j)), o[d]);
+        for (int p = 0; p < 3; ++p)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const __bf16 part_ = (__bf16)v[e];
+            qa[p][j][e] = part_;
+            v[e] -= (float)part_;
+          }
       }
     }
   }
+  // o[2 j + x][i]: dim 32 j + 8 quad + 2 i + x of row r16, times 2^-ex
+  floatx4_t o[2 * J];
 #pragma unroll
-  for (int d = 0; d < DPL; ++d) out[rh * HD + d * 64 + lane] = round_to<T>(sum == 0.f ? 0.f : o[d] / sum);
+  for (int x = 0; x < 2 * J; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  float mx = -INFINITY, sum = 0.f;  // of row r16; sum: this lane's keys alone
+  int ex = -25;                     // 16-bit types: exponent of V's largest scale so far, below all of them at first
+  int i = left ? __builtin_ctzll(left) : 0;
+  if (left) {
+    copy(i, true);
+    copy(i, false);
+  }
+  while (left) {
+    const int base = (e0 + i) * KV_BLOCK;
+    left &= left - 1;
+    const bool more = left != 0;
+    const int next = more ? __builtin_ctzll(left) : 0;
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");  // K is there, V may not be
+    float s[4][4];  // key 16 t + 8 (lane's quad) .. as p below: 32 (t / 2) + 8 quad + 4 (t % 2) + e
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int key = 32 * (t / 2) + 8 * (r16 >> 2) + 4 * (t & 1) + (r16 & 3);
+      uint32_t piece[J];
+      if constexpr (J == 4) {
+        const u32x4_tt v = *(const u32x4_tt *)(ks + key * (HD / 2) + ((quad ^ swz(key)) * 16));
+#pragma unroll
+        for (int j = 0; j < J; ++j) piece[j] = v[j];
+      } else {
+        const u32x2_tt v = *(const u32x2_tt *)(ks + key * (HD / 2) + (((quad >> 1) ^ swz(key)) * 16) + (quad & 1) * 8);
+#pragma unroll
+        for (int j = 0; j < J; ++j) piece[j] = v[j];
+      }
+      _Float16 sk[4 * J];  // [key][group]
+#pragma unroll
+      for (int x = 0; x < J / 2; ++x)
+        *(u32x4_tt *)(sk + 8 * x) =
+            *(const u32x4_tt *)(ks + F::k_scale(32 * (t / 2) + 8 * quad + 4 * (t & 1), 0) + 16 * x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const qv8 c = codes8<QT>(piece[j]);
+        floatx4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < NP; ++p) acc = Mfma<QT>::m16(c, qa[p][j], acc);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[t][e] = fmaf((float)sk[e * J + j], acc[e], s[t][e]);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
+    if (more) copy(next, true);
+    const int end = min(KV_BLOCK, ctx - base);  // the row's keys: those below
+    const bool partly = base + KV_BLOCK > ctx_lo;
+    if (partly) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (32 * (t / 2) + 8 * quad + 4 * (t & 1) + e >= end) s[t][e] = -INFINITY;
+    }
+    float m = s[0][0];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = fmaxf(m, s[t][e]);
+    m = fmaxf(mx, quads_max(m));
+    if (__any(m > mx)) {
+      const float corr = m == mx ? 1.f : __builtin_amdgcn_exp2f((mx - m) * c2);
+      mx = m;
+      sum *= corr;
+#pragma unroll
+      for (int x = 0; x < 2 * J; ++x)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[x][e] *= corr;
+    }
+    const float m0 = mx == -INFINITY ? 0.f : mx;  // a row that has seen no key yet
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[t][e] = __builtin_amdgcn_exp2f((s[t][e] - m0) * c2);
+        sum += s[t][e];
+      }
+    if (more)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");  // V is there
+    else
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (!WIDE) {
+      // weights times scales stay within fp16's range for values of any size:
+      // they are taken by the exponent of the largest scale (the tile's keys alone)
+      float big = 0.f;
+      const int keys = top - base;
+#pragma unroll
+      for (int x = 0; x < J; ++x) {
+        const float v = (float)*(const _Float16 *)(vs + 32 * HD + (x * 64 + lane) * 2);
+        if (lane < keys) big = fmaxf(big, v);
+      }
+      big = wave_max(big);
+      const int e = __builtin_amdgcn_readfirstlane(big > 0.f ? __builtin_amdgcn_frexp_expf(fminf(big, 65504.f)) : -25);
+      if (e > ex) {
+        const float f = __builtin_amdgcn_ldexpf(1.f, max(ex - e, -60));
+        ex = e;
+#pragma unroll
+        for (int x = 0; x < 2 * J; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) o[x][y] *= f;
+      }
+      const float f = __builtin_amdgcn_ldexpf(1.f, -ex);
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) s[t][y] *= f;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // words of keys 32 h + 8 quad .. + 7, then pairs of keys: lo the even dims', hi the odd ones'
+      uint32_t x[8], lo[4], hi[4];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int p = 32 * h + 8 * quad + 4 * y;
+        const u32x4_tt v = *(const u32x4_tt *)(vs - PART + F::v_word(p, J == 4 ? r16 : r16 >> 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * y + e] = J == 4 ? v[e] : v[e] >> ((r16 & 1) * 16);
+      }
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        lo[y] = (x[2 * y] & 0x0F0F0F0Fu) | ((x[2 * y + 1] << 4) & 0xF0F0F0F0u);
+        hi[y] = ((x[2 * y] >> 4) & 0x0F0F0F0Fu) | (x[2 * y + 1] & 0xF0F0F0F0u);
+      }
+      auto group = [&](auto j_c) __attribute__((always_inline)) {
+        constexpr int j = decltype(j_c)::value;
+        u32x4_tt raw = *(const u32x4_tt *)(vs - PART + F::v_scale(32 * h + 8 * quad, j));
+        if (partly) {
+          // scales at places that the row does not see may be anything, and 0 * NaN is not 0
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int key = 32 * h + 8 * quad + 2 * y;
+            raw[y] &= (key < end ? 0xFFFFu : 0u) | (key + 1 < end ? 0xFFFF0000u : 0u);
+          }
+        }
+        _Float16 sv[8];
+        *(u32x4_tt *)sv = raw;
+        pv8 p[NP];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const float f = s[2 * h + y / 4][y % 4] * (float)sv[y];
+          if constexpr (!WIDE) {
+            p[0][y] = (_Float16)f;
+          } else {
+            float v = f;
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+              const __bf16 part_ = (__bf16)v;
+              p[k][y] = part_;
+              v -= (float)part_;
+            }
+          }
+        }
+        const u32x4_tt c0 = {kv4_pair16<PT, j>(lo[0]), kv4_pair16<PT, j>(lo[1]), kv4_pair16<PT, j>(lo[2]),
+                             kv4_pair16<PT, j>(lo[3])};
+        const u32x4_tt c1 = {kv4_pair16<PT, j>(hi[0]), kv4_pair16<PT, j>(hi[1]), kv4_pair16<PT, j>(hi[2]),
+                             kv4_pair16<PT, j>(hi[3])};
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+          o[2 * j] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c0), p[k], o[2 * j]);
+          o[2 * j + 1] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c1), p[k], o[2 * j + 1]);
+        }
+      };
+      group(std::integral_constant<int, 0>());
+      group(std::integral_constant<int, 1>());
+      if constexpr (J == 4) {
+        group(std::integral_constant<int, 2>());
+        group(std::integral_constant<int, 3>());
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
+    if (more) copy(next, false);
+    i = next;
+  }
+  const float back = WIDE ? 1.f : __builtin_amdgcn_ldexpf(1.f, ex);
+  sum = quads_sum(sum);
+  const int nrows = a.b.seq_start ? 16 : min(16, a.G - r0);
+  // o goes where K and V were, row r16's dims side by side
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  if (quad == 0) wm[wave * 16 + r16] = mx, wl[wave * 16 + r16] = sum;
+  if (r16 < nrows) {
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float4 v = make_float4(o[2 * j][2 * y] * back, o[2 * j + 1][2 * y] * back, o[2 * j][2 * y + 1] * back,
+                                     o[2 * j + 1][2 * y + 1] * back);
+        *(float4 *)(ks + (r16 * HD + 32 * j + 8 * quad + 4 * y) * 4) = v;
+      }
+  }
+  __syncthreads();
+  // a wave a row: its lanes over the dims
+  for (int r = wave; r < nrows; r += NW) {
+    if (!__builtin_amdgcn_readlane((int)live, r)) continue;
+    const int token = __builtin_amdgcn_readlane(w.token, r), h = __builtin_amdgcn_readlane(w.head, r);
+    float M = -INFINITY, L = 0.f, v[HD / 64];
+    for (int k = 0; k < NW; ++k) M = fmaxf(M, wm[k * 16 + r]);
+#pragma unroll
+    for (int d = 0; d < HD / 64; ++d) v[d] = 0.f;
+    for (int k = 0; k < NW; ++k) {
+      const float m = wm[k * 16 + r], f = m == M ? 1.f : __builtin_amdgcn_exp2f((m - M) * c2);
+      L += f * wl[k * 16 + r];
+#pragma unroll
+      for (int d = 0; d < HD / 64; ++d) v[d] += f * ((const float *)(lds + k * F::BYTES))[r * HD + d * 64 + lane];
+    }
+    const bool none = __builtin_amdgcn_readlane(ctx, r) == 0;
+    const int64_t row = (int64_t)token * Hq + h, rec = row * a.splits + part;
+#pragma unroll
+    for (int d = 0; d < HD / 64; ++d) {
+      if (none) v[d] = 0.f;
+      if (direct)
+        out[row * HD + d * 64 + lane] = round_to<T>(L == 0.f ? 0.f : v[d] / L);
+      else if (e0 < e1)
+        a.po[rec * HD + d * 64 + lane] = v[d];
+    }
+    if (!direct && lane == 0) *(float2 *)(a.pml + rec * 2) = none ? make_float2(-INFINITY, 0.f) : make_float2(M, L);
+  }
 }
 
-size_t kv4_attention_ws_bytes(bool, int, int, int, int, int) { return 0; }
+// ------------------------------------------------------------------ plan
+
+// Blocks of a split.
+static int kv4_split(int64_t pairs, int blocks) {
+  const int want = (int)std::max<int64_t>(1, 1024 / std::max<int64_t>(1, std::min<int64_t>(pairs, 1024)));
+  return std::min(64, std::max(ceil_div(blocks, want), std::min(blocks, 8)));
+}
+
+static void kv4_plan(Kv4Args &a, bool decode, int rows, int n_heads, int n_kv_heads, int max_ctx, int n_seq,
+                     int max_new) {
+  a.G = n_heads / n_kv_heads;
+  const int live = std::min(n_seq, rows);
+  a.units = decode ? rows * ceil_div(a.G, 16)
+                   : (int)std::min((int64_t)live * ceil_div((int64_t)std::min(max_new, rows) * a.G, 16),
+                                   (int64_t)rows * a.G / 16 + live);
+  const int blocks = ceil_div(max_ctx, KV_BLOCK);
+  a.sblk = kv4_split((int64_t)a.units * n_kv_heads, blocks);
+  a.splits = ceil_div(blocks, a.sblk);
+}
+
+size_t kv4_attention_ws_bytes(bool, int rows, int n_heads, int, int head_dim, int max_ctx) {
+  const int64_t blocks = ceil_div(max_ctx, KV_BLOCK);
+  return (size_t)rows * n_heads * ceil_div(blocks, 8) * (head_dim + 2) * sizeof(float);
+}
+
+template <typename T, int HD>
+static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s) {
+  Kv4Args a{};
+  a.b = b;
+  const bool decode = !b.seq_start;
+  const int Hkv = b.kv.n_kv_heads;
+  kv4_plan(a, decode, b.rows, b.n_heads, Hkv, b.max_ctx, b.n_seq, b.max_new);
+  a.po = ws;
+  a.pml = ws + (size_t)b.rows * b.n_heads * a.splits * HD;
+  a.by_g = divisor(a.G);
+  a.by_hkv = divisor(Hkv);
+  a.by_units = divisor(a.units);
+  a.by_per = divisor(ceil_div(a.G, 16));
+  const int64_t wgs = (int64_t)a.units * a.splits * Hkv;
+  if (std::max(wgs, attention_join_wgs(b, a.splits)) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads
+  kv4_rows_kernel<T, HD, 4><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
+  if (a.splits > 1) launch_attention_join<T>(out, b, a.splits, a.sblk, a.po, a.pml, s);
+  return true;
+}
 
 template <typename T>
-bool launch_kv4_attention(const T *q, T *out, const PrefixBatch &b, float *, hipStream_t s) {
-  const int64_t wgs = ((int64_t)b.rows * b.n_heads + 3) / 4;
-  if (wgs >= 1 << 23) return false;  // a launch has fewer than 2^32 threads
-  if (b.kv.head_dim == 128)
-    kv4_attention_kernel<T, 128><<<(unsigned)wgs, 256, 0, s>>>(q, out, b);
-  else
-    kv4_attention_kernel<T, 64><<<(unsigned)wgs, 256, 0, s>>>(q, out, b);
-  return true;
+bool launch_kv4_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s) {
+  return b.kv.head_dim == 128 ? launch_kv4_hd<T, 128>(q, out, b, ws, s) : launch_kv4_hd<T, 64>(q, out, b, ws, s);
 }
 
 #define INST(T) template bool launch_kv4_attention<T>(const T *, T *, const PrefixBatch &, float *, hipStream_t);

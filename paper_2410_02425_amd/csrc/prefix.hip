@@ -40,17 +40,6 @@ struct PrefixArgs {
 template <int HD>
 constexpr float SCORE_C2 = (HD == 64 ? 0.125f : 0.08838834764831845f) * 1.44269504088896341f;
 
-struct PrefixRow {
-  int token, head, t;  // t: the token's place in its sequence, or in the batch
-};
-
-// Row l of the packed rows from r0 (uniform) on: of all tokens, or of a sequence
-// whose first token is `start`.
-__device__ __forceinline__ PrefixRow packed_row(const PrefixArgs &a, int start, int r0, int l, int g) {
-  const int t0 = div_by(r0, a.by_g), x = r0 - t0 * a.G + l, dt = div_by(x, a.by_g);
-  return PrefixRow{start + t0 + dt, g * a.G + x - dt * a.G, t0 + dt};
-}
-
 // Keys that a packed row sees, -1 if the row does not exist: token t of sequence
 // j (which has n rows), or with j < 0 token t of the batch.
 __device__ __forceinline__ int packed_ctx(const PrefixArgs &a, int j, int t, int n) {
@@ -74,34 +63,6 @@ __device__ __forceinline__ int packed_ctx(const PrefixArgs &a, int j, int t, int
   seq_rows(a.b, at, start, n);
   t -= start;
   return t >= 0 && t < n && t < a.b.max_new ? row_ctx(a.b, at, t) : -1;
-}
-
-// Own tile u of RT packed rows: sequence by sequence, each with as many tiles as
-// its rows need.  Each wave finds it on its own: an inclusive sum over 64
-// sequences at a time, the first whose sum exceeds u.  False past the last.
-template <int RT>
-__device__ __forceinline__ bool own_tile(const PrefixArgs &a, int u, int &j, int &r0) {
-  const int lane = threadIdx.x & 63;
-  if (!a.b.seq_start) {  // one row a sequence
-    j = div_by(u, a.by_per);
-    r0 = (u - j * (int)a.by_per.d) * RT;
-    return j < a.b.n_seq;
-  }
-  for (int base = 0; base < a.b.n_seq; base += 64) {
-    int start, n = 0;
-    if (base + lane < a.b.n_seq) seq_rows(a.b, base + lane, start, n);
-    const int tiles = (int)(((int64_t)min(n, a.b.max_new) * a.G + RT - 1) / RT);
-    const int incl = (int)wave_scan((uint64_t)tiles);
-    const int total = __builtin_amdgcn_readlane(incl, 63);
-    if (u < total) {
-      const int k = __popcll(__ballot(incl <= u));  // sequences wholly before the tile
-      j = base + k;
-      r0 = (__shfl(incl, k, 64) - 1 - u) * RT;  // from the last, whose rows see most
-      return true;
-    }
-    u -= total;
-  }
-  return false;
 }
 
 // An entry's block id, -1 for none.
@@ -1073,6 +1034,20 @@ size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_he
   return (size_t)(shared + of_rows) * n_heads * (head_dim + 2) * sizeof(float);
 }
 
+static int64_t join_wgs(const PrefixBatch &b, int parts) {
+  return parts <= 16 ? ((int64_t)b.rows * b.n_heads + 3) / 4 : (int64_t)b.rows * b.n_heads;
+}
+template <typename T, int HD>
+static void launch_join(T *out, const PrefixArgs &a, hipStream_t s) {
+  const unsigned wgs = (unsigned)join_wgs(a.b, a.parts);
+  if (a.parts <= 4)
+    prefix_join_kernel<T, HD, 4, 1><<<wgs, 256, 0, s>>>(out, a);
+  else if (a.parts <= 16)
+    prefix_join_kernel<T, HD, 16, 1><<<wgs, 256, 0, s>>>(out, a);
+  else
+    prefix_join_kernel<T, HD, 16, 4><<<wgs, 256, 0, s>>>(out, a);
+}
+
 template <typename T, int HD>
 static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s) {
   PrefixArgs a{};
@@ -1101,8 +1076,7 @@ static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   a.by_shared = divisor(a.shared_rows);
   a.by_per = divisor(ceil_div(a.G, rto));
   const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.units * a.osplits) * Hkv;
-  const int64_t joins = a.parts <= 16 ? ((int64_t)b.rows * b.n_heads + 3) / 4 : (int64_t)b.rows * b.n_heads;
-  if (std::max(items, joins) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads, 512 to a workgroup
+  if (std::max(items, join_wgs(b, a.parts)) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads, 512 to a workgroup
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
   if (a.whole) {
     prefix_row_kernel<T, HD><<<grid((int64_t)a.otiles * Hkv), WHOLE_WAVES<T, HD> * 64, 0, s>>>(q, out, a);
@@ -1114,14 +1088,7 @@ static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   } else {
     prefix_rows_kernel<T, HD><<<grid(items), 256, 0, s>>>(q, out, a);
   }
-  if (!a.direct && !a.whole) {
-    if (a.parts <= 4)
-      prefix_join_kernel<T, HD, 4, 1><<<grid(joins), 256, 0, s>>>(out, a);
-    else if (a.parts <= 16)
-      prefix_join_kernel<T, HD, 16, 1><<<grid(joins), 256, 0, s>>>(out, a);
-    else
-      prefix_join_kernel<T, HD, 16, 4><<<grid(joins), 256, 0, s>>>(out, a);
-  }
+  if (!a.direct && !a.whole) launch_join<T, HD>(out, a, s);
   return true;
 }
 
@@ -1130,7 +1097,23 @@ bool launch_prefix_attention(const T *q, T *out, const PrefixBatch &b, float *ws
   return b.kv.head_dim == 128 ? launch_prefix_hd<T, 128>(q, out, b, ws, s) : launch_prefix_hd<T, 64>(q, out, b, ws, s);
 }
 
-#define INST(T) template bool launch_prefix_attention<T>(const T *, T *, const PrefixBatch &, float *, hipStream_t);
+int64_t attention_join_wgs(const PrefixBatch &b, int parts) { return join_wgs(b, parts); }
+
+template <typename T>
+void launch_attention_join(T *out, const PrefixBatch &b, int parts, int part_blocks, float *po, float *pml,
+                           hipStream_t s) {
+  PrefixArgs a{};
+  a.b = b;
+  a.osplits = a.parts = parts;
+  a.oblk = part_blocks;
+  a.po = po;
+  a.pml = pml;
+  b.kv.head_dim == 128 ? launch_join<T, 128>(out, a, s) : launch_join<T, 64>(out, a, s);
+}
+
+#define INST(T)                                                                                             \
+  template bool launch_prefix_attention<T>(const T *, T *, const PrefixBatch &, float *, hipStream_t);     \
+  template void launch_attention_join<T>(T *, const PrefixBatch &, int, int, float *, float *, hipStream_t);
 INST(float)
 INST(bf16_t)
 INST(f16_t)
