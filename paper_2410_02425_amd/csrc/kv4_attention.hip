@@ -40,6 +40,16 @@ __device__ __forceinline__ typename Mfma<T>::v8 codes8(uint32_t w) {
   return __builtin_bit_cast(typename Mfma<T>::v8, v);
 }
 
+// Two products of fp32 weights and fp16 scales (x the low half of sv's, y the high
+// one's), each rounded once to fp16.
+__device__ __forceinline__ uint32_t mul_pair(float x, float y, uint32_t sv) {
+  uint32_t d;
+  asm("v_fma_mixlo_f16 %0, %1, %3, 0 op_sel_hi:[0,1,0]\n\tv_fma_mixhi_f16 %0, %2, %3, 0 op_sel:[0,1,0] op_sel_hi:[0,1,0]"
+      : "=&v"(d)
+      : "v"(x), "v"(y), "v"(sv));
+  return d;
+}
+
 // Maximum / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
 __device__ __forceinline__ float quads_max(float v) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -58,7 +68,7 @@ __device__ __forceinline__ float quads_sum(float v) {
 // V^T P^T as it lies; V's pairs of keys are made from its words of one key by
 // exchanging halves of bytes.
 template <typename T, int HD, int NW>
-__global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 ? 3 : 4))) void kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef Kv4<HD> F;
   constexpr bool WIDE = sizeof(T) == 4;
   typedef std::conditional_t<WIDE, bf16_t, T> QT;      // operands of the scores
@@ -87,9 +97,9 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
   const int e0 = part * a.sblk, e1 = min(e0 + a.sblk, (top + KV_BLOCK - 1) / KV_BLOCK);
   const bool direct = a.splits == 1;
   if (!direct && !a.b.seq_start && e0 >= e1) return;  // decode's join reads no such part
-  const PrefixRow w = packed_row(a, start, r0, r16, g);
-  const bool live = w.t < n && w.t < a.b.max_new;
-  const int ctx = live ? row_ctx(a.b, seq, w.t) : 0;
+  auto row_live = [&](const PrefixRow &w) __attribute__((always_inline)) { return w.t < n && w.t < a.b.max_new; };
+  const PrefixRow row = packed_row(a, start, r0, r16, g);
+  const int ctx = row_live(row) ? row_ctx(a.b, seq, row.t) : 0;
   // keys that every row of the tile sees; rows that see nothing get zeros at the end
   const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
   // lane i: block id of entry e0 + i (an item has at most 64), -1 for none
@@ -113,19 +123,19 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
                       ((int64_t)__builtin_amdgcn_readlane(id, i) * Hkv + g) * F::BYTES + (is_k ? 0 : PART);
     const uint32_t dst = is_k ? kl : vl;
     const uint32_t last = (is_k ? keys * (HD / 2) : (keys + 3) / 4 * 2 * HD) - 16;
+    const uint32_t tail = __builtin_amdgcn_readfirstlane(dst + 32 * HD);  // kept scalar where lanes part
+    if (lane < TAIL) dma16s(src, 32 * HD + lane * 16, tail);  // the scales
 #pragma unroll
     for (int c = 0; c < FULL; ++c) {
       uint32_t off = c * 1024 + lane * 16;
       if (is_k) off ^= swz(off / (HD / 2)) * 16;
       dma16s(src, min(off, last), dst + c * 1024);
     }
-    const uint32_t tail = __builtin_amdgcn_readfirstlane(dst + 32 * HD);  // kept scalar where lanes part
-    if (lane < TAIL) dma16s(src, 32 * HD + lane * 16, tail);
   };
 
   qv8 qa[NP][J];  // Q^T as the B operand: this lane's row, dims 32 j + 8 quad ..
   {
-    const T *qr = q + ((int64_t)(live ? w.token : start) * Hq + w.head) * HD + quad * 8;
+    const T *qr = q + ((int64_t)(row_live(row) ? row.token : start) * Hq + row.head) * HD + quad * 8;
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       if constexpr (!WIDE) {
@@ -149,7 +159,12 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
 #pragma unroll
   for (int x = 0; x < 2 * J; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   float mx = -INFINITY, sum = 0.f;  // of row r16; sum: this lane's keys alone
-  int ex = -25;                     // 16-bit types: exponent of V's largest scale so far, below all of them at first
+  int ex = -24;                     // 16-bit types: 2^ex is above V's largest scale so far, at first the least of all
+  // this lane's places in K's and V's halves, the rest of an address being constant
+  int kat = (8 * (r16 >> 2) + (r16 & 3)) * (HD / 2) + (J == 4 ? quad : quad >> 1) * 16;
+  kat = (kat ^ ((r16 >> 2) & (KP - 1)) * 16) + (J == 4 ? 0 : (quad & 1) * 8);
+  int skat = F::k_scale(8 * quad, 0), vat = F::v_word(8 * quad, J == 4 ? r16 : r16 >> 1), svat = F::v_scale(8 * quad, 0);
+  asm volatile("" : "+v"(kat), "+v"(skat), "+v"(vat), "+v"(svat));
   int i = left ? __builtin_ctzll(left) : 0;
   if (left) {
     copy(i, true);
@@ -164,14 +179,15 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
     float s[4][4];  // key 16 t + 8 (lane's quad) .. as p below: 32 (t / 2) + 8 quad + 4 (t % 2) + e
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const int key = 32 * (t / 2) + 8 * (r16 >> 2) + 4 * (t & 1) + (r16 & 3);
+      constexpr int ROW = HD / 2;
+      const int tk = 32 * (t / 2) + 4 * (t & 1);  // the swizzle of a key is that of 8 (r16 / 4)
       uint32_t piece[J];
       if constexpr (J == 4) {
-        const u32x4_tt v = *(const u32x4_tt *)(ks + key * (HD / 2) + ((quad ^ swz(key)) * 16));
+        const u32x4_tt v = *(const u32x4_tt *)(ks + kat + tk * ROW);
 #pragma unroll
         for (int j = 0; j < J; ++j) piece[j] = v[j];
       } else {
-        const u32x2_tt v = *(const u32x2_tt *)(ks + key * (HD / 2) + (((quad >> 1) ^ swz(key)) * 16) + (quad & 1) * 8);
+        const u32x2_tt v = *(const u32x2_tt *)(ks + kat + tk * ROW);
 #pragma unroll
         for (int j = 0; j < J; ++j) piece[j] = v[j];
       }
@@ -179,7 +195,7 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
 #pragma unroll
       for (int x = 0; x < J / 2; ++x)
         *(u32x4_tt *)(sk + 8 * x) =
-            *(const u32x4_tt *)(ks + F::k_scale(32 * (t / 2) + 8 * quad + 4 * (t & 1), 0) + 16 * x);
+            *(const u32x4_tt *)(ks + skat + tk * 2 * J + 16 * x);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[t][e] = 0.f;
 #pragma unroll
@@ -191,17 +207,18 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[t][e] = fmaf((float)sk[e * J + j], acc[e], s[t][e]);
       }
+      asm volatile("" : "+v"(s[t][0]), "+v"(s[t][1]), "+v"(s[t][2]), "+v"(s[t][3]));  // products end here
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
     if (more) copy(next, true);
-    const int end = min(KV_BLOCK, ctx - base);  // the row's keys: those below
+    const int end = min(KV_BLOCK, ctx - base) - 8 * quad;  // the row's keys, from the lane's first one on: those below
     const bool partly = base + KV_BLOCK > ctx_lo;
     if (partly) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (32 * (t / 2) + 8 * quad + 4 * (t & 1) + e >= end) s[t][e] = -INFINITY;
+          if (32 * (t / 2) + 4 * (t & 1) + e >= end) s[t][e] = -INFINITY;
     }
     float m = s[0][0];
 #pragma unroll
@@ -209,61 +226,59 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
 #pragma unroll
       for (int e = 0; e < 4; ++e) m = fmaxf(m, s[t][e]);
     m = fmaxf(mx, quads_max(m));
-    if (__any(m > mx)) {
-      const float corr = m == mx ? 1.f : __builtin_amdgcn_exp2f((mx - m) * c2);
+    int e = ex;
+    if constexpr (!WIDE) {
+      // weights times scales stay within fp16's range for values of any size: the
+      // weights are taken by 2^ex, above the largest of the scales so far (of keys that a row of the tile sees)
+      if (more)
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND + FULL) : "memory");  // V's scales are there
+      else
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(FULL) : "memory");
+      // lane l: J scales from l J on, of keys l J mod 64 ..
+      typedef uint32_t piece_t __attribute__((ext_vector_type(J / 2)));
+      piece_t raw = *(const piece_t *)(vs + 32 * HD + lane * J * 2);
+      const int keys = top - base - lane * J % 64;
+      float big = 0.f;
+#pragma unroll
+      for (int x = 0; x < J / 2; ++x) {
+        if (base + KV_BLOCK > top) raw[x] &= (2 * x < keys ? 0xFFFFu : 0u) | (2 * x + 1 < keys ? 0xFFFF0000u : 0u);
+        big = fmaxf(big, (float)__builtin_bit_cast(_Float16, (uint16_t)raw[x]));
+        big = fmaxf(big, (float)__builtin_bit_cast(_Float16, (uint16_t)(raw[x] >> 16)));
+      }
+      big = wave_max(big);
+      e = __builtin_amdgcn_readfirstlane(big > 0.f ? __builtin_amdgcn_frexp_expf(fminf(big, 65504.f)) : ex);
+      e = max(e, ex);
+    }
+    if (e > ex || __any(m > mx && ctx > 0)) {
+      const float corr = __builtin_amdgcn_exp2f((m == mx ? 0.f : (mx - m) * c2) + (float)(ex - e));
       mx = m;
+      ex = e;
       sum *= corr;
 #pragma unroll
       for (int x = 0; x < 2 * J; ++x)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[x][e] *= corr;
+        for (int y = 0; y < 4; ++y) o[x][y] *= corr;
     }
     const float m0 = mx == -INFINITY ? 0.f : mx;  // a row that has seen no key yet
+    const float by = WIDE ? 0.f : (float)-ex;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[t][e] = __builtin_amdgcn_exp2f((s[t][e] - m0) * c2);
-        sum += s[t][e];
+      for (int y = 0; y < 4; ++y) {
+        s[t][y] = __builtin_amdgcn_exp2f(fmaf(s[t][y] - m0, c2, by));
+        sum += s[t][y];
       }
     if (more)
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");  // V is there
     else
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    if constexpr (!WIDE) {
-      // weights times scales stay within fp16's range for values of any size:
-      // they are taken by the exponent of the largest scale (the tile's keys alone)
-      float big = 0.f;
-      const int keys = top - base;
-#pragma unroll
-      for (int x = 0; x < J; ++x) {
-        const float v = (float)*(const _Float16 *)(vs + 32 * HD + (x * 64 + lane) * 2);
-        if (lane < keys) big = fmaxf(big, v);
-      }
-      big = wave_max(big);
-      const int e = __builtin_amdgcn_readfirstlane(big > 0.f ? __builtin_amdgcn_frexp_expf(fminf(big, 65504.f)) : -25);
-      if (e > ex) {
-        const float f = __builtin_amdgcn_ldexpf(1.f, max(ex - e, -60));
-        ex = e;
-#pragma unroll
-        for (int x = 0; x < 2 * J; ++x)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) o[x][y] *= f;
-      }
-      const float f = __builtin_amdgcn_ldexpf(1.f, -ex);
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) s[t][y] *= f;
-    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       // words of keys 32 h + 8 quad .. + 7, then pairs of keys: lo the even dims', hi the odd ones'
       uint32_t x[8], lo[4], hi[4];
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const int p = 32 * h + 8 * quad + 4 * y;
-        const u32x4_tt v = *(const u32x4_tt *)(vs - PART + F::v_word(p, J == 4 ? r16 : r16 >> 1));
+        const u32x4_tt v = *(const u32x4_tt *)(ks + vat + (8 * h + y) * 2 * HD);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[4 * y + e] = J == 4 ? v[e] : v[e] >> ((r16 & 1) * 16);
       }
@@ -274,25 +289,28 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
       }
       auto group = [&](auto j_c) __attribute__((always_inline)) {
         constexpr int j = decltype(j_c)::value;
-        u32x4_tt raw = *(const u32x4_tt *)(vs - PART + F::v_scale(32 * h + 8 * quad, j));
+        u32x4_tt raw = *(const u32x4_tt *)(ks + svat + 64 * h + 128 * j);
         if (partly) {
           // scales at places that the row does not see may be anything, and 0 * NaN is not 0
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            const int key = 32 * h + 8 * quad + 2 * y;
+            const int key = 32 * h + 2 * y;
             raw[y] &= (key < end ? 0xFFFFu : 0u) | (key + 1 < end ? 0xFFFF0000u : 0u);
           }
         }
-        _Float16 sv[8];
-        *(u32x4_tt *)sv = raw;
         pv8 p[NP];
+        if constexpr (!WIDE) {
+          u32x4_tt pw;
 #pragma unroll
-        for (int y = 0; y < 8; ++y) {
-          const float f = s[2 * h + y / 4][y % 4] * (float)sv[y];
-          if constexpr (!WIDE) {
-            p[0][y] = (_Float16)f;
-          } else {
-            float v = f;
+          for (int y = 0; y < 4; ++y)
+            pw[y] = mul_pair(s[2 * h + y / 2][y % 2 * 2], s[2 * h + y / 2][y % 2 * 2 + 1], raw[y]);
+          p[0] = __builtin_bit_cast(pv8, pw);
+        } else {
+          _Float16 sv[8];
+          *(u32x4_tt *)sv = raw;
+#pragma unroll
+          for (int y = 0; y < 8; ++y) {
+            float v = s[2 * h + y / 4][y % 4] * (float)sv[y];
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
               const __bf16 part_ = (__bf16)v;
@@ -310,6 +328,7 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
           o[2 * j] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c0), p[k], o[2 * j]);
           o[2 * j + 1] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c1), p[k], o[2 * j + 1]);
         }
+        __builtin_amdgcn_sched_barrier(0);  // a group's loads and operands at a time: 128 registers
       };
       group(std::integral_constant<int, 0>());
       group(std::integral_constant<int, 1>());
@@ -323,7 +342,7 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
     i = next;
   }
   const float back = WIDE ? 1.f : __builtin_amdgcn_ldexpf(1.f, ex);
-  sum = quads_sum(sum);
+  sum = quads_sum(sum) * back;
   const int nrows = a.b.seq_start ? 16 : min(16, a.G - r0);
   // o goes where K and V were, row r16's dims side by side
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -339,6 +358,10 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
       }
   }
   __syncthreads();
+  int l16 = r16;
+  asm volatile("" : "+v"(l16));  // found again here, not held in registers over the walk
+  const PrefixRow w = packed_row(a, start, r0, l16, g);
+  const bool live = row_live(w);
   // a wave a row: its lanes over the dims
   for (int r = wave; r < nrows; r += NW) {
     if (!__builtin_amdgcn_readlane((int)live, r)) continue;
@@ -372,7 +395,7 @@ __global__ __launch_bounds__(NW * 64) void kv4_rows_kernel(const T *__restrict__
 // Blocks of a split.
 static int kv4_split(int64_t pairs, int blocks) {
   const int want = (int)std::max<int64_t>(1, 1024 / std::max<int64_t>(1, std::min<int64_t>(pairs, 1024)));
-  return std::min(64, std::max(ceil_div(blocks, want), std::min(blocks, 8)));
+  return std::min(std::max(ceil_div(blocks, want), std::min(blocks, 8)), 24);
 }
 
 static void kv4_plan(Kv4Args &a, bool decode, int rows, int n_heads, int n_kv_heads, int max_ctx, int n_seq,
