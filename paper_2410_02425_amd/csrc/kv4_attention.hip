@@ -390,6 +390,325 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
   }
 }
 
+// Many rows of a 16-bit type, on 32x32x16 MFMAs in fp16: a workgroup owns 128 packed
+// rows of a sequence, 32 to a wave, and walks the sequence's blocks.  Codes are
+// turned into values once for all of its rows: a block's are loaded into
+// registers while the one before is worked on, multiplied by their scales (exact:
+// a value has 8 significant bits) and put into LDS, K by rows, V by dims, with the
+// 16-byte pieces of a row XOR-swizzled against bank conflicts.  Two stages.
+//   S^T = K Q^T: a lane holds one row's scores; the K row of MFMA row i is i with
+//   bits 2 and 3 swapped, so that the eight weights a lane holds of each 16 keys
+//   are consecutive keys, the operand of O^T += V^T P^T.
+// bf16: a row of q is taken by its largest exponent, which the scores' factor
+// brings back; its fp16 is then exact but for values below 2^-14 of the largest,
+// whose rounding (2^-25 of the largest) is that of the fp32 sums.
+// Values at places that no row of the tile sees are 0.  Where V's scale is not of
+// the format (NaN: the group held an infinity or NaN), the values are 0 as well, and the
+// rows that see the place get NaN in the group's dims afterwards.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv4_tile_kernel(
+    const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
+  typedef Kv4<HD> F;
+  typedef f16x8_t v8;
+  typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+  constexpr int QW = 4, RT = QW * 32;  // waves, rows
+  constexpr int J = F::J, KS = HD / 16, NT = HD / 32;
+  constexpr int CK = HD / 8;           // 16-byte pieces of a K row
+  constexpr int PB = 64 * HD * 2, STAGE = 2 * PB;
+  typedef uint32_t words_t __attribute__((ext_vector_type(J)));
+  __shared__ __attribute__((aligned(1024))) char lds[2 * STAGE];
+  __shared__ int odd_at[2];  // 1 + the block of a stage whose V scales are not all of the format
+  const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int l32 = lane & 31, hh = lane >> 5;
+  const int i0 = div_by(blockIdx.x, a.by_hkv), g = blockIdx.x - i0 * Hkv;
+  const int part = div_by(i0, a.by_units);
+  int j_, r0;
+  if (!own_tile<RT>(a, i0 - part * a.units, j_, r0)) return;
+  const int seq = __builtin_amdgcn_readfirstlane(j_);
+  r0 = __builtin_amdgcn_readfirstlane(r0);
+  int start, n;
+  seq_rows(a.b, seq, start, n);
+  const int slot = a.b.seq_slot[seq];
+  const int top = row_ctx(a.b, seq, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
+  const int e0 = part * a.sblk, e1 = min(e0 + a.sblk, (top + KV_BLOCK - 1) / KV_BLOCK);
+  const PrefixRow w = packed_row(a, start, r0, wave * 32 + l32, g);
+  const bool live = w.t < n && w.t < a.b.max_new;
+  const int wctx = live ? row_ctx(a.b, seq, w.t) : 0;
+  // rows that do not exist or see nothing (zeros at the end, whatever is summed for them) ask for no mask
+  const int ctx = wctx ? wctx : INT_MAX;
+  const int ctx_lo = (int)wave_min_u32((uint32_t)ctx);
+  const int ctx_top = (int)~wave_min_u32(~(uint32_t)wctx);
+
+  // Block ids: lane i holds that of entry win + i, -1 for none.
+  int win = e0, ids = -1;
+  auto window = [&]() __attribute__((always_inline)) {
+    ids = -1;
+    if (win + lane < e1 && win + lane < a.b.kv.max_blocks) {
+      ids = a.b.kv.block_table[(int64_t)slot * a.b.kv.max_blocks + win + lane];
+      if (ids >= a.b.kv.n_blocks) ids = -1;
+    }
+  };
+  // This thread's share of a block: K row kr, octets ki of its groups; V word vw of positions 4 vq ..
+  const int kr = tid >> 2, ki = tid & 3, vq = tid & 15, vw = tid >> 4;
+  const bool has_v = vw < HD / 8;
+  words_t kc;
+  _Float16 ksc[J];
+  u32x4_tt vc;
+  u32x2_tt vsc[J];
+  int loaded = -1;  // id of the block in these registers, -1 for none
+  auto head_of = [&](int id) __attribute__((always_inline)) {
+    return (const char *)a.b.kv.k + ((int64_t)id * Hkv + g) * F::BYTES;
+  };
+  auto load = [&](int e) __attribute__((always_inline)) {
+    if (e >= win + 64) {
+      win = e;
+      window();
+    }
+    loaded = __builtin_amdgcn_readlane(ids, e - win);
+    if (loaded < 0) return;
+    const char *src = head_of(loaded);
+    kc = *(const words_t *)(src + F::k_row(kr) + 4 * J * ki);
+    if constexpr (J == 4)
+      *(u32x2_tt *)ksc = *(const u32x2_tt *)(src + F::k_scale(kr, 0));
+    else
+      *(uint32_t *)ksc = *(const uint32_t *)(src + F::k_scale(kr, 0));
+    if (has_v) {
+      vc = *(const u32x4_tt *)(src + F::v_word(4 * vq, vw));
+#pragma unroll
+      for (int j = 0; j < J; ++j) vsc[j] = *(const u32x2_tt *)(src + F::v_scale(4 * vq, j));
+    }
+  };
+  auto swz = [](int row) __attribute__((always_inline)) { return CK == 16 ? row & 15 : (row >> 1) & 7; };
+  // The loaded block's values into a stage.
+  auto fill = [&](int e, int stage) __attribute__((always_inline)) {
+    char *ks = lds + stage * STAGE, *vs = ks + PB;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const half2_t s = {ksc[j], ksc[j]};
+      const half2_t y[4] = {__builtin_bit_cast(half2_t, kv4_pair16<f16_t, 0>(kc[j])) * s,
+                            __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 1>(kc[j])) * s,
+                            __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 2>(kc[j])) * s,
+                            __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 3>(kc[j])) * s};
+      const u32x4_tt v = {__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]),
+                          __builtin_bit_cast(uint32_t, y[2]), __builtin_bit_cast(uint32_t, y[3])};
+      *(u32x4_tt *)(ks + kr * HD * 2 + (((4 * j + ki) ^ swz(kr)) * 16)) = v;
+    }
+    if (!has_v) return;
+    const int keys = top - e * KV_BLOCK - 4 * vq;  // that some row sees, of this thread's four
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        uint32_t s = vsc[j][y] & ((2 * y < keys ? 0xFFFFu : 0u) | (2 * y + 1 < keys ? 0xFFFF0000u : 0u));
+        // past 10752, the largest scale, are the infinities and NaN
+        if ((s & 0x7FFFu) > 0x7140u) odd = true, s &= 0xFFFF0000u;
+        if ((s & 0x7FFF0000u) > 0x71400000u) odd = true, s &= 0xFFFFu;
+        vsc[j][y] = s;
+      }
+    if (odd) odd_at[stage] = e + 1;
+    uint32_t lo[2], hi[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      lo[y] = (vc[2 * y] & 0x0F0F0F0Fu) | ((vc[2 * y + 1] << 4) & 0xF0F0F0F0u);
+      hi[y] = ((vc[2 * y] >> 4) & 0x0F0F0F0Fu) | (vc[2 * y + 1] & 0xF0F0F0F0u);
+    }
+    auto byte = [&](auto b_c) __attribute__((always_inline)) {
+      constexpr int b = decltype(b_c)::value, j = b % J;
+      const int d = 32 * j + 2 * ((4 * vw + b) / J);
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const half2_t y0 = __builtin_bit_cast(half2_t, kv4_pair16<f16_t, b>(z ? hi[0] : lo[0])) *
+                           __builtin_bit_cast(half2_t, (uint32_t)vsc[j][0]);
+        const half2_t y1 = __builtin_bit_cast(half2_t, kv4_pair16<f16_t, b>(z ? hi[1] : lo[1])) *
+                           __builtin_bit_cast(half2_t, (uint32_t)vsc[j][1]);
+        const u32x2_tt v = {__builtin_bit_cast(uint32_t, y0), __builtin_bit_cast(uint32_t, y1)};
+        *(u32x2_tt *)(vs + (d + z) * KV_BLOCK * 2 + (((vq >> 1) ^ ((d >> 1) & 7)) * 16) + (vq & 1) * 8) = v;
+      }
+    };
+    byte(std::integral_constant<int, 0>());
+    byte(std::integral_constant<int, 1>());
+    byte(std::integral_constant<int, 2>());
+    byte(std::integral_constant<int, 3>());
+  };
+
+  if (e0 < e1) {
+    window();
+    load(e0);
+  }
+  v8 qb[KS];  // Q^T as the operand: this lane's row, dims 16 k + 8 hh ..
+  float c2 = KV4_C2<HD>, unit = 1.f;  // base-2 factor of a score, the row's power of two
+  {
+    const T *qr = q + ((int64_t)(live ? w.token : start) * Hq + w.head) * HD + hh * 8;
+    if constexpr (std::is_same_v<T, f16_t>) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) qb[k] = load8<T>(qr + k * 16);
+    } else {
+      bf16x8_t x[KS];
+      float big = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        x[k] = load8<T>(qr + k * 16);
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const float v = fabsf((float)x[k][y]);
+          big = v < INFINITY ? fmaxf(big, v) : big;
+        }
+      }
+      big = half_swap_max(big);
+      const int ex = big > 0.f ? __builtin_amdgcn_frexp_expf(big) : 0;
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int y = 0; y < 8; ++y) qb[k][y] = (_Float16)__builtin_amdgcn_ldexpf((float)x[k][y], -ex);
+      unit = __builtin_amdgcn_ldexpf(1.f, ex);
+      c2 *= unit;
+    }
+  }
+  floatx16_t o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  // running maximum (scores in the row's unit), this half's share of the sum
+  float mx = -INFINITY, lsum = 0.f;
+  const int krow = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
+  const int kfb = krow * HD * 2, kfx = (hh ^ swz(krow)) << 4;
+  const int vfb = l32 * KV_BLOCK * 2, vfx = (hh ^ ((l32 >> 1) & 7)) << 4;
+  if (tid < 2) odd_at[tid] = 0;
+  int staged = loaded;  // id of the stage's block
+  __syncthreads();  // odd_at is 0
+  if (e0 < e1) {
+    if (loaded >= 0) fill(e0, 0);
+    if (e0 + 1 < e1) load(e0 + 1);
+  }
+  __syncthreads();
+  for (int e = e0; e < e1; ++e) {
+    const int base = e * KV_BLOCK, stage = (e - e0) & 1;
+    char *ks = lds + stage * STAGE, *vs = ks + PB;
+    if (staged >= 0 && base < ctx_top) {  // else no block, or wholly past this wave's rows
+      floatx16_t s[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const v8 f = *(const v8 *)(ks + kfb + t * 32 * HD * 2 + (kfx ^ (k << 5)));
+          s[t] = Mfma<f16_t>::m32(f, qb[k], s[t]);
+        }
+      }
+      // s[t][r]: key 32 t + 16 (r / 8) + 8 hh + r % 8 of the block
+      const int end = min(KV_BLOCK, ctx - base);  // the row's keys: those below
+      if (base + KV_BLOCK > ctx_lo || base + KV_BLOCK > top) {
+        const int lim = min(end, top - base) - 8 * hh;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (t * 32 + (r >> 3) * 16 + (r & 7) >= lim) s[t][r] = -INFINITY;
+      }
+      float m = s[0][0];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fmaxf(m, s[t][r]);
+      m = half_swap_max(m);
+      if (__any(m > mx)) {
+        const float nm = fmaxf(mx, m);
+        const float corr = nm == mx ? 1.f : __builtin_amdgcn_exp2f((mx - nm) * c2);
+        mx = nm;
+        lsum *= corr;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[t][r] *= corr;
+      }
+      const float m0 = mx == -INFINITY ? 0.f : mx;  // a row that has seen no key yet
+      v8 pb[4];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float p[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            p[r] = __builtin_amdgcn_exp2f((s[t][u * 8 + r] - m0) * c2);
+            lsum += p[r];
+          }
+          // the one rounding below 32 bits before the result's: MFMA operands have 16 (the sum stays unrounded)
+          pb[t * 2 + u] = pack8<f16_t>(p);
+        }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const v8 f = *(const v8 *)(vs + vfb + t * 32 * KV_BLOCK * 2 + (vfx ^ (k << 5)));
+          o[t] = Mfma<f16_t>::m32(f, pb[k], o[t]);
+        }
+      if (odd_at[stage] == e + 1) {
+        const char *sc = head_of(staged);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint32_t x = *(const uint16_t *)(sc + F::v_scale(lane, t));
+          const uint64_t bad = __ballot((x & 0x7FFFu) > 0x7140u);
+          const uint64_t mine = end >= 64 ? ~0ull : end > 0 ? (1ull << end) - 1 : 0;
+          if (bad & mine) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[t][r] = __uint_as_float(0x7FC00000u);
+          }
+        }
+      }
+    }
+    staged = loaded;
+    if (e + 1 < e1) {
+      if (loaded >= 0) fill(e + 1, stage ^ 1);
+      if (e + 2 < e1) load(e + 2);
+    }
+    __syncthreads();
+  }
+  if (!wctx) {
+    mx = -INFINITY;
+    lsum = 0.f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
+  }
+  // o[t][r]: dim 32 t + 8 (r / 4) + 4 hh + r % 4 of this lane's row
+  const float sum = half_swap_sum(lsum);
+  const int64_t row = (int64_t)w.token * Hq + w.head;
+  if (a.splits == 1) {
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) store_o32(out + row * HD + t * 32, o[t], inv, hh, live);
+    return;
+  }
+  // Through LDS, so that a row's dims leave as one run of bytes: 16-byte pieces
+  // XOR-swizzled by the row, the wave's 32 rows in a place of its own.
+  constexpr int LR = HD / 4, RI = 64 / LR;  // lanes of a row, rows of a store
+  char *own = lds + wave * 32 * HD * 4;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const int piece = t * 8 + r / 2 + hh;
+      *(float4 *)(own + l32 * HD * 4 + ((piece ^ (l32 % LR)) * 16)) =
+          make_float4(o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3]);
+    }
+  if (live && hh == 0) *(float2 *)(a.pml + (row * a.splits + part) * 2) = make_float2(mx * unit, sum);
+  const uint32_t rows_live = e0 < e1 ? (uint32_t)__ballot(live) : 0;  // the join skips o of empty parts
+#pragma unroll 4
+  for (int i = 0; i < 32 / RI; ++i) {
+    const int x = i * RI + lane / LR;
+    const float4 v = *(const float4 *)(own + x * HD * 4 + (((lane % LR) ^ (x % LR)) * 16));
+    const PrefixRow y = packed_row(a, start, r0, wave * 32 + x, g);
+    if (rows_live >> x & 1)
+      *(float4 *)(a.po + (((int64_t)y.token * Hq + y.head) * a.splits + part) * HD + lane % LR * 4) = v;
+  }
+}
+
 // ------------------------------------------------------------------ plan
 
 // Blocks of a split.
@@ -398,15 +717,20 @@ static int kv4_split(int64_t pairs, int blocks) {
   return std::min(std::max(ceil_div(blocks, want), std::min(blocks, 8)), 24);
 }
 
-static void kv4_plan(Kv4Args &a, bool decode, int rows, int n_heads, int n_kv_heads, int max_ctx, int n_seq,
+static void kv4_plan(Kv4Args &a, bool decode, bool tile, int rows, int n_heads, int n_kv_heads, int max_ctx, int n_seq,
                      int max_new) {
   a.G = n_heads / n_kv_heads;
-  const int live = std::min(n_seq, rows);
+  const int live = std::min(n_seq, rows), rt = tile ? 128 : 16;
   a.units = decode ? rows * ceil_div(a.G, 16)
-                   : (int)std::min((int64_t)live * ceil_div((int64_t)std::min(max_new, rows) * a.G, 16),
-                                   (int64_t)rows * a.G / 16 + live);
+                   : (int)std::min((int64_t)live * ceil_div((int64_t)std::min(max_new, rows) * a.G, rt),
+                                   (int64_t)rows * a.G / rt + live);
   const int blocks = ceil_div(max_ctx, KV_BLOCK);
-  a.sblk = kv4_split((int64_t)a.units * n_kv_heads, blocks);
+  if (tile) {
+    const int64_t items = (int64_t)a.units * n_kv_heads;
+    a.sblk = items >= 256 ? blocks : std::max(ceil_div(blocks, 512 / items), std::min(blocks, 8));
+  } else {
+    a.sblk = kv4_split((int64_t)a.units * n_kv_heads, blocks);
+  }
   a.splits = ceil_div(blocks, a.sblk);
 }
 
@@ -421,7 +745,8 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   a.b = b;
   const bool decode = !b.seq_start;
   const int Hkv = b.kv.n_kv_heads;
-  kv4_plan(a, decode, b.rows, b.n_heads, Hkv, b.max_ctx, b.n_seq, b.max_new);
+  const bool tile = sizeof(T) == 2 && !decode && (int64_t)std::min(b.max_new, b.rows) * (b.n_heads / Hkv) > 32;
+  kv4_plan(a, decode, tile, b.rows, b.n_heads, Hkv, b.max_ctx, b.n_seq, b.max_new);
   a.po = ws;
   a.pml = ws + (size_t)b.rows * b.n_heads * a.splits * HD;
   a.by_g = divisor(a.G);
@@ -430,7 +755,9 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   a.by_per = divisor(ceil_div(a.G, 16));
   const int64_t wgs = (int64_t)a.units * a.splits * Hkv;
   if (std::max(wgs, attention_join_wgs(b, a.splits)) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads
-  kv4_rows_kernel<T, HD, 4><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
+  if constexpr (sizeof(T) == 2)
+    if (tile) kv4_tile_kernel<T, HD><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
+  if (!tile) kv4_rows_kernel<T, HD, 4><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
   if (a.splits > 1) launch_attention_join<T>(out, b, a.splits, a.sblk, a.po, a.pml, s);
   return true;
 }

@@ -127,61 +127,213 @@ void launch_kv4_append(const QkvAppend &a, T *q, uint8_t *cache, hipStream_t s) 
 
 // ------------------------------------------------------------------ read
 
-// A thread takes one word (8 codes) of K or V of a row and head.
-template <typename T, int HD>
+// Whether rows q .. q + 3 go from four places side by side to four others, both
+// on a multiple of four: their V words are then one 16-byte load, and a dim's
+// four positions one store.
+__device__ __forceinline__ bool kv4_quartet(const Kv4Read &a, int q) {
+  if (q < 0 || q > a.rows - 4) return false;
+  const int64_t s = a.src_entry[q], d = a.dst_entry[q];
+  if (s < 0 || d < 0 || ((s | d) & 3) || s >= a.n_blocks * KV_BLOCK || d >= a.n_dst_blocks * KV_BLOCK) return false;
+  bool run = true;
+#pragma unroll
+  for (int i = 1; i < 4; ++i) run = run && a.src_entry[q + i] == s + i && a.dst_entry[q + i] == d + i;
+  return run;
+}
+
+// A K row's octets i of every group (J words), scaled: J runs of eight dims.
+template <typename T, int J, typename W, typename S>
+__device__ __forceinline__ void kv4_k_store(T *dst, const W &c, const S &s) {
+  typedef T vec8 __attribute__((ext_vector_type(8)));
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const f32x2_t y[4] = {kv4_pair32<0>(c[j]), kv4_pair32<1>(c[j]), kv4_pair32<2>(c[j]), kv4_pair32<3>(c[j])};
+    vec8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = round_to<T>(y[e / 2][e % 2] * (float)s[j]);
+    __builtin_nontemporal_store(o, (vec8 *)(dst + 32 * j));
+  }
+}
+
+// V's word w of four positions, scaled: eight dims of `there` positions from dst on.
+template <typename T, int J, typename S>
+__device__ __forceinline__ void kv4_v_store(T *dst, const u32x4_tt &x, const S *s, int w, int there) {
+  typedef T vec4 __attribute__((ext_vector_type(4)));
+  // pairs of positions: bytes of even dims, of odd ones
+  uint32_t lo[2], hi[2];
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    lo[y] = (x[2 * y] & 0x0F0F0F0Fu) | ((x[2 * y + 1] << 4) & 0xF0F0F0F0u);
+    hi[y] = ((x[2 * y] >> 4) & 0x0F0F0F0Fu) | (x[2 * y + 1] & 0xF0F0F0F0u);
+  }
+  auto byte = [&](auto b_c) __attribute__((always_inline)) {
+    constexpr int b = decltype(b_c)::value, j = b % J;
+    const int d = 32 * j + 2 * ((4 * w + b) / J);
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const f32x2_t y0 = kv4_pair32<b>(z ? hi[0] : lo[0]), y1 = kv4_pair32<b>(z ? hi[1] : lo[1]);
+      const vec4 o = {round_to<T>(y0[0] * (float)s[j][0]), round_to<T>(y0[1] * (float)s[j][1]),
+                      round_to<T>(y1[0] * (float)s[j][2]), round_to<T>(y1[1] * (float)s[j][3])};
+      T *to = dst + (d + z) * KV_BLOCK;
+      if (there >= 4) {
+        __builtin_nontemporal_store(o, (vec4 *)to);
+      } else {
+        for (int e = 0; e < there; ++e) to[e] = o[e];
+      }
+    }
+  };
+  byte(std::integral_constant<int, 0>());
+  byte(std::integral_constant<int, 1>());
+  byte(std::integral_constant<int, 2>());
+  byte(std::integral_constant<int, 3>());
+}
+
+// A workgroup takes about ROWS rows of a head.  It begins at the first of its ROWS
+// places in the list that goes to a multiple of ROWS, if there is one, and ends
+// where the next workgroup begins: rows in the order of their positions are then
+// taken block by block, and no line of V is written by two workgroups (16 contexts
+// of 13B heads, bf16: 231 us without).
+//   * Rows that go from the beginning of a block to the beginning of one, place by
+//     place: all loads are requested at once, four threads a row of K, a thread
+//     a word of V of four positions, so that a wave's stores are whole lines of
+//     dims' positions.
+//   * Others: quartets (rows that go from four places to four) are listed first
+//     and stored alike, rows of no quartet go one by one.
+// Bound by memory, which is nearly all writes.
+template <typename T, int HD, int ROWS>
 __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Read a, T *__restrict__ k, T *__restrict__ v) {
   typedef Kv4<HD> F;
   constexpr int J = F::J, WORDS = HD / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int w = (int)(i % WORDS);
-  const int64_t unit = i / WORDS;
-  const int h = (int)(unit % (2 * a.n_kv_heads));
-  const int64_t row = unit / (2 * a.n_kv_heads);
-  if (row >= a.rows) return;
-  const int64_t from = a.src_entry[row], to = a.dst_entry[row];
-  if (from < 0 || from >= a.n_blocks * KV_BLOCK || to < 0 || to >= a.n_dst_blocks * KV_BLOCK) return;
-  const bool is_k = h < a.n_kv_heads;
-  const int head = is_k ? h : h - a.n_kv_heads, p = (int)(from % KV_BLOCK), d = (int)(to % KV_BLOCK);
-  const uint8_t *src = a.cache + (from / KV_BLOCK * a.n_kv_heads + head) * (int64_t)F::BYTES;
-  const int64_t base = (to / KV_BLOCK * a.n_kv_heads + head) * (int64_t)(KV_BLOCK * HD);
-  const auto pairs = [](uint32_t c, f32x2_t *x) __attribute__((always_inline)) {
-    x[0] = kv4_pair32<0>(c);
-    x[1] = kv4_pair32<1>(c);
-    x[2] = kv4_pair32<2>(c);
-    x[3] = kv4_pair32<3>(c);
+  typedef uint32_t words_t __attribute__((ext_vector_type(J)));
+  typedef _Float16 scales_t __attribute__((ext_vector_type(J)));
+  typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+  __shared__ int first[ROWS], counts[2];  // quartets' first rows from the front, single rows from the back
+  const int t = threadIdx.x, lane = t & 63;
+  const int tile = blockIdx.x / a.n_kv_heads, h = blockIdx.x - tile * a.n_kv_heads;
+  const int64_t src_end = a.n_blocks * KV_BLOCK, dst_end = a.n_dst_blocks * KV_BLOCK;
+  auto src_of = [&](uint64_t from) __attribute__((always_inline)) {
+    return a.cache + (from / KV_BLOCK * a.n_kv_heads + h) * F::BYTES;
   };
-  f32x2_t x[4];
-  if (is_k) {
-    const int o = w / J, j = w % J;
-    pairs(*(const uint32_t *)(src + F::k_row(p) + 4 * w), x);
-    const float s = (float)*(const _Float16 *)(src + F::k_scale(p, j));
-    T *dst = k + base + d * HD + 32 * j + 8 * o;
+  auto dst_of = [&](uint64_t to) __attribute__((always_inline)) {
+    return (int64_t)((to / KV_BLOCK * a.n_kv_heads + h) * (KV_BLOCK * HD));
+  };
+  // the entries of this workgroup's places and of the next one's
+  const int at = tile * ROWS;
+  int64_t s[2], d[2];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      dst[2 * b] = round_to<T>(x[b][0] * s);
-      dst[2 * b + 1] = round_to<T>(x[b][1] * s);
-    }
-  } else {
-    pairs(*(const uint32_t *)(src + F::v_word(p, w)), x);
+  for (int x = 0; x < 2; ++x) {
+    const int r = at + x * ROWS + lane;
+    const bool there = lane < ROWS && r < a.rows;
+    s[x] = there ? a.src_entry[r] : -1;
+    d[x] = there ? a.dst_entry[r] : -1;
+  }
+  const uint64_t b0 = __ballot((d[0] & (ROWS - 1)) == 0), b1 = __ballot((d[1] & (ROWS - 1)) == 0);
+  const int skip = tile && b0 ? __builtin_ctzll(b0) : 0;
+  int r0 = at + skip;
+  const int end = min(at + ROWS + (b1 ? __builtin_ctzll(b1) : 0), a.rows);
+  if (ROWS == 64 && r0 < end) {
+    const int n = min(ROWS, end - r0);
+    const uint64_t s0 = readlane_u64(s[0], skip), d0 = readlane_u64(d[0], skip);
+    bool run = true;
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const int j = b % J, r = (4 * w + b) / J;
-      const float s = (float)*(const _Float16 *)(src + F::v_scale(p, j));
-      T *dst = v + base + (int64_t)(32 * j + 2 * r) * KV_BLOCK + d;
-      dst[0] = round_to<T>(x[b][0] * s);
-      dst[KV_BLOCK] = round_to<T>(x[b][1] * s);
+    for (int x = 0; x < 2; ++x) {
+      const int i = x * ROWS + lane - skip;  // of the rows from r0 on
+      run = run && (i < 0 || i >= n || (s[x] == (int64_t)s0 + i && d[x] == (int64_t)d0 + i));
     }
+    if (__all(run) && ((s0 | d0) & 63) == 0 && s0 < (uint64_t)src_end && d0 < (uint64_t)dst_end) {
+      const uint8_t *src = src_of(s0);
+      const int row = t / 4, i = t % 4;
+      const int q = t % 16, w = t / 16, there = w < WORDS ? n - 4 * q : 0;
+      words_t kc;
+      scales_t ks;
+      u32x4_tt x;
+      half4 vs[J];
+      if (row < n) {
+        kc = *(const words_t *)(src + F::k_row(row) + 4 * J * i);
+        ks = *(const scales_t *)(src + F::k_scale(row, 0));
+      }
+      if (there > 0) {
+        x = *(const u32x4_tt *)(src + F::v_word(4 * q, w));
+#pragma unroll
+        for (int j = 0; j < J; ++j) vs[j] = *(const half4 *)(src + F::v_scale(4 * q, j));
+      }
+      if (row < n) kv4_k_store<T, J>(k + dst_of(d0) + row * HD + 8 * i, kc, ks);
+      if (there > 0) kv4_v_store<T, J>(v + dst_of(d0) + 4 * q, x, vs, w, there);
+      r0 += n;
+    }
+  }
+  for (; r0 < end; r0 += ROWS) {
+    const int n = min(ROWS, end - r0);
+    if (t < 64) {
+      const int r = r0 + t;
+      const bool lead = t < n && kv4_quartet(a, r);
+      bool single = false;
+      if (!lead && t < n) {
+        const int64_t from = a.src_entry[r], to = a.dst_entry[r];
+        single = from >= 0 && from < src_end && to >= 0 && to < dst_end && !kv4_quartet(a, r - (int)(to & 3));
+      }
+      const uint64_t leads = __ballot(lead), singles = __ballot(single), below = (1ull << t) - 1;
+      if (lead) first[__popcll(leads & below)] = r;
+      if (single) first[ROWS - 1 - __popcll(singles & below)] = r;
+      if (t == 0) counts[0] = __popcll(leads), counts[1] = __popcll(singles);
+    }
+    if (t / 4 < n) {
+      const int i = t % 4;
+      const int64_t from = a.src_entry[r0 + t / 4], to = a.dst_entry[r0 + t / 4];
+      if (from >= 0 && from < src_end && to >= 0 && to < dst_end) {
+        const uint8_t *src = src_of(from);
+        const int p = (int)(from % KV_BLOCK);
+        const words_t c = *(const words_t *)(src + F::k_row(p) + 4 * J * i);
+        const scales_t ks = *(const scales_t *)(src + F::k_scale(p, 0));
+        kv4_k_store<T, J>(k + dst_of(to) + (int)(to % KV_BLOCK) * HD + 8 * i, c, ks);
+      }
+    }
+    __syncthreads();
+    const int quartets = counts[0], singles = counts[1];
+    for (int i = t; i < ROWS / 4 * WORDS; i += 256) {
+      const int q = i % (ROWS / 4), w = i / (ROWS / 4);
+      if (q >= quartets) continue;
+      const uint64_t from = a.src_entry[first[q]], to = a.dst_entry[first[q]];
+      const uint8_t *src = src_of(from);
+      const int p = (int)(from % KV_BLOCK);
+      half4 vs[J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) vs[j] = *(const half4 *)(src + F::v_scale(p, j));
+      kv4_v_store<T, J>(v + dst_of(to) + (int)(to % KV_BLOCK), *(const u32x4_tt *)(src + F::v_word(p, w)), vs, w, 4);
+    }
+    for (int i = t; i < singles * WORDS; i += 256) {
+      const int w = i / singles, r = first[ROWS - 1 - (i - w * singles)];  // lanes are rows: neighbours may be beside each other
+      const uint64_t from = a.src_entry[r], to = a.dst_entry[r];
+      const uint8_t *src = src_of(from);
+      const int p = (int)(from % KV_BLOCK);
+      const uint32_t c = *(const uint32_t *)(src + F::v_word(p, w));
+      const f32x2_t y[4] = {kv4_pair32<0>(c), kv4_pair32<1>(c), kv4_pair32<2>(c), kv4_pair32<3>(c)};
+      T *dst = v + dst_of(to) + (int)(to % KV_BLOCK);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        const float f = (float)*(const _Float16 *)(src + F::v_scale(p, b % J));
+        const int dim = 32 * (b % J) + 2 * ((4 * w + b) / J);
+        dst[dim * KV_BLOCK] = round_to<T>(y[b][0] * f);
+        dst[(dim + 1) * KV_BLOCK] = round_to<T>(y[b][1] * f);
+      }
+    }
+    __syncthreads();  // the lists have been used
   }
 }
 
 template <typename T>
 void launch_kv4_read(const Kv4Read &a, T *k, T *v, hipStream_t s) {
-  const int64_t threads = (int64_t)a.rows * 2 * a.n_kv_heads * (a.head_dim / 8);
-  const unsigned wgs = (unsigned)((threads + 255) / 256);
+  const auto run = [&](auto hd, auto rows) {
+    constexpr int HD = decltype(hd)::value, ROWS = decltype(rows)::value;
+    const unsigned wgs = (unsigned)ceil_div(a.rows, ROWS) * (unsigned)a.n_kv_heads;
+    kv4_read_kernel<T, HD, ROWS><<<wgs, 256, 0, s>>>(a, k, v);
+  };
+  typedef std::integral_constant<int, 64> c64;
+  typedef std::integral_constant<int, 16> c16;
+  const bool large = (int64_t)ceil_div(a.rows, 64) * a.n_kv_heads >= 512;
   if (a.head_dim == 128)
-    kv4_read_kernel<T, 128><<<wgs, 256, 0, s>>>(a, k, v);
+    large ? run(std::integral_constant<int, 128>(), c64()) : run(std::integral_constant<int, 128>(), c16());
   else
-    kv4_read_kernel<T, 64><<<wgs, 256, 0, s>>>(a, k, v);
+    large ? run(c64(), c64()) : run(c64(), c16());
 }
 
 #define INST(T)                                                                        \
