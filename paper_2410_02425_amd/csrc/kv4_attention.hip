@@ -405,13 +405,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 // Values at places that no row of the tile sees are 0.  Where V's scale is not of
 // the format (NaN: the group held an infinity or NaN), the values are 0 as well, and the
 // rows that see the place get NaN in the group's dims afterwards.
-template <typename T, int HD>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv4_tile_kernel(
+constexpr float KV4_LAZY = 8.f;
+constexpr float KV4_LARGE = 64.f;  // base-2 score up to which the rounded mc is within 2^-19: weights within 1.3e-6
+template <typename T, int HD, int QW>
+__global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) void kv4_tile_kernel(
     const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef Kv4<HD> F;
   typedef f16x8_t v8;
   typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-  constexpr int QW = 4, RT = QW * 32;  // waves, rows
+  constexpr int RT = QW * 32;          // rows, QW waves
   constexpr int J = F::J, KS = HD / 16, NT = HD / 32;
   constexpr int CK = HD / 8;           // 16-byte pieces of a K row
   constexpr int PB = 64 * HD * 2, STAGE = 2 * PB;
@@ -450,41 +452,79 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     }
   };
   // This thread's share of a block: K row kr, octets ki of its groups; V word vw of positions 4 vq ..
-  const int kr = tid >> 2, ki = tid & 3, vq = tid & 15, vw = tid >> 4;
-  const bool has_v = vw < HD / 8;
+  // (of eight waves, four take K and four V)
+  const int kr = (tid >> 2) & 63, ki = tid & 3, vq = tid & 15, vw = (tid >> 4) & 15;
+  const bool has_k = QW == 4 || wave < 4, has_v = (QW == 4 || wave >= 4) && (HD == 128 || vw < HD / 8);
+  const uint32_t k_off = F::k_row(kr) + 4 * J * ki, ks_off = F::k_scale(kr, 0), v_off = F::v_word(4 * vq, vw),
+                 vs_off = 8 * vq;
   words_t kc;
   _Float16 ksc[J];
   u32x4_tt vc;
   u32x2_tt vsc[J];
-  int loaded = -1;  // id of the block in these registers, -1 for none
   auto head_of = [&](int id) __attribute__((always_inline)) {
     return (const char *)a.b.kv.k + ((int64_t)id * Hkv + g) * F::BYTES;
   };
-  auto load = [&](int e) __attribute__((always_inline)) {
+  auto find = [&](int e) __attribute__((always_inline)) {  // block id of entry e, -1 past the last
     if (e >= win + 64) {
       win = e;
       window();
     }
-    loaded = __builtin_amdgcn_readlane(ids, e - win);
-    if (loaded < 0) return;
-    const char *src = head_of(loaded);
-    kc = *(const words_t *)(src + F::k_row(kr) + 4 * J * ki);
+    return e < e1 ? __builtin_amdgcn_readlane(ids, e - win) : -1;
+  };
+  // Loads of a block that is not there are left out: what the registers hold
+  // then goes into a stage that is not read.
+  auto load_k = [&](int id) __attribute__((always_inline)) {
+    if (id < 0 || !has_k) return;
+    const char *src = head_of(id);
+    kc = *(const words_t *)(src + k_off);
     if constexpr (J == 4)
-      *(u32x2_tt *)ksc = *(const u32x2_tt *)(src + F::k_scale(kr, 0));
+      *(u32x2_tt *)ksc = *(const u32x2_tt *)(src + ks_off);
     else
-      *(uint32_t *)ksc = *(const uint32_t *)(src + F::k_scale(kr, 0));
-    if (has_v) {
-      vc = *(const u32x4_tt *)(src + F::v_word(4 * vq, vw));
+      *(uint32_t *)ksc = *(const uint32_t *)(src + ks_off);
+  };
+  auto load_v = [&](int id) __attribute__((always_inline)) {
+    if (id < 0 || !has_v) return;
+    const char *src = head_of(id);
+    vc = *(const u32x4_tt *)(src + v_off);
 #pragma unroll
-      for (int j = 0; j < J; ++j) vsc[j] = *(const u32x2_tt *)(src + F::v_scale(4 * vq, j));
-    }
+    for (int j = 0; j < J; ++j) vsc[j] = *(const u32x2_tt *)(src + F::v_scale(0, j) + vs_off);
   };
   auto swz = [](int row) __attribute__((always_inline)) { return CK == 16 ? row & 15 : (row >> 1) & 7; };
-  // The loaded block's values into a stage.
-  auto fill = [&](int e, int stage) __attribute__((always_inline)) {
-    char *ks = lds + stage * STAGE, *vs = ks + PB;
+  // V's scales of the loaded block as its values take them: 0 at places that no row
+  // sees and where they are not of the format.
+  auto check = [&](int e, int stage) __attribute__((always_inline)) {
+    if (!has_v) return;
+    if ((e + 1) * KV_BLOCK > top) {
+      const int keys = top - e * KV_BLOCK - 4 * vq;  // that some row sees, of this thread's four
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+          vsc[j][y] &= (2 * y < keys ? 0xFFFFu : 0u) | (2 * y + 1 < keys ? 0xFFFF0000u : 0u);
+    }
+    typedef uint16_t pair_t __attribute__((ext_vector_type(2)));
+    pair_t big = {0, 0};
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        big = __builtin_elementwise_max(big, __builtin_bit_cast(pair_t, (uint32_t)vsc[j][y]));
+    if (max(big[0], big[1]) > 0x7140) {  // past 10752, the largest scale, are the infinities and NaN
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t s = vsc[j][y];
+          vsc[j][y] = ((s & 0xFFFFu) > 0x7140u ? 0 : s & 0xFFFFu) | (s >= 0x71410000u ? 0 : s & 0xFFFF0000u);
+        }
+      odd_at[stage] = e + 1;
+    }
+  };
+  // The loaded block's values into a stage (where there is none, what the
+  // registers hold: that stage is not read).
+  auto fill_k = [&](int stage, int j) __attribute__((always_inline)) {  // group j
+    char *ks = lds + stage * STAGE;
+    if (has_k) {
       const half2_t s = {ksc[j], ksc[j]};
       const half2_t y[4] = {__builtin_bit_cast(half2_t, kv4_pair16<f16_t, 0>(kc[j])) * s,
                             __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 1>(kc[j])) * s,
@@ -494,48 +534,51 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                           __builtin_bit_cast(uint32_t, y[2]), __builtin_bit_cast(uint32_t, y[3])};
       *(u32x4_tt *)(ks + kr * HD * 2 + (((4 * j + ki) ^ swz(kr)) * 16)) = v;
     }
-    if (!has_v) return;
-    const int keys = top - e * KV_BLOCK - 4 * vq;  // that some row sees, of this thread's four
-    bool odd = false;
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        uint32_t s = vsc[j][y] & ((2 * y < keys ? 0xFFFFu : 0u) | (2 * y + 1 < keys ? 0xFFFF0000u : 0u));
-        // past 10752, the largest scale, are the infinities and NaN
-        if ((s & 0x7FFFu) > 0x7140u) odd = true, s &= 0xFFFF0000u;
-        if ((s & 0x7FFF0000u) > 0x71400000u) odd = true, s &= 0xFFFFu;
-        vsc[j][y] = s;
-      }
-    if (odd) odd_at[stage] = e + 1;
-    uint32_t lo[2], hi[2];
+  };
+  auto pair_v = [&]() __attribute__((always_inline)) {  // vc: bytes of even dims, of odd ones, each of two positions
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      lo[y] = (vc[2 * y] & 0x0F0F0F0Fu) | ((vc[2 * y + 1] << 4) & 0xF0F0F0F0u);
-      hi[y] = ((vc[2 * y] >> 4) & 0x0F0F0F0Fu) | (vc[2 * y + 1] & 0xF0F0F0F0u);
+      const uint32_t x0 = vc[2 * y], x1 = vc[2 * y + 1];
+      vc[2 * y] = (x0 & 0x0F0F0F0Fu) | ((x1 << 4) & 0xF0F0F0F0u);
+      vc[2 * y + 1] = ((x0 >> 4) & 0x0F0F0F0Fu) | (x1 & 0xF0F0F0F0u);
     }
+  };
+  auto fill_v = [&](int stage, int byte_) __attribute__((always_inline)) {  // byte of the word
+    if (!has_v) return;
+    char *vs = lds + stage * STAGE + PB;
     auto byte = [&](auto b_c) __attribute__((always_inline)) {
       constexpr int b = decltype(b_c)::value, j = b % J;
       const int d = 32 * j + 2 * ((4 * vw + b) / J);
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
-        const half2_t y0 = __builtin_bit_cast(half2_t, kv4_pair16<f16_t, b>(z ? hi[0] : lo[0])) *
+        const half2_t y0 = __builtin_bit_cast(half2_t, kv4_pair16<f16_t, b>(vc[z])) *
                            __builtin_bit_cast(half2_t, (uint32_t)vsc[j][0]);
-        const half2_t y1 = __builtin_bit_cast(half2_t, kv4_pair16<f16_t, b>(z ? hi[1] : lo[1])) *
+        const half2_t y1 = __builtin_bit_cast(half2_t, kv4_pair16<f16_t, b>(vc[2 + z])) *
                            __builtin_bit_cast(half2_t, (uint32_t)vsc[j][1]);
         const u32x2_tt v = {__builtin_bit_cast(uint32_t, y0), __builtin_bit_cast(uint32_t, y1)};
         *(u32x2_tt *)(vs + (d + z) * KV_BLOCK * 2 + (((vq >> 1) ^ ((d >> 1) & 7)) * 16) + (vq & 1) * 8) = v;
       }
     };
-    byte(std::integral_constant<int, 0>());
-    byte(std::integral_constant<int, 1>());
-    byte(std::integral_constant<int, 2>());
-    byte(std::integral_constant<int, 3>());
+    if (byte_ == 0) byte(std::integral_constant<int, 0>());
+    if (byte_ == 1) byte(std::integral_constant<int, 1>());
+    if (byte_ == 2) byte(std::integral_constant<int, 2>());
+    if (byte_ == 3) byte(std::integral_constant<int, 3>());
+  };
+  auto fill = [&](int stage) __attribute__((always_inline)) {
+    pair_v();
+#pragma unroll
+    for (int j = 0; j < J; ++j) fill_k(stage, j);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) fill_v(stage, b);
   };
 
+  // ids of the blocks in the stage in use, in the registers, -1 for none
+  int staged = -1, loaded = -1;
   if (e0 < e1) {
     window();
-    load(e0);
+    staged = find(e0);
+    load_k(staged);
+    load_v(staged);
   }
   v8 qb[KS];  // Q^T as the operand: this lane's row, dims 16 k + 8 hh ..
   float c2 = KV4_C2<HD>, unit = 1.f;  // base-2 factor of a score, the row's power of two
@@ -571,22 +614,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   for (int t = 0; t < NT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[t][r] = 0.f;
-  // running maximum (scores in the row's unit), this half's share of the sum
-  float mx = -INFINITY, lsum = 0.f;
+  // running maximum (scores in the row's unit), its base-2 value, this half's share of the sum
+  float mx = -INFINITY, mc = 0.f, lsum = 0.f;
+  bool large = false;  // wave-uniform: a row's |mc| is past KV4_LARGE
   const int krow = (l32 & 0x13) | ((l32 & 4) << 1) | ((l32 & 8) >> 1);
   const int kfb = krow * HD * 2, kfx = (hh ^ swz(krow)) << 4;
   const int vfb = l32 * KV_BLOCK * 2, vfx = (hh ^ ((l32 >> 1) & 7)) << 4;
   if (tid < 2) odd_at[tid] = 0;
-  int staged = loaded;  // id of the stage's block
   __syncthreads();  // odd_at is 0
   if (e0 < e1) {
-    if (loaded >= 0) fill(e0, 0);
-    if (e0 + 1 < e1) load(e0 + 1);
+    check(e0, 0);
+    fill(0);
+    loaded = find(e0 + 1);
+    load_k(loaded);
+    load_v(loaded);
   }
   __syncthreads();
   for (int e = e0; e < e1; ++e) {
     const int base = e * KV_BLOCK, stage = (e - e0) & 1;
     char *ks = lds + stage * STAGE, *vs = ks + PB;
+    const int next = find(e + 2);
     if (staged >= 0 && base < ctx_top) {  // else no block, or wholly past this wave's rows
       floatx16_t s[2];
 #pragma unroll
@@ -597,8 +644,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         for (int k = 0; k < KS; ++k) {
           const v8 f = *(const v8 *)(ks + kfb + t * 32 * HD * 2 + (kfx ^ (k << 5)));
           s[t] = Mfma<f16_t>::m32(f, qb[k], s[t]);
+          // the next block's values between the matrix instructions
+          if (k % 4 == 3) fill_k(stage ^ 1, t * (KS / 4) + k / 4);
         }
       }
+      load_k(next);  // a part of a walk's step ahead of their use, like V's below
+      if (e + 1 < e1) check(e + 1, stage ^ 1);
+      pair_v();
       // s[t][r]: key 32 t + 16 (r / 8) + 8 hh + r % 8 of the block
       const int end = min(KV_BLOCK, ctx - base);  // the row's keys: those below
       if (base + KV_BLOCK > ctx_lo || base + KV_BLOCK > top) {
@@ -615,7 +667,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
         for (int r = 0; r < 16; ++r) m = fmaxf(m, s[t][r]);
       m = half_swap_max(m);
-      if (__any(m > mx)) {
+      // The reference follows the maximum once that is past it by 2^8: weights up to
+      // there are fp16 numbers like any others, and most blocks leave o alone.
+      if (__any((m - mx) * c2 > KV4_LAZY)) {
         const float nm = fmaxf(mx, m);
         const float corr = nm == mx ? 1.f : __builtin_amdgcn_exp2f((mx - nm) * c2);
         mx = nm;
@@ -624,8 +678,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[t][r] *= corr;
+        mc = nm == -INFINITY ? 0.f : nm * c2;  // a row that has seen no key yet
+        large = __any(fabsf(mc) > KV4_LARGE);
       }
-      const float m0 = mx == -INFINITY ? 0.f : mx;  // a row that has seen no key yet
+      // s c2 - mc in one FMA is off 0 at the maximum by what mc's rounding left
+      // out: large scores have the maximum taken off before the product instead
+      float mo = mc;
+      if (large) {
+        const float m0 = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[t][r] -= m0;
+        mo = 0.f;
+      }
       v8 pb[4];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -634,25 +700,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
           float p[8];
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
-            p[r] = __builtin_amdgcn_exp2f((s[t][u * 8 + r] - m0) * c2);
+            p[r] = __builtin_amdgcn_exp2f(fmaf(s[t][u * 8 + r], c2, -mo));
             lsum += p[r];
           }
           // the one rounding below 32 bits before the result's: MFMA operands have 16 (the sum stays unrounded)
           pb[t * 2 + u] = pack8<f16_t>(p);
         }
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           const v8 f = *(const v8 *)(vs + vfb + t * 32 * KV_BLOCK * 2 + (vfx ^ (k << 5)));
           o[t] = Mfma<f16_t>::m32(f, pb[k], o[t]);
         }
+        fill_v(stage ^ 1, k);
+      }
+      load_v(next);
       if (odd_at[stage] == e + 1) {
         const char *sc = head_of(staged);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           const uint32_t x = *(const uint16_t *)(sc + F::v_scale(lane, t));
-          const uint64_t bad = __ballot((x & 0x7FFFu) > 0x7140u);
+          const uint64_t bad = __ballot(x > 0x7140u);
           const uint64_t mine = end >= 64 ? ~0ull : end > 0 ? (1ull << end) - 1 : 0;
           if (bad & mine) {
 #pragma unroll
@@ -660,12 +729,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
           }
         }
       }
+    } else {
+      if (e + 1 < e1) check(e + 1, stage ^ 1);
+      fill(stage ^ 1);
+      load_k(next);
+      load_v(next);
     }
     staged = loaded;
-    if (e + 1 < e1) {
-      if (loaded >= 0) fill(e + 1, stage ^ 1);
-      if (e + 2 < e1) load(e + 2);
-    }
+    loaded = next;
     __syncthreads();
   }
   if (!wctx) {
@@ -687,25 +758,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   }
   // Through LDS, so that a row's dims leave as one run of bytes: 16-byte pieces
   // XOR-swizzled by the row, the wave's 32 rows in a place of its own.
-  constexpr int LR = HD / 4, RI = 64 / LR;  // lanes of a row, rows of a store
-  char *own = lds + wave * 32 * HD * 4;
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) {
-      const int piece = t * 8 + r / 2 + hh;
-      *(float4 *)(own + l32 * HD * 4 + ((piece ^ (l32 % LR)) * 16)) =
-          make_float4(o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3]);
-    }
+  // (of eight waves, half of the dims at a time)
+  constexpr int TT = NT * 4 / QW, LR = TT * 8, RI = 64 / LR;  // 32-dim tiles, lanes of a row, rows of a store
+  char *own = lds + wave * 32 * LR * 16;
   if (live && hh == 0) *(float2 *)(a.pml + (row * a.splits + part) * 2) = make_float2(mx * unit, sum);
   const uint32_t rows_live = e0 < e1 ? (uint32_t)__ballot(live) : 0;  // the join skips o of empty parts
+#pragma unroll
+  for (int t0 = 0; t0 < NT; t0 += TT) {
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const int piece = t * 8 + r / 2 + hh;
+        *(float4 *)(own + l32 * LR * 16 + ((piece ^ (l32 % LR)) * 16)) =
+            make_float4(o[t0 + t][r], o[t0 + t][r + 1], o[t0 + t][r + 2], o[t0 + t][r + 3]);
+      }
 #pragma unroll 4
-  for (int i = 0; i < 32 / RI; ++i) {
-    const int x = i * RI + lane / LR;
-    const float4 v = *(const float4 *)(own + x * HD * 4 + (((lane % LR) ^ (x % LR)) * 16));
-    const PrefixRow y = packed_row(a, start, r0, wave * 32 + x, g);
-    if (rows_live >> x & 1)
-      *(float4 *)(a.po + (((int64_t)y.token * Hq + y.head) * a.splits + part) * HD + lane % LR * 4) = v;
+    for (int i = 0; i < 32 / RI; ++i) {
+      const int x = i * RI + lane / LR;
+      const float4 v = *(const float4 *)(own + x * LR * 16 + (((lane % LR) ^ (x % LR)) * 16));
+      const PrefixRow y = packed_row(a, start, r0, wave * 32 + x, g);
+      if (rows_live >> x & 1)
+        *(float4 *)(a.po + (((int64_t)y.token * Hq + y.head) * a.splits + part) * HD + t0 * 32 + lane % LR * 4) = v;
+    }
   }
 }
 
@@ -717,15 +792,15 @@ static int kv4_split(int64_t pairs, int blocks) {
   return std::min(std::max(ceil_div(blocks, want), std::min(blocks, 8)), 24);
 }
 
-static void kv4_plan(Kv4Args &a, bool decode, bool tile, int rows, int n_heads, int n_kv_heads, int max_ctx, int n_seq,
+static void kv4_plan(Kv4Args &a, bool decode, int rt, int rows, int n_heads, int n_kv_heads, int max_ctx, int n_seq,
                      int max_new) {
   a.G = n_heads / n_kv_heads;
-  const int live = std::min(n_seq, rows), rt = tile ? 128 : 16;
+  const int live = std::min(n_seq, rows);
   a.units = decode ? rows * ceil_div(a.G, 16)
                    : (int)std::min((int64_t)live * ceil_div((int64_t)std::min(max_new, rows) * a.G, rt),
                                    (int64_t)rows * a.G / rt + live);
   const int blocks = ceil_div(max_ctx, KV_BLOCK);
-  if (tile) {
+  if (rt > 16) {
     const int64_t items = (int64_t)a.units * n_kv_heads;
     a.sblk = items >= 256 ? blocks : std::max(ceil_div(blocks, 512 / items), std::min(blocks, 8));
   } else {
@@ -746,7 +821,8 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   const bool decode = !b.seq_start;
   const int Hkv = b.kv.n_kv_heads;
   const bool tile = sizeof(T) == 2 && !decode && (int64_t)std::min(b.max_new, b.rows) * (b.n_heads / Hkv) > 32;
-  kv4_plan(a, decode, tile, b.rows, b.n_heads, Hkv, b.max_ctx, b.n_seq, b.max_new);
+  const int rt = !tile ? 16 : (int64_t)b.rows * (b.n_heads / Hkv) * Hkv >= 256 * 256 ? 256 : 128;
+  kv4_plan(a, decode, rt, b.rows, b.n_heads, Hkv, b.max_ctx, b.n_seq, b.max_new);
   a.po = ws;
   a.pml = ws + (size_t)b.rows * b.n_heads * a.splits * HD;
   a.by_g = divisor(a.G);
@@ -756,7 +832,9 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   const int64_t wgs = (int64_t)a.units * a.splits * Hkv;
   if (std::max(wgs, attention_join_wgs(b, a.splits)) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads
   if constexpr (sizeof(T) == 2)
-    if (tile) kv4_tile_kernel<T, HD><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
+    if (tile)
+      rt == 256 ? kv4_tile_kernel<T, HD, 8><<<(unsigned)wgs, 512, 0, s>>>(q, out, a)
+                : kv4_tile_kernel<T, HD, 4><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
   if (!tile) kv4_rows_kernel<T, HD, 4><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
   if (a.splits > 1) launch_attention_join<T>(out, b, a.splits, a.sblk, a.po, a.pml, s);
   return true;
