@@ -217,7 +217,7 @@ struct Kv4Read {
 };
 template <typename T>
 void launch_kv4_read(const Kv4Read &a, T *k, T *v, hipStream_t s);
-size_t kv4_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_heads, int head_dim, int max_ctx);
+size_t kv4_attention_ws_bytes(bool decode, int rows, int n_heads, int head_dim, int max_ctx);
 // False, with nothing launched, where the sizes need more workgroups than a launch may have.
 template <typename T>
 bool launch_kv4_attention(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s);

@@ -102,14 +102,22 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
   const int ctx = row_live(row) ? row_ctx(a.b, seq, row.t) : 0;
   // keys that every row of the tile sees; rows that see nothing get zeros at the end
   const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
-  // lane i: block id of entry e0 + i (an item has at most 64), -1 for none
-  int id = -1;
-  if (e0 + lane < e1 && e0 + lane < a.b.kv.max_blocks) {
-    id = a.b.kv.block_table[(int64_t)slot * a.b.kv.max_blocks + e0 + lane];
-    if (id >= a.b.kv.n_blocks) id = -1;
-  }
-  constexpr uint64_t every = NW == 1 ? ~0ull : ~0ull / ((1ull << NW) - 1);  // every NW-th
-  uint64_t left = __ballot(id >= 0) & (every << wave);
+  // Lane i: block id of entry win + i, -1 for none; left: those of them that are
+  // there and this wave's still to take, every NW-th.
+  int win = e0 - 64, id = -1;
+  uint64_t left = 0;
+  auto more = [&]() __attribute__((always_inline)) {
+    while (!left && win + 64 < e1) {
+      win += 64;
+      id = -1;
+      if (win + lane < e1 && win + lane < a.b.kv.max_blocks) {
+        id = a.b.kv.block_table[(int64_t)slot * a.b.kv.max_blocks + win + lane];
+        if (id >= a.b.kv.n_blocks) id = -1;
+      }
+      left = __ballot(id >= 0) & (~0ull / ((1ull << NW) - 1) << wave);
+    }
+    return left != 0;
+  };
 
   char *ks = lds + wave * F::BYTES, *vs = ks + PART;
   const uint32_t kl = lds_addr(ks), vl = kl + PART;
@@ -117,8 +125,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
   // bank conflicts.  Pieces past the last key repeat the last one before it.
   constexpr int KP = HD / 32;  // 16-byte pieces of a K row
   auto swz = [](int key) __attribute__((always_inline)) { return (key >> 3) & (KP - 1); };
-  auto copy = [&](int i, bool is_k) __attribute__((always_inline)) {
-    const int keys = min(KV_BLOCK, top - (e0 + i) * KV_BLOCK);
+  auto copy = [&](int i, bool is_k) __attribute__((always_inline)) {  // of entry win + i
+    const int keys = min(KV_BLOCK, top - (win + i) * KV_BLOCK);
     const char *src = (const char *)a.b.kv.k +
                       ((int64_t)__builtin_amdgcn_readlane(id, i) * Hkv + g) * F::BYTES + (is_k ? 0 : PART);
     const uint32_t dst = is_k ? kl : vl;
@@ -165,16 +173,18 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
   kat = (kat ^ ((r16 >> 2) & (KP - 1)) * 16) + (J == 4 ? 0 : (quad & 1) * 8);
   int skat = F::k_scale(8 * quad, 0), vat = F::v_word(8 * quad, J == 4 ? r16 : r16 >> 1), svat = F::v_scale(8 * quad, 0);
   asm volatile("" : "+v"(kat), "+v"(skat), "+v"(vat), "+v"(svat));
-  int i = left ? __builtin_ctzll(left) : 0;
-  if (left) {
+  int i = 0;
+  bool go = more();
+  if (go) {
+    i = __builtin_ctzll(left);
     copy(i, true);
     copy(i, false);
   }
-  while (left) {
-    const int base = (e0 + i) * KV_BLOCK;
+  while (go) {
+    const int base = (win + i) * KV_BLOCK;
     left &= left - 1;
-    const bool more = left != 0;
-    const int next = more ? __builtin_ctzll(left) : 0;
+    go = more();
+    i = go ? __builtin_ctzll(left) : 0;  // the next one
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");  // K is there, V may not be
     float s[4][4];  // key 16 t + 8 (lane's quad) .. as p below: 32 (t / 2) + 8 quad + 4 (t % 2) + e
 #pragma unroll
@@ -210,7 +220,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
       asm volatile("" : "+v"(s[t][0]), "+v"(s[t][1]), "+v"(s[t][2]), "+v"(s[t][3]));  // products end here
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
-    if (more) copy(next, true);
+    if (go) copy(i, true);
     const int end = min(KV_BLOCK, ctx - base) - 8 * quad;  // the row's keys, from the lane's first one on: those below
     const bool partly = base + KV_BLOCK > ctx_lo;
     if (partly) {
@@ -230,7 +240,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
     if constexpr (!WIDE) {
       // weights times scales stay within fp16's range for values of any size: the
       // weights are taken by 2^ex, above the largest of the scales so far (of keys that a row of the tile sees)
-      if (more)
+      if (go)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND + FULL) : "memory");  // V's scales are there
       else
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(FULL) : "memory");
@@ -268,7 +278,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
         s[t][y] = __builtin_amdgcn_exp2f(fmaf(s[t][y] - m0, c2, by));
         sum += s[t][y];
       }
-    if (more)
+    if (go)
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND) : "memory");  // V is there
     else
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -338,8 +348,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
-    if (more) copy(next, false);
-    i = next;
+    if (go) copy(i, false);
   }
   const float back = WIDE ? 1.f : __builtin_amdgcn_ldexpf(1.f, ex);
   sum = quads_sum(sum) * back;
@@ -407,13 +416,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 // rows that see the place get NaN in the group's dims afterwards.
 constexpr float KV4_LAZY = 8.f;
 constexpr float KV4_LARGE = 64.f;  // base-2 score up to which the rounded mc is within 2^-19: weights within 1.3e-6
-template <typename T, int HD, int QW>
-__global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) void kv4_tile_kernel(
+template <typename T, int HD>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv4_tile_kernel(
     const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef Kv4<HD> F;
   typedef f16x8_t v8;
   typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
-  constexpr int RT = QW * 32;          // rows, QW waves
+  constexpr int RT = 128;
   constexpr int J = F::J, KS = HD / 16, NT = HD / 32;
   constexpr int CK = HD / 8;           // 16-byte pieces of a K row
   constexpr int PB = 64 * HD * 2, STAGE = 2 * PB;
@@ -452,9 +461,8 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     }
   };
   // This thread's share of a block: K row kr, octets ki of its groups; V word vw of positions 4 vq ..
-  // (of eight waves, four take K and four V)
-  const int kr = (tid >> 2) & 63, ki = tid & 3, vq = tid & 15, vw = (tid >> 4) & 15;
-  const bool has_k = QW == 4 || wave < 4, has_v = (QW == 4 || wave >= 4) && (HD == 128 || vw < HD / 8);
+  const int kr = tid >> 2, ki = tid & 3, vq = tid & 15, vw = tid >> 4;
+  const bool has_v = HD == 128 || vw < HD / 8;
   const uint32_t k_off = F::k_row(kr) + 4 * J * ki, ks_off = F::k_scale(kr, 0), v_off = F::v_word(4 * vq, vw),
                  vs_off = 8 * vq;
   words_t kc;
@@ -474,7 +482,7 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   // Loads of a block that is not there are left out: what the registers hold
   // then goes into a stage that is not read.
   auto load_k = [&](int id) __attribute__((always_inline)) {
-    if (id < 0 || !has_k) return;
+    if (id < 0) return;
     const char *src = head_of(id);
     kc = *(const words_t *)(src + k_off);
     if constexpr (J == 4)
@@ -523,17 +531,14 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   // The loaded block's values into a stage (where there is none, what the
   // registers hold: that stage is not read).
   auto fill_k = [&](int stage, int j) __attribute__((always_inline)) {  // group j
-    char *ks = lds + stage * STAGE;
-    if (has_k) {
-      const half2_t s = {ksc[j], ksc[j]};
-      const half2_t y[4] = {__builtin_bit_cast(half2_t, kv4_pair16<f16_t, 0>(kc[j])) * s,
-                            __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 1>(kc[j])) * s,
-                            __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 2>(kc[j])) * s,
-                            __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 3>(kc[j])) * s};
-      const u32x4_tt v = {__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]),
-                          __builtin_bit_cast(uint32_t, y[2]), __builtin_bit_cast(uint32_t, y[3])};
-      *(u32x4_tt *)(ks + kr * HD * 2 + (((4 * j + ki) ^ swz(kr)) * 16)) = v;
-    }
+    const half2_t s = {ksc[j], ksc[j]};
+    const half2_t y[4] = {__builtin_bit_cast(half2_t, kv4_pair16<f16_t, 0>(kc[j])) * s,
+                          __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 1>(kc[j])) * s,
+                          __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 2>(kc[j])) * s,
+                          __builtin_bit_cast(half2_t, kv4_pair16<f16_t, 3>(kc[j])) * s};
+    const u32x4_tt v = {__builtin_bit_cast(uint32_t, y[0]), __builtin_bit_cast(uint32_t, y[1]),
+                        __builtin_bit_cast(uint32_t, y[2]), __builtin_bit_cast(uint32_t, y[3])};
+    *(u32x4_tt *)(lds + stage * STAGE + kr * HD * 2 + (((4 * j + ki) ^ swz(kr)) * 16)) = v;
   };
   auto pair_v = [&]() __attribute__((always_inline)) {  // vc: bytes of even dims, of odd ones, each of two positions
 #pragma unroll
@@ -648,6 +653,15 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
           if (k % 4 == 3) fill_k(stage ^ 1, t * (KS / 4) + k / 4);
         }
       }
+      // K's fragments four ahead of their MFMAs, which else wait for LDS one by one
+      // (three long prompts 720 us)
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * KS - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x8, 4, 0);
       load_k(next);  // a part of a walk's step ahead of their use, like V's below
       if (e + 1 < e1) check(e + 1, stage ^ 1);
       pair_v();
@@ -758,60 +772,90 @@ __global__ __launch_bounds__(QW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   }
   // Through LDS, so that a row's dims leave as one run of bytes: 16-byte pieces
   // XOR-swizzled by the row, the wave's 32 rows in a place of its own.
-  // (of eight waves, half of the dims at a time)
-  constexpr int TT = NT * 4 / QW, LR = TT * 8, RI = 64 / LR;  // 32-dim tiles, lanes of a row, rows of a store
-  char *own = lds + wave * 32 * LR * 16;
+  constexpr int LR = HD / 4, RI = 64 / LR;  // lanes of a row, rows of a store
+  char *own = lds + wave * 32 * HD * 4;
   if (live && hh == 0) *(float2 *)(a.pml + (row * a.splits + part) * 2) = make_float2(mx * unit, sum);
   const uint32_t rows_live = e0 < e1 ? (uint32_t)__ballot(live) : 0;  // the join skips o of empty parts
 #pragma unroll
-  for (int t0 = 0; t0 < NT; t0 += TT) {
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; r += 4) {
-        const int piece = t * 8 + r / 2 + hh;
-        *(float4 *)(own + l32 * LR * 16 + ((piece ^ (l32 % LR)) * 16)) =
-            make_float4(o[t0 + t][r], o[t0 + t][r + 1], o[t0 + t][r + 2], o[t0 + t][r + 3]);
-      }
-#pragma unroll 4
-    for (int i = 0; i < 32 / RI; ++i) {
-      const int x = i * RI + lane / LR;
-      const float4 v = *(const float4 *)(own + x * LR * 16 + (((lane % LR) ^ (x % LR)) * 16));
-      const PrefixRow y = packed_row(a, start, r0, wave * 32 + x, g);
-      if (rows_live >> x & 1)
-        *(float4 *)(a.po + (((int64_t)y.token * Hq + y.head) * a.splits + part) * HD + t0 * 32 + lane % LR * 4) = v;
+    for (int r = 0; r < 16; r += 4) {
+      const int piece = t * 8 + r / 2 + hh;
+      *(float4 *)(own + l32 * HD * 4 + ((piece ^ (l32 % LR)) * 16)) =
+          make_float4(o[t][r], o[t][r + 1], o[t][r + 2], o[t][r + 3]);
     }
+#pragma unroll 4
+  for (int i = 0; i < 32 / RI; ++i) {
+    const int x = i * RI + lane / LR;
+    const float4 v = *(const float4 *)(own + x * HD * 4 + (((lane % LR) ^ (x % LR)) * 16));
+    const PrefixRow y = packed_row(a, start, r0, wave * 32 + x, g);
+    if (rows_live >> x & 1)
+      *(float4 *)(a.po + (((int64_t)y.token * Hq + y.head) * a.splits + part) * HD + lane % LR * 4) = v;
   }
 }
 
 // ------------------------------------------------------------------ plan
 
-// Blocks of a split.
-static int kv4_split(int64_t pairs, int blocks) {
-  const int want = (int)std::max<int64_t>(1, 1024 / std::max<int64_t>(1, std::min<int64_t>(pairs, 1024)));
-  return std::min(std::max(ceil_div(blocks, want), std::min(blocks, 8)), 24);
+// 16-row items.  A workgroup's waves share its blocks, so a row (or 16 packed ones)
+// and KV head, a "pair", is one item of all blocks where there are pairs enough,
+// and with few blocks, for which a second launch costs more than it brings;
+// eight waves share it then while that fills the GPU once.  Else items of a few
+// blocks, about 1,024 of them, at most 24 blocks each, so that long rows end with
+// the others.  (Graphs of calls, 8B heads unless said, blocks of an item with four
+// waves, "all" with eight: one row of 300 tokens 8 8.3 us, all 7.4; 4 rows of 613 4
+// 8.8, all 10.6; one of 2,000 4 9.2, 8 10.5, 16 14.7; one of 8,000 4 10.1, 8 12.0;
+// 16 of 1,000 4 16.3, 8 15.2, 16 17.0; 32 of 600, 256 pairs, 4 16.4, all 15.3; 64 of
+// 1,000, 512 pairs, 16 28.8, 32 31.1, all 28.0; 64 of 7,000 8 141, 16 132, 32 131, 64
+// 139; 13B 64 of 1,200, 2,560 pairs, 8 95.8, 16 91.5, all with four 87.2, with eight
+// 91.3.)
+struct Kv4Split {
+  int blocks, waves;
+};
+static Kv4Split kv4_rows_split(int64_t pairs, int blocks) {
+  if (blocks <= 12 || (blocks <= 40 && pairs >= 256) || pairs >= 2048) return {blocks, pairs <= 512 ? 8 : 4};
+  const int even = (int)std::min<int64_t>((blocks * std::min<int64_t>(pairs, 1024) + 1023) / 1024, 24);
+  return {std::min(blocks, std::max(even, pairs < 64 ? 4 : 8)), 4};
 }
 
-static void kv4_plan(Kv4Args &a, bool decode, int rt, int rows, int n_heads, int n_kv_heads, int max_ctx, int n_seq,
-                     int max_new) {
-  a.G = n_heads / n_kv_heads;
-  const int live = std::min(n_seq, rows);
-  a.units = decode ? rows * ceil_div(a.G, 16)
-                   : (int)std::min((int64_t)live * ceil_div((int64_t)std::min(max_new, rows) * a.G, rt),
-                                   (int64_t)rows * a.G / rt + live);
-  const int blocks = ceil_div(max_ctx, KV_BLOCK);
-  if (rt > 16) {
-    const int64_t items = (int64_t)a.units * n_kv_heads;
-    a.sblk = items >= 256 ? blocks : std::max(ceil_div(blocks, 512 / items), std::min(blocks, 8));
-  } else {
-    a.sblk = kv4_split((int64_t)a.units * n_kv_heads, blocks);
+// Prompts' tiles of 128 rows: blocks of a split, for `items` tiles and KV heads.
+// In us: a block takes 1.45 alone on a CU, 2.45 with a second tile beside it, a
+// tile 4 more, and the join 3 and 1.6e-4 a row, head and part (more past four parts).
+// Contexts are taken to be 0.6 of the longest.  Fitted to (new + cached tokens, graphs
+// of calls): 8B 16 x 40 + 1,500 all blocks 76.5, 24 63.7, 16 56.7, 12 70.2; 4 x 100 +
+// 3,000 all 93, 24 52.7, 16 50.6, 8 56; 8 x 200 + 1,000 all 64.7, 24 78; 1 x 2,000 all
+// 58.6, 16 79; 70B 1 x 100 + 2,000 all 52.5, 16 35.4, 8 27.9, 4 28.4; 7B 1 x 547 all
+// 18.8, 6 26.2; 13B 4 x 100 + 1,000 all 50.8, 16 48.5, 12 42.7, 8 46.6.
+static int kv4_tile_split(int64_t items, int blocks, int64_t rows_heads) {
+  int best = blocks;
+  double least = 0;
+  for (int s = 1; s <= ceil_div(blocks, 4) && (s == 1 || items * s <= 1024); ++s) {
+    const int n = ceil_div(blocks, s);
+    if (ceil_div(blocks, n) != s) continue;
+    const double work = items * (double)blocks * 0.6 * 2.45 / 512;
+    const double t = 4 + std::max(n * 1.45, work + n * 0.75) +
+                     (s == 1 ? 0 : 3 + rows_heads * s * 1.6e-4 + (s > 4 ? 5 : 0));
+    if (s == 1 || t < least) {
+      least = t;
+      best = n;
+    }
   }
-  a.splits = ceil_div(blocks, a.sblk);
+  return best;
 }
 
-size_t kv4_attention_ws_bytes(bool, int rows, int n_heads, int, int head_dim, int max_ctx) {
-  const int64_t blocks = ceil_div(max_ctx, KV_BLOCK);
-  return (size_t)rows * n_heads * ceil_div(blocks, 8) * (head_dim + 2) * sizeof(float);
+// Partials (row, head and part) that a plan may have, ascending in rows and contexts
+// so that a workspace for a batch's limits serves its smaller steps.  Plans stay
+// within it by themselves but for batches with far more rows than their sequences
+// can have: 16-row items split only below 2,048 pairs, 32,768 rows and heads, into
+// parts of 24 blocks, or smaller ones (of four at least) up to about 1,024 items;
+// tiles up to 1,024 items of 128 rows.
+static int64_t kv4_partials(bool decode, int64_t rows_heads, int blocks) {
+  const int64_t quarter = rows_heads * ((blocks + 3) / 4);
+  return std::max(std::min<int64_t>(rows_heads, 32768) * ((blocks + 23) / 24),
+                  std::min<int64_t>(quarter, decode ? 32768 : 131072));
+}
+size_t kv4_attention_ws_bytes(bool decode, int rows, int n_heads, int head_dim, int max_ctx) {
+  return (size_t)kv4_partials(decode, (int64_t)rows * n_heads, ceil_div(max_ctx, KV_BLOCK)) * (head_dim + 2) *
+         sizeof(float);
 }
 
 template <typename T, int HD>
@@ -819,23 +863,42 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   Kv4Args a{};
   a.b = b;
   const bool decode = !b.seq_start;
-  const int Hkv = b.kv.n_kv_heads;
-  const bool tile = sizeof(T) == 2 && !decode && (int64_t)std::min(b.max_new, b.rows) * (b.n_heads / Hkv) > 32;
-  const int rt = !tile ? 16 : (int64_t)b.rows * (b.n_heads / Hkv) * Hkv >= 256 * 256 ? 256 : 128;
-  kv4_plan(a, decode, rt, b.rows, b.n_heads, Hkv, b.max_ctx, b.n_seq, b.max_new);
+  const int Hkv = b.kv.n_kv_heads, blocks = ceil_div(b.max_ctx, KV_BLOCK), live = std::min(b.n_seq, b.rows);
+  a.G = b.n_heads / Hkv;
+  const auto units = [&](int rt) {  // row tiles at most, of rt rows
+    if (decode) return b.rows * ceil_div(a.G, rt);
+    return (int)std::min((int64_t)live * ceil_div((int64_t)std::min(b.max_new, b.rows) * a.G, rt),
+                         (int64_t)b.rows * a.G / rt + live);
+  };
+  // Few rows over more than two blocks take 16-row items, as fp32 does (new + cached
+  // tokens, 16-row items against tiles, at their best splits: 8B 30 + 2,000, 64 pairs,
+  // 13.2 us and 15.5, 100 + 500, 200 pairs, 12.7 and 14.8, 30 alone 7.9 and 7.0; 70B
+  // 16 + 1,000, 64, 13.4 and 15.6, 100 + 2,000, 400, 31.8 and 27.9; 7B 547, 1,120, 20.2
+  // and 18.8).
+  const bool tile = sizeof(T) == 2 && !decode && ((int64_t)units(16) * Hkv > 256 || blocks <= 2);
+  a.units = units(tile ? 128 : 16);
+  const int64_t pairs = (int64_t)a.units * Hkv;
+  const Kv4Split split = tile ? Kv4Split{kv4_tile_split(pairs, blocks, (int64_t)b.rows * b.n_heads), 4}
+                              : kv4_rows_split(pairs, blocks);
+  const int64_t most = std::max<int64_t>(1, kv4_partials(decode, (int64_t)b.rows * b.n_heads, blocks) /
+                                                ((int64_t)b.rows * b.n_heads));
+  a.sblk = std::max(split.blocks, ceil_div(blocks, most));
+  a.splits = ceil_div(blocks, a.sblk);
   a.po = ws;
   a.pml = ws + (size_t)b.rows * b.n_heads * a.splits * HD;
   a.by_g = divisor(a.G);
   a.by_hkv = divisor(Hkv);
   a.by_units = divisor(a.units);
   a.by_per = divisor(ceil_div(a.G, 16));
-  const int64_t wgs = (int64_t)a.units * a.splits * Hkv;
+  const int64_t wgs = pairs * a.splits;
   if (std::max(wgs, attention_join_wgs(b, a.splits)) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads
+  const unsigned grid = (unsigned)wgs;
   if constexpr (sizeof(T) == 2)
-    if (tile)
-      rt == 256 ? kv4_tile_kernel<T, HD, 8><<<(unsigned)wgs, 512, 0, s>>>(q, out, a)
-                : kv4_tile_kernel<T, HD, 4><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
-  if (!tile) kv4_rows_kernel<T, HD, 4><<<(unsigned)wgs, 256, 0, s>>>(q, out, a);
+    if (tile) kv4_tile_kernel<T, HD><<<grid, 256, 0, s>>>(q, out, a);
+  if (!tile && split.waves == 8)
+    kv4_rows_kernel<T, HD, 8><<<grid, 512, 0, s>>>(q, out, a);
+  else if (!tile)
+    kv4_rows_kernel<T, HD, 4><<<grid, 256, 0, s>>>(q, out, a);
   if (a.splits > 1) launch_attention_join<T>(out, b, a.splits, a.sblk, a.po, a.pml, s);
   return true;
 }

@@ -389,13 +389,13 @@ extern "C" int lp_op_kv4_read(int32_t dtype, const void *cache, int64_t n_blocks
 extern "C" size_t lp_op_kv4_decode_attention_ws_bytes(int32_t M, int32_t n_heads, int32_t n_kv_heads,
                                                       int32_t head_dim, int32_t max_ctx) {
   if (!prefix_sizes(M, n_heads, n_kv_heads, head_dim, 0, max_ctx)) return 0;
-  return kv4_attention_ws_bytes(true, M, n_heads, n_kv_heads, head_dim, max_ctx);
+  return kv4_attention_ws_bytes(true, M, n_heads, head_dim, max_ctx);
 }
 
 extern "C" size_t lp_op_kv4_prefill_attention_ws_bytes(int32_t rows, int32_t n_heads, int32_t n_kv_heads,
                                                        int32_t head_dim, int32_t max_ctx) {
   if (!prefix_sizes(rows, n_heads, n_kv_heads, head_dim, 0, max_ctx)) return 0;
-  return kv4_attention_ws_bytes(false, rows, n_heads, n_kv_heads, head_dim, max_ctx);
+  return kv4_attention_ws_bytes(false, rows, n_heads, head_dim, max_ctx);
 }
 
 // The checks that both phases share; `b` is complete but for them.
@@ -413,8 +413,7 @@ static int kv4_attention(int32_t dtype, const void *q, void *out, const PrefixBa
         "kv4 attention: pointers");
   OPCHK(aligned16(q) && aligned16(out) && aligned16(b.kv.k) && aligned16(ws),
         "kv4 attention: q, out, the cache and ws start on 16 bytes");
-  const size_t need =
-      kv4_attention_ws_bytes(decode, b.rows, b.n_heads, b.kv.n_kv_heads, b.kv.head_dim, b.max_ctx);
+  const size_t need = kv4_attention_ws_bytes(decode, b.rows, b.n_heads, b.kv.head_dim, b.max_ctx);
   OPCHK(need == 0 || (ws && ws_bytes >= need), "kv4 attention: ws");
   hipStream_t s = (hipStream_t)stream;
   bool fits;
