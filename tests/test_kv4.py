@@ -545,3 +545,654 @@ def test_a_service_from_projection_to_read_back(dtype, Hq, Hkv, hd):
         ref, tol = b.reference(qj, j, [int(cached[j]) - 1])
         tol16 = tol + 2 * UNIT[dtype] * np.abs(V[j]).max() if dtype != "f32" else tol
         assert np.all(np.abs(again[j:j + 1].double().cpu().numpy() - ref) <= tol16)
+
+
+# ------------------------------------------------------------------ attention: what may be in the data
+
+# heads and rows of a prompt that take 16-row items, and that take tiles (16-bit types)
+FEW, MANY = (8, 2), (32, 16)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,hd", [("f16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("heads", [FEW, MANY])
+def test_missing_blocks_slots_and_positions(dtype, hd, heads):
+    """Missing blocks (-1 and past the pool) are left out of a row's keys; slots
+    outside the table and negative positions give zeros; contexts are clamped to max_ctx."""
+    rng = np.random.default_rng(5)
+    Hq, Hkv = heads
+    b = Batch(rng, dtype, Hkv, hd, [500, 300, 260, 210, 150])
+    b.table[b.slot[0], [1, 5]] = -1, b.n_blocks
+    b.table[b.slot[1], 3:] = -7
+    b.table[b.slot[3], :] = -1
+    rows = [(0, 499), (1, 299), (2, 259), (3, -1), (3, 209), (4, 149), (2, 255)]
+    q = values(rng, (len(rows), Hq, hd), dtype)
+    slots = [b.slot[j] for j, _ in rows]
+    slots[6] = b.table.shape[0]
+    got = run_decode(b, q, rows, Hq, max_ctx=490, slots=slots)
+    gone = {0: [(64, 128), (320, 384)], 1: [(192, 300)], 2: [], 3: [(0, 210)], 4: []}
+    seqs = [(0, 370, 130), (1, 200, 95), (4, 140, 10)]
+    q2 = values(rng, (sum(x for _, _, x in seqs), Hq, hd), dtype)
+    got2 = run_prefill(b, q2, seqs, Hq, max_ctx=490, slots=[b.slot[0], b.slot[1], -1])
+
+    def check(qr, have, j, p):
+        keep = np.array([i for i in range(min(p + 1, 490)) if not any(lo <= i < hi for lo, hi in gone[j])], dtype=int)
+        if not len(keep):
+            assert np.all(have == 0), (j, p)
+            return
+        K, V = b.K[j][keep], b.V[j][keep]
+        args = ([p], np.arange(len(keep)), Hkv)
+        ref, mag = (T.attention(qr, K, v, *args) for v in (V, np.abs(V)))
+        assert np.all(np.abs(have - ref) <= bound(dtype, qr, K, V, ref, mag)), (j, p)
+
+    for m, (j, p) in enumerate(rows):
+        if m in (3, 6):
+            assert np.all(got[m] == 0)
+        else:
+            check(q[m:m + 1], got[m:m + 1], j, p)
+    assert np.all(got2[225:] == 0)
+    for r in range(0, 225, 3):
+        j, p = (0, 370 + r) if r < 130 else (1, 200 + r - 130)
+        check(q2[r:r + 1], got2[r:r + 1], j, p)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,hd", [("f16", 128), ("bf16", 64), ("f32", 64), ("bf16", 128)])
+@pytest.mark.parametrize("heads", [FEW, MANY])
+def test_nan_groups_reach_the_rows_that_see_them(dtype, hd, heads):
+    """A group that held an infinity reads as NaN: rows before its position keep
+    their results to the bit, those from there on get NaN, of K in all dims of
+    its head, of V in the group's dims alone."""
+    rng = np.random.default_rng(6)
+    Hq, Hkv = heads
+    G, n, bad = Hq // Hkv, 190, 107
+    b = Batch(rng, dtype, Hkv, hd, [n, 140])
+    q = values(rng, (n + 40, Hq, hd), dtype)
+    seqs = [(0, 0, n), (1, 100, 40)]
+    clean = run_prefill(b, q, seqs, Hq)
+    check_prefill(b, q, clean, seqs)
+    kb, vb, half, ks, vs = byte_tables(hd)
+    blk, p = b.bytes[b.table[b.slot[0], bad // 64]], bad % 64
+    blk[0, [ks[p, 1], ks[p, 1] + 1]] = 0x00, 0x7E
+    blk[1, [vs[p, 1], vs[p, 1] + 1]] = 0x00, 0x7E
+    got = run_prefill(b, q, seqs, Hq)
+    dec = run_decode(b, q[:3], [(0, bad - 1), (0, bad), (0, n - 1)], Hq)
+    assert np.array_equal(got[:bad], clean[:bad]) and np.array_equal(got[n:], clean[n:])
+    ref, tol = b.reference(q[:1], 0, [bad - 1])
+    assert np.all(np.abs(dec[:1] - ref) <= tol)
+    keep = np.arange(hd) // 32 != 1
+    for rows, was in ((got[bad:n], clean[bad:n]), (dec[1:], None)):
+        assert np.isnan(rows[:, :G]).all() and np.isnan(rows[:, G:2 * G][..., ~keep]).all()
+        assert np.isfinite(rows[:, 2 * G:]).all() and np.isfinite(rows[:, G:2 * G][..., keep]).all()
+        if was is not None:
+            assert np.array_equal(rows[:, 2 * G:], was[:, 2 * G:])
+            assert np.array_equal(rows[:, G:2 * G][..., keep], was[:, G:2 * G][..., keep])
+
+
+@gpu
+@pytest.mark.parametrize("dtype,lo,hi", [("f16", 4, 30), ("bf16", 4, 90), ("f32", 4, 90)])
+@pytest.mark.parametrize("many", [False, True])
+def test_scores_of_any_size(dtype, lo, hi, many):
+    """Scores from 2^lo to 2^hi, one size a head, each exact in fp32: the weights
+    are right whatever the size, in decode, in 16-row items and in tiles."""
+    rng = np.random.default_rng(hi)
+    Hq = Hkv = 16 if many else 8
+    hd, ctx = 64, [131, 200, 420, 130]
+    b = Batch(rng, dtype, Hkv, hd, ctx)
+    e = np.linspace(lo, hi, Hkv).astype(int)
+    a = np.clip(e - 14, -8, 14 if dtype == "f16" else 80)     # q = 2^a, k = 6 m 2^(e - a - 14): 64 dims add 6 bits
+    for j, c in enumerate(ctx):
+        m = rng.integers(32, 64, (c, Hkv)) * rng.choice([-1.0, 1.0], (c, Hkv))
+        k = np.repeat((6 * m * np.exp2(e - a - 14))[:, :, None], hd, axis=2)
+        code = quantise(k)
+        assert np.array_equal(held(*code), k)
+        b.K[j] = k
+        for p in range(c):
+            v = quantise(b.V[j][p])
+            b.store(b.slot[j], p, [x[p] for x in code], v)
+            b.V[j][p] = held(*v)
+    ones = lambda n: np.broadcast_to(np.exp2(a)[None, :, None], (n, Hq, hd)).copy()
+    got = run_decode(b, ones(4), [(j, c - 1) for j, c in enumerate(ctx)], Hq)
+    seqs = [(j, c - 100, 100) for j, c in enumerate(ctx)]
+    pre = run_prefill(b, ones(400), seqs, Hq)
+    u = UNIT[dtype]
+
+    def check(have, j, p):
+        args = ([p], np.arange(p + 1), Hkv)
+        ref, mag = (T.attention(ones(1), b.K[j][:p + 1], v[:p + 1], *args) for v in (b.V[j], np.abs(b.V[j])))
+        # the scores are exact: only weights (times scales), sums and the result are rounded; the scale 1/8 is
+        # exact, its base-2 factor is not: 2^-23 of a score's distance from the largest, which weights that are not
+        # yet 0 keep below 2^7
+        tol = ((p + 97) * 2.0 ** -24 + 2.0 ** -15) * mag + 2.0 ** -24
+        if dtype != "f32":
+            tol = tol + (2.0 ** -11 * mag + u * np.abs(ref)) * 1.02 + (p + 1) * 2.0 ** -24 * np.abs(b.V[j]).max()
+        else:
+            tol = tol + 2.0 ** -24 * np.abs(ref)
+        assert np.all(np.abs(have - ref) <= tol), (j, p, (np.abs(have - ref) / tol).max())
+
+    for j, c in enumerate(ctx):
+        check(got[j:j + 1], j, c - 1)
+        for i in (0, 1, 50, 99):
+            check(pre[100 * j + i:100 * j + i + 1], j, c - 100 + i)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,hd", [("f16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("heads", [FEW, MANY])
+@pytest.mark.parametrize("vscale", [2.0 ** -21, 1e-4, 9000.0])
+def test_values_of_any_size(dtype, hd, heads, vscale):
+    """V near the least numbers held and near the largest, and of sizes that differ from place to place."""
+    rng = np.random.default_rng(hd)
+    Hq, Hkv = heads
+    ctx = [200, 77]
+    spread = np.exp2(rng.integers(-4, 1, (200, 1, 1)))
+    b = Batch(rng, dtype, Hkv, hd, ctx)
+    for j, c in enumerate(ctx):
+        v = quantise(rng.standard_normal((c, Hkv, hd)) * vscale * spread[:c])
+        b.V[j] = held(*v)
+        k = quantise(b.K[j])
+        b.K[j] = held(*k)
+        for p in range(c):
+            b.store(b.slot[j], p, [x[p] for x in k], [x[p] for x in v])
+    q = values(rng, (250, Hq, hd), dtype)
+    seqs = [(0, 0, 200), (1, 27, 50)]
+    got = run_prefill(b, q, seqs, Hq)
+    dec = run_decode(b, q[:2], [(0, 199), (1, 76)], Hq)
+    for have, pairs in ((got, [(r, 0, r) for r in range(200)] + [(200 + r, 1, 27 + r) for r in range(50)]),
+                        (dec, [(0, 0, 199), (1, 1, 76)])):
+        for r, j, p in pairs[::7] + pairs[-1:]:
+            ref, tol = b.reference(q[r:r + 1], j, [p])
+            if dtype == "f16":      # results below 2^-14 are rounded to steps of 2^-24
+                tol = tol + 2.0 ** -25
+            else:
+                tol = tol - 2.0 ** -25 * (dtype == "bf16")
+            assert np.all(np.abs(have[r:r + 1] - ref) <= tol), (j, p)
+
+
+@gpu
+def test_bf16_queries_of_any_size():
+    """Rows of q of very different sizes, and dims of very different sizes in a row, in tiles."""
+    rng = np.random.default_rng(12)
+    Hq, Hkv, hd = 32, 16, 128
+    b = Batch(rng, "bf16", Hkv, hd, [150])
+    q = values(rng, (150, Hq, hd), "bf16")
+    size = np.exp2(rng.integers(-100, 1, (150, Hq, 1)).astype(float))
+    wide = np.exp2(-rng.integers(0, 60, (150, Hq, hd)).astype(float))
+    wide[:, ::2] = 1.0
+    q = torch.from_numpy(q * size * wide).bfloat16().double().numpy()
+    q[7] = 0
+    got = run_prefill(b, q, [(0, 0, 150)], Hq)
+    for r in range(0, 150, 7):      # each row's bound is of its own size
+        for h in range(0, Hq, 5):
+            K, V = b.K[0][:r + 1, h // 2:h // 2 + 1], b.V[0][:r + 1, h // 2:h // 2 + 1]
+            qr = q[r:r + 1, h:h + 1]
+            ref, mag = (T.attention(qr, K, v, [r], np.arange(r + 1), 1) for v in (V, np.abs(V)))
+            assert np.all(np.abs(got[r:r + 1, h:h + 1] - ref) <= bound("bf16", qr, K, V, ref, mag)), (r, h)
+
+
+# ------------------------------------------------------------------ attention: shapes of batches
+
+@gpu
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd,n", [("f16", 8, 2, 128, 40), ("bf16", 16, 16, 64, 45), ("f32", 24, 1, 64, 12),
+                                               ("f16", 40, 1, 128, 33), ("bf16", 10, 5, 128, 300)])
+def test_decode_batches_of_odd_rows(dtype, Hq, Hkv, hd, n):
+    """Rows that share slots, in any order, of any position, with padding between; max_ctx above all contexts."""
+    rng = np.random.default_rng(n)
+    b = Batch(rng, dtype, Hkv, hd, [300, 64, 1, 129])
+    rows = [(m % 4, [-1, 0, 63, 64, 127, 128, 299][m * 3 % 7]) for m in range(n)]
+    rows = [(j, min(p, b.ctx[j] - 1)) for j, p in rows]
+    q = values(rng, (n, Hq, hd), dtype)
+    for top in (300, 320):
+        b.table = np.pad(b.table, ((0, 0), (0, max(0, 5 - b.table.shape[1]))), constant_values=-1)
+        got = run_decode(b, q, rows, Hq, max_ctx=top)
+        for m, (j, p) in enumerate(rows):
+            if p < 0:
+                assert np.all(got[m] == 0)
+            else:
+                ref, tol = b.reference(q[m:m + 1], j, [p])
+                assert np.all(np.abs(got[m:m + 1] - ref) <= tol), m
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", [FEW, MANY])
+def test_prefill_of_a_padded_batch(dtype, heads):
+    """150 places for sequences of which five have rows, the others none and no slot."""
+    rng = np.random.default_rng(150)
+    (Hq, Hkv), hd = heads, 64
+    new = np.zeros(150, int)
+    new[[3, 63, 64, 100, 149]] = [40, 1, 33, 70, 9]
+    b = Batch(rng, dtype, Hkv, hd, [90 + n if n else 0 for n in new])
+    q = values(rng, (new.sum() + 4, Hq, hd), dtype)
+    seqs = [(j, 90, n) for j, n in enumerate(new)]
+    got = run_prefill(b, q, seqs, Hq, tail=4, slots=[s if n else -1 for s, n in zip(b.slot, new)])
+    assert np.all(got[-4:] == 7)
+    check_prefill(b, q, got, seqs)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_prefill_of_few_rows_among_many_empty_places(dtype):
+    """16 rows of five sequences among 2^20 places, as a step of fixed size may hold."""
+    rng = np.random.default_rng(20)
+    Hq, Hkv, hd, places = 32, 8, 128, 1 << 20
+    at, new, ctx = [0, 5, 64, 70000, places - 1], [1, 6, 1, 3, 5], [130, 76, 71, 73, 200]
+    b = Batch(rng, dtype, Hkv, hd, ctx)
+    q = values(rng, (16, Hq, hd), dtype)
+    n, slot, pos = np.zeros(places, int), np.full(places, -1), np.full(places, -1)
+    n[at], slot[at], pos[at] = new, b.slot, np.subtract(ctx, new)
+    start, qd = i32(np.concatenate([[0], np.cumsum(n)])), torch.from_numpy(q).to(TYPES[dtype]).to(DEV)
+    for max_new in (1, 6):                # one row a sequence, and all
+        out = torch.full_like(qd, 7.0)
+        ws = torch.empty(lp.kv4_prefill_attention_ws_bytes(16, Hq, Hkv, hd, 200), dtype=torch.uint8, device=DEV)
+        lp.op_kv4_prefill_attention(qd, out, b.cache(), i32(b.table), start, i32(slot), i32(pos), max_new, 200, ws)
+        got, r = out.double().cpu().numpy(), 0
+        for j, (x, c) in enumerate(zip(new, ctx)):
+            rows = min(x, max_new)
+            ref, tol = b.reference(q[r:r + rows], j, np.arange(c - x, c - x + rows))
+            assert np.all(np.abs(got[r:r + rows] - ref) <= tol), j
+            r += x
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("heads", [FEW, MANY])
+def test_rows_past_max_new_and_outside_the_rows(dtype, heads):
+    """Of a sequence with more rows than max_new the first max_new are right, and
+    those of the next sequences; entries of seq_start below 0 and above the rows
+    count as these; a negative seq_pos is no row with keys."""
+    rng = np.random.default_rng(8)
+    (Hq, Hkv), hd = heads, 64
+    b = Batch(rng, dtype, Hkv, hd, [190, 120, 160])
+    q = values(rng, (112, Hq, hd), dtype)
+    got = run_prefill(b, q, [(0, 100, 90), (1, 100, 20)], Hq, max_new=40, tail=2)
+    for j, r, n in ((0, 0, 40), (1, 90, 20)):
+        ref, tol = b.reference(q[r:r + n], j, np.arange(100, 100 + n))
+        assert np.all(np.abs(got[r:r + n] - ref) <= tol)
+    assert np.all(got[110:] == 7)
+    n = 50
+    for max_new in (n, 100):
+        out = torch.full((n, Hq, hd), 7.0, dtype=TYPES[dtype], device=DEV)
+        ws = torch.empty(max(16, lp.kv4_prefill_attention_ws_bytes(n, Hq, Hkv, hd, 160)), dtype=torch.uint8, device=DEV)
+        lp.op_kv4_prefill_attention(torch.from_numpy(q[:n]).to(TYPES[dtype]).to(DEV), out, b.cache(), i32(b.table),
+                                    i32([-9, 12, 30, 70, 90]), i32([b.slot[0], b.slot[1], b.slot[2], b.slot[0]]),
+                                    i32([100, -3, 120, 5]), max_new, 160, ws)
+        have = out.double().cpu().numpy()
+        for j, r0, r1, p in ((0, 0, 12, 100), (2, 30, 50, 120)):
+            ref, tol = b.reference(q[r0:r1], j, np.arange(p, p + r1 - r0))
+            assert np.all(np.abs(have[r0:r1] - ref) <= tol), j
+        assert np.all(have[12:30] == 0)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_many_rows_that_no_sequence_has(dtype):
+    """A batch of 3,000 rows of which sequences have three: its plan stays inside its workspace."""
+    rng = np.random.default_rng(2)
+    Hq, Hkv, hd = 32, 8, 64
+    b = Batch(rng, dtype, Hkv, hd, [2000, 700])
+    q = values(rng, (3000, Hq, hd), dtype)
+    got = run_prefill(b, q, [(0, 1998, 2), (1, 699, 1)], Hq, start=1, tail=2996)
+    check_prefill(b, q, got, [(0, 1998, 2), (1, 699, 1)], 1)
+    assert np.all(got[0] == 7) and np.all(got[4:] == 7)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_walks_of_more_than_64_blocks(dtype):
+    """All blocks of a row in one item, 71 of them: decode, and prompts in 16-row items (fp32) and tiles (fp16)."""
+    rng = np.random.default_rng(64)
+    hd, c = 64, 4540
+    b = Batch(rng, dtype, 8, hd, [c])
+    rows = [(0, c - 1 - 13 * m) for m in range(260)]
+    q = values(rng, (260, 8, hd), dtype)
+    got = run_decode(b, q, rows, 8)
+    for m in (0, 1, 130, 259):
+        ref, tol = b.reference(q[m:m + 1], 0, [rows[m][1]])
+        assert np.all(np.abs(got[m:m + 1] - ref) <= tol), m
+    seqs = [(0, c - 3 - 11 * m, 3) for m in range(270)]
+    q = values(rng, (810, 8, hd), dtype)
+    got = run_prefill(b, q, seqs, 8)
+    for m in (0, 7, 269):
+        ref, tol = b.reference(q[3 * m:3 * m + 3], 0, list(range(seqs[m][1], seqs[m][1] + 3)))
+        assert np.all(np.abs(got[3 * m:3 * m + 3] - ref) <= tol), m
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_one_row_of_more_than_64_parts(dtype):
+    rng = np.random.default_rng(65)
+    c = 64 * 4 * 66 + 5
+    b = Batch(rng, dtype, 1, 64, [c])
+    q = values(rng, (2, 2, 64), dtype)
+    got = run_decode(b, q, [(0, c - 1), (0, 3000)], 2)
+    for m, p in enumerate((c - 1, 3000)):
+        ref, tol = b.reference(q[m:m + 1], 0, [p])
+        assert np.all(np.abs(got[m:m + 1] - ref) <= tol)
+    got = run_prefill(b, q, [(0, c - 2, 2)], 2)
+    check_prefill(b, q, got, [(0, c - 2, 2)])
+
+
+@gpu
+def test_caches_past_4_gib():
+    """Blocks whose byte offsets pass 32 bits: what a small cache gives, to the bit."""
+    rng = np.random.default_rng(21)
+    Hq, Hkv, hd = 16, 8, 128
+    ctx = [201 + 40 * i for i in range(12)]
+    b = Batch(rng, "f16", Hkv, hd, ctx)
+    n = 59000                     # of 73,728 bytes
+    big = torch.empty(n, Hkv, 72 * hd, dtype=torch.uint8, device=DEV)
+    big[-b.n_blocks:] = b.cache()
+    up = n - b.n_blocks
+    small_cache, small_table = b.cache, b.table
+
+    def call(f, *args):
+        small = f(b, *args)
+        b.cache, b.table, b.n_blocks = lambda: big, np.where(b.table >= 0, b.table + up, -1), n
+        large = f(b, *args)
+        b.cache, b.table, b.n_blocks = small_cache, small_table, n - up
+        assert np.isfinite(small).all() and np.array_equal(small, large)
+
+    q = values(rng, (700, Hq, hd), "f16")
+    call(run_decode, q[:2], [(j, ctx[j] - 1) for j in range(2)], Hq)
+    call(run_decode, q[:144], [(j, ctx[j] - 1) for j in range(12)] * 12, Hq)
+    call(run_prefill, q[:100], [(0, 200, 1), (11, 300, 99)], Hq)
+    call(run_prefill, q[:600], [(j, 100, 50) for j in range(12)], Hq)
+    # append at the last places and read them back, into an ordinary cache past 4 GiB too
+    rows, m = 65, 34000
+    entry = torch.arange(n * 64 - 70, n * 64 - 5, dtype=torch.int64, device=DEV)
+    x = rng.standard_normal((rows, (Hq + 2 * Hkv) * hd)).astype(np.float32)
+    cos, sin = np.ones((4, hd // 2), np.float32), np.zeros((4, hd // 2), np.float32)
+    qd = torch.empty(rows, Hq, hd, dtype=torch.float16, device=DEV)
+    lp.op_kv4_append(torch.from_numpy(x).to(DEV), torch.from_numpy(cos).to(DEV), torch.from_numpy(sin).to(DEV),
+                     i32([1] * rows), entry, qd, big)
+    kc = torch.empty(m, Hkv, 64, hd, dtype=torch.float16, device=DEV)
+    vc = torch.empty(m, Hkv, hd, 64, dtype=torch.float16, device=DEV)
+    to = torch.arange(m * 64 - 66, m * 64 - 1, dtype=torch.int64, device=DEV)
+    lp.op_kv4_read(big, entry, to, kc, vc)
+    torch.cuda.synchronize()
+    h = x.reshape(rows, -1, hd)
+    for r in (0, 1, 63, 64):
+        blk, p = divmod(int(to[r]), 64)
+        assert np.array_equal(kc[blk, :, p].double().cpu().numpy(), held(*quantise(h[r, Hq:Hq + Hkv])))
+        assert np.array_equal(vc[blk, :, :, p].double().cpu().numpy(), held(*quantise(h[r, Hq + Hkv:])))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_read_of_many_contexts(dtype):
+    """Contexts block by block, one after the other in the list, with rows of no
+    entry, a place left out and a context that starts inside a block among them."""
+    rng = np.random.default_rng(44)
+    Hkv, hd, n_blocks = 40, 128, 60
+    cache = noise(rng, n_blocks, Hkv, hd)
+    for lo in (32 * hd, 68 * hd):
+        s = scales(np.abs(rng.standard_normal((n_blocks, Hkv, 2 * hd))))
+        cache[:, :, lo:lo + 4 * hd] = s.astype(np.float16).view(np.uint8)
+    free, src, dst, at = rng.permutation(n_blocks), [], [], 0
+    for c in (130, 64, 1, 300, 63, 192, 129):
+        blocks, free = free[:ceil64(c)], free[ceil64(c):]
+        p = np.arange(c)
+        src += (blocks[p // 64] * 64 + p % 64).tolist() + [-1] * (c % 3)
+        dst += (at + p).tolist() + [-1] * (c % 3)
+        at += ceil64(c) * 64
+    src, dst = np.array(src), np.array(dst)
+    src[200], dst[333] = -1, 1 << 40
+    p = np.arange(70)                     # from the middle of a block to the middle of one
+    src, dst = np.append(src, free[0] * 64 + 5 + p % 50), np.append(dst, at + 9 + p)
+    n_dst = at // 64 + 2
+    kc = torch.full((n_dst, Hkv, 64, hd), 7.0, dtype=TYPES[dtype], device=DEV)
+    vc = torch.full((n_dst, Hkv, hd, 64), 7.0, dtype=TYPES[dtype], device=DEV)
+    lp.op_kv4_read(torch.from_numpy(cache).to(DEV), i64(src), i64(dst), kc, vc)
+    torch.cuda.synchronize()
+    wk, wv = np.full(kc.shape, 7.0), np.full(vc.shape, 7.0)
+    for s, d in zip(src, dst):
+        if 0 <= s and 0 <= d < n_dst * 64:
+            wk[d // 64, :, d % 64], wv[d // 64, :, :, d % 64] = get(cache[s // 64], s % 64)
+    assert np.array_equal(kc.double().cpu().numpy(), wk) and np.array_equal(vc.double().cpu().numpy(), wv)
+
+
+# ------------------------------------------------------------------ graphs and streams
+
+@gpu
+def test_steps_in_captured_graphs():
+    """Append, decode and read-back captured once, a prefill beside them with the
+    same workspace, replayed in turn with eager work between, against eager results."""
+    rng = np.random.default_rng(30)
+    Hq, Hkv, hd, n = 32, 8, 128, 20
+    b = Batch(rng, "f16", Hkv, hd, [960 + i for i in range(n)])
+    cache, table, slot, top, new = b.cache(), i32(b.table), i32(b.slot), 1024, 30
+    qp = torch.from_numpy(values(rng, (n * new, Hq, hd), "f16")).half().to(DEV)
+    x = torch.from_numpy(rng.standard_normal((n, (Hq + 2 * Hkv) * hd)).astype(np.float32)).to(DEV)
+    cos, sin = (torch.from_numpy(t).to(DEV) for t in rope_tables(1100, hd))
+    start, first = i32(np.arange(n + 1) * new), i32([900] * n)
+    pos = [959 + i for i in range(n)]
+    entry = i64([b.table[s, p // 64] * 64 + p % 64 for s, p in zip(b.slot, pos)])
+    pos, to = i32(pos), i64(np.arange(n))
+    ws = torch.empty(max(lp.kv4_decode_attention_ws_bytes(n, Hq, Hkv, hd, top),
+                         lp.kv4_prefill_attention_ws_bytes(n * new, Hq, Hkv, hd, top)), dtype=torch.uint8, device=DEV)
+    qd = torch.zeros(n, Hq, hd, dtype=torch.float16, device=DEV)
+    outs = [torch.zeros_like(qp), torch.zeros_like(qd)]
+    kc = torch.zeros(1, Hkv, 64, hd, dtype=torch.float16, device=DEV)
+    vc = torch.zeros(1, Hkv, hd, 64, dtype=torch.float16, device=DEV)
+
+    def prefill():
+        lp.op_kv4_prefill_attention(qp, outs[0], cache, table, start, slot, first, new, top, ws)
+
+    def decode():
+        lp.op_kv4_append(x, cos, sin, pos, entry, qd, cache)
+        lp.op_kv4_decode_attention(qd, outs[1], cache, table, slot, pos, top, ws)
+        lp.op_kv4_read(cache, entry, to, kc, vc)
+
+    def results():
+        torch.cuda.synchronize()
+        return [t.clone() for t in (*outs, qd, kc, vc, cache)]
+
+    decode()                # the appended rows stay the same from here on
+    prefill()
+    want, graphs = results(), []
+    for f in (prefill, decode):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            f()
+        graphs.append(graph)
+    for _ in range(4):
+        for t in (*outs, qd, kc, vc):
+            t.fill_(9)
+        want_k = want[3].clone()
+        want_k[:, :, n:] = 9
+        want_v = want[4].clone()
+        want_v[..., n:] = 9
+        for k in (0, 1):
+            ws.random_(0, 256)
+            graphs[k].replay()
+        have = results()
+        assert torch.equal(have[0], want[0]) and torch.equal(have[1], want[1]) and torch.equal(have[2], want[2])
+        assert torch.equal(have[3], want_k) and torch.equal(have[4], want_v) and torch.equal(have[5], want[5])
+        assert torch.isfinite(have[0]).all() and torch.isfinite(have[1]).all()
+        torch.ones(1000, device=DEV).sum().item()
+
+
+@gpu
+def test_two_streams_at_once():
+    """The same calls on two streams with workspaces of their own, many times over, give what one gives alone."""
+    rng = np.random.default_rng(3)
+    Hq, Hkv, hd, ctx = 32, 8, 128, [701 + 40 * i for i in range(16)]
+    b = Batch(rng, "f16", Hkv, hd, ctx)
+    q = [torch.from_numpy(values(rng, (16, Hq, hd), "f16")).half().to(DEV) for _ in range(2)]
+    cache, slot, pos, table, top = b.cache(), i32(b.slot), i32([c - 1 for c in ctx]), i32(b.table), max(ctx)
+    nb = lp.kv4_decode_attention_ws_bytes(16, Hq, Hkv, hd, top)
+
+    def call(k, out, ws):
+        lp.op_kv4_decode_attention(q[k], out, cache, table, slot, pos, top, ws)
+
+    wss = [torch.empty(nb, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    alone = [torch.empty_like(q[0]) for _ in range(2)]
+    for k in range(2):
+        call(k, alone[k], wss[k])
+    outs = [[torch.empty_like(q[0]) for _ in range(10)] for _ in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i in range(10):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                call(k, outs[k][i], wss[k])
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(o, alone[k]) for o in outs[k])
+
+
+# ------------------------------------------------------------------ refusals (no GPU is touched)
+
+F16, F32, OK, EINVAL = lp.LP_F16, lp.LP_F32, lp.LP_OK, lp.LP_EINVAL
+A = 1 << 20  # an aligned address that is never read: every call below returns before a launch
+
+
+def test_cache_bytes():
+    f = lp.lib().lp_op_kv4_cache_bytes
+    assert f(7, 8, 128) == 7 * 8 * 9216 and f(1, 1, 64) == 4608 and f(1 << 33, 40, 128) == (1 << 33) * 40 * 9216
+    assert f(0, 8, 128) == f(7, 0, 128) == f(7, 8, 96) == f(-1, 8, 64) == 0
+
+
+def test_append_refusals():
+    f = lp.lib().lp_op_kv4_append
+    names = ("dtype", "qkv", "ld", "cos", "sin", "n_pos", "pos", "entry", "rows", "q", "cache", "n_blocks", "Hq", "Hkv",
+             "hd", "stream")
+    good = [F16, A, 1536, A, A, 100, A, A, 3, A, A, 5, 8, 2, 128, None]
+
+    def call(**bad):
+        return f(*[bad.get(k, v) for k, v in zip(names, good)])
+
+    assert call(rows=0) == OK
+    assert call(rows=0, qkv=None, cos=None, sin=None, pos=None, entry=None, q=None, cache=None) == OK
+    for bad in (dict(dtype=7), dict(ld=1534), dict(ld=1537), dict(n_pos=0), dict(rows=-1), dict(n_blocks=0), dict(Hq=9),
+                dict(Hkv=0), dict(hd=96)):
+        assert call(**bad) == EINVAL, bad
+        assert call(**{"rows": 0, **bad}) == EINVAL, bad
+    for k in ("qkv", "cos", "sin", "pos", "entry", "q", "cache"):
+        assert call(**{k: None}) == EINVAL, k
+    for bad in (dict(qkv=A + 4), dict(cos=A + 4), dict(sin=A + 4), dict(q=A + 8), dict(cache=A + 8), dict(rows=700000)):
+        assert call(**bad) == EINVAL, bad
+
+
+def test_read_refusals():
+    f = lp.lib().lp_op_kv4_read
+    names = ("dtype", "cache", "n_blocks", "src", "dst", "rows", "k", "v", "n_dst", "Hkv", "hd", "stream")
+    good = [F16, A, 5, A, A, 3, A, A, 6, 2, 128, None]
+
+    def call(**bad):
+        return f(*[bad.get(k, v) for k, v in zip(names, good)])
+
+    pointers = ("cache", "src", "dst", "k", "v")
+    assert call(rows=0) == OK and call(rows=0, **dict.fromkeys(pointers)) == OK
+    for bad in (dict(dtype=7), dict(n_blocks=0), dict(rows=-1), dict(n_dst=0), dict(Hkv=0), dict(hd=80),
+                dict(rows=1 << 26)):
+        assert call(**bad) == EINVAL, bad
+    for k in pointers:
+        assert call(**{k: None}) == EINVAL, k
+    for k in ("cache", "k", "v"):
+        assert call(**{k: A + 8}) == EINVAL, k
+
+
+@pytest.mark.parametrize("decode", [True, False])
+def test_attention_refusals(decode):
+    L = lp.lib()
+    f = L.lp_op_kv4_decode_attention if decode else L.lp_op_kv4_prefill_attention
+    size = L.lp_op_kv4_decode_attention_ws_bytes if decode else L.lp_op_kv4_prefill_attention_ws_bytes
+    head = dict(dtype=F16, q=A, out=A, cache=A, n_blocks=50, table=A, n_slots=4, wide=8)
+    mid = dict(slot=A, pos=A, rows=4) if decode else dict(start=A, slot=A, pos=A, n=2, rows=40, max_new=30)
+    tail = dict(Hq=8, Hkv=2, hd=128, max_ctx=500, ws=A, ws_bytes=1 << 40, stream=None)
+    good = {**head, **mid, **tail}
+
+    def call(**bad):
+        return f(*[bad.get(k, v) for k, v in good.items()])
+
+    pointers = [k for k in ("q", "out", "cache", "table", "start", "slot", "pos", "ws") if k in good]
+    assert call(rows=0) == OK and call(**{"rows": 0, **dict.fromkeys(pointers)}) == OK
+    if not decode:
+        assert call(n=0) == OK and call(n=-1) == EINVAL and call(max_new=0) == EINVAL
+    for bad in (dict(dtype=9), dict(rows=-1), dict(n_blocks=0), dict(n_slots=0), dict(wide=0), dict(wide=7), dict(Hq=9),
+                dict(Hkv=0), dict(hd=80), dict(max_ctx=0), dict(max_ctx=(1 << 30) + 1), dict(rows=1 << 28)):
+        assert call(**bad) == EINVAL, bad
+        if "rows" not in bad:
+            assert call(**{"rows": 0, **bad}) == EINVAL, bad
+    for k in pointers:
+        assert call(**{k: None}) == EINVAL, k
+    for k in ("q", "out", "cache", "ws"):
+        assert call(**{k: A + 8}) == EINVAL, k
+    need = size(good["rows"], 8, 2, 128, 500)
+    assert need > 0 and call(ws_bytes=need - 1) == EINVAL
+    assert size(-1, 8, 2, 128, 500) == 0 and size(4, 8, 3, 128, 500) == 0 and size(4, 8, 2, 96, 500) == 0
+    assert "kv4 attention" in L.lp_last_error(None).decode()
+
+
+@pytest.mark.parametrize("decode", [True, False])
+@pytest.mark.parametrize("dtype", [F16, lp.LP_BF16, F32])
+def test_work_past_one_launch_is_refused(decode, dtype):
+    """Sizes within the limits each, whose workgroups together are too many."""
+    L = lp.lib()
+    f = L.lp_op_kv4_decode_attention if decode else L.lp_op_kv4_prefill_attention
+    for rows, Hq, Hkv, ctx in ((1 << 21, 16, 16, 1), (1 << 25, 8, 8, 500), (1 << 29, 1, 1, 64)):
+        seqs = [A, A, rows] if decode else [A, A, A, rows, rows, 1]
+        assert f(dtype, A, A, A, 50, A, 4, 1 << 24, *seqs, Hq, Hkv, 64, ctx, A, 1 << 60, None) == EINVAL, rows
+        assert "launch" in L.lp_last_error(None).decode()
+
+
+@pytest.mark.parametrize("decode", [True, False])
+def test_a_workspace_serves_smaller_steps(decode):
+    """Sizes ascend with rows and contexts."""
+    f = lp.kv4_decode_attention_ws_bytes if decode else lp.kv4_prefill_attention_ws_bytes
+    rng = np.random.default_rng(1)
+    for _ in range(2000):
+        rows, ctx = int(np.exp(rng.uniform(0, 10))), int(np.exp(rng.uniform(0, 12)))
+        Hkv, G = int(rng.integers(1, 41)), int(rng.integers(1, 20))
+        less = f(int(rng.integers(1, rows + 1)), Hkv * G, Hkv, 128, int(rng.integers(1, ctx + 1)))
+        assert 0 < less <= f(rows, Hkv * G, Hkv, 128, ctx)
+
+
+def test_binding_refuses_tensors_that_do_not_fit():
+    """Wrong devices, types, shapes and layouts raise before the library is called."""
+    h = lambda *shape: torch.zeros(*shape, dtype=torch.float16)
+    n = lambda *shape: torch.zeros(*shape, dtype=torch.int32)
+    c = lambda *shape: torch.zeros(*shape, dtype=torch.uint8)
+    e = torch.zeros(2, dtype=torch.int64)
+    with pytest.raises(ValueError, match="GPU"):
+        lp.op_kv4_decode_attention(h(2, 4, 64), h(2, 4, 64), c(3, 2, 4608), n(2, 3), n(2), n(2), 70, c(64))
+    with pytest.raises(ValueError, match="GPU"):
+        lp.op_kv4_prefill_attention(h(2, 4, 64), h(2, 4, 64), c(3, 2, 4608), n(2, 3), n(2), n(1), n(1), 2, 70, c(64))
+    with pytest.raises(ValueError, match="GPU"):
+        lp.op_kv4_read(c(3, 2, 4608), e, e, h(3, 2, 64, 64), h(3, 2, 64, 64))
+    with pytest.raises(ValueError, match="cache"):
+        lp.op_kv4_append(torch.zeros(2, 512), torch.zeros(9, 32), torch.zeros(9, 32), n(2), e, h(2, 4, 64), c(3, 2, 4600))
+
+
+@gpu
+def test_binding_refuses_shapes_on_the_gpu():
+    h = lambda *shape: torch.zeros(*shape, dtype=torch.float16, device=DEV)
+    n = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=DEV)
+    c = lambda *shape: torch.zeros(*shape, dtype=torch.uint8, device=DEV)
+    e = torch.zeros(2, dtype=torch.int64, device=DEV)
+    good = dict(q=h(2, 4, 64), out=h(2, 4, 64), cache=c(3, 2, 4608), block_table=n(2, 3), row_slot=n(2), row_pos=n(2),
+                max_ctx=70, ws=c(1 << 20))
+    lp.op_kv4_decode_attention(**good)
+    for bad in (dict(q=h(2, 4, 128)[:, :, ::2]), dict(out=h(3, 4, 64)), dict(cache=c(3, 2, 4600)), dict(row_slot=n(3)),
+                dict(row_pos=n(2).long()), dict(cache=h(3, 2, 4608)), dict(block_table=n(3, 2).T), dict(row_slot=n(2).cpu()),
+                dict(cache=c(3, 2, 9216)), dict(q=h(2, 4, 80), out=h(2, 4, 80))):
+        with pytest.raises(ValueError):
+            lp.op_kv4_decode_attention(**{**good, **bad})
+    with pytest.raises(lp.LPError):
+        lp.op_kv4_decode_attention(**{**good, "max_ctx": 200})
+    good = dict(cache=c(3, 2, 4608), src_entry=e, dst_entry=e, kc=h(2, 2, 64, 64), vc=h(2, 2, 64, 64))
+    e.fill_(-1)
+    lp.op_kv4_read(**good)
+    for bad in (dict(dst_entry=e[:1]), dict(src_entry=e.int()), dict(vc=h(2, 2, 64, 32)), dict(kc=h(2, 3, 64, 64),
+                vc=h(2, 3, 64, 64)), dict(vc=h(2, 2, 64, 64).float()), dict(cache=c(3, 2, 9216))):
+        with pytest.raises(ValueError):
+            lp.op_kv4_read(**{**good, **bad})
+    torch.cuda.synchronize()
+
+
+def test_loads_into_lds_keep_their_wait_states(tmp_path):
+    """What is checked of the other kernels' loads into LDS, for these."""
+    import test_device_code
+    test_device_code.test_loads_into_lds_keep_their_wait_states("kv4_attention", tmp_path)
