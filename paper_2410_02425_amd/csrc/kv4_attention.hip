@@ -797,22 +797,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // ------------------------------------------------------------------ plan
 
 // 16-row items.  A workgroup's waves share its blocks, so a row (or 16 packed ones)
-// and KV head, a "pair", is one item of all blocks where there are pairs enough,
-// and with few blocks, for which a second launch costs more than it brings;
-// eight waves share it then while that fills the GPU once.  Else items of a few
-// blocks, about 1,024 of them, at most 24 blocks each, so that long rows end with
-// the others.  (Graphs of calls, 8B heads unless said, blocks of an item with four
-// waves, "all" with eight: one row of 300 tokens 8 8.3 us, all 7.4; 4 rows of 613 4
-// 8.8, all 10.6; one of 2,000 4 9.2, 8 10.5, 16 14.7; one of 8,000 4 10.1, 8 12.0;
-// 16 of 1,000 4 16.3, 8 15.2, 16 17.0; 32 of 600, 256 pairs, 4 16.4, all 15.3; 64 of
-// 1,000, 512 pairs, 16 28.8, 32 31.1, all 28.0; 64 of 7,000 8 141, 16 132, 32 131, 64
-// 139; 13B 64 of 1,200, 2,560 pairs, 8 95.8, 16 91.5, all with four 87.2, with eight
-// 91.3.)
+// and KV head, a "pair", is one item of all blocks where there are pairs enough
+// or few blocks, for which a second launch costs more than it brings; eight
+// waves share it while that fills the GPU once.  Else items of a few blocks, about
+// 1,024 of them, at most 24 blocks each, so that long rows end with the others.
+// (Graphs of calls; an item's blocks with four waves, "all" with eight.  8B heads:
+// one row of 300 tokens 4 8.4 us, all 7.4; four of 613, longest 16 blocks, 4 8.8, all
+// 10.6; one of 2,000 4 9.2, 8 10.5, 16 14.7; one of 8,000 4 10.1, 8 12.0; 16 of 1,000 4
+// 16.3, 8 15.2, all 17.3; 20 of 300, 160 pairs, 12 13.2, all 10.8; 24 of 800, 192, 16
+// 17.7, all 15.6; 64 of 1,000, 512, 16 28.8, all 28.0; 64 of 2,300 16 54.2, 24 49.8, 32
+// 52.4, 48 54.5; 70B 64 of 8,000 16 152.7, 24 141.4, 32 141.6, 48 146.4; 13B 64 of
+// 1,200, 2,560 pairs, 8 95.8, 16 91.5, all with four waves 87.2, with eight 91.3.)
 struct Kv4Split {
   int blocks, waves;
 };
 static Kv4Split kv4_rows_split(int64_t pairs, int blocks) {
-  if (blocks <= 12 || (blocks <= 40 && pairs >= 256) || pairs >= 2048) return {blocks, pairs <= 512 ? 8 : 4};
+  if (blocks <= 12 || (blocks <= 40 && pairs >= 7 * blocks) || pairs >= 2048) return {blocks, pairs <= 512 ? 8 : 4};
   const int even = (int)std::min<int64_t>((blocks * std::min<int64_t>(pairs, 1024) + 1023) / 1024, 24);
   return {std::min(blocks, std::max(even, pairs < 64 ? 4 : 8)), 4};
 }
