@@ -1,8 +1,9 @@
 /* lp_ops.h -- single-kernel entry points of the serving step, for parity
  * checks and kernel timing.  They launch exactly the kernels the engine runs
  * (those of the last two sections, a batch that shares a prefix and a cache
- * held in 4 bits, are for callers that plan their own steps), on caller-provided device buffers,
- * asynchronously on `hip_stream` (a hipStream_t, NULL for the null stream).
+ * held in 4 bits, are for callers that plan their own steps), on
+ * caller-provided device buffers, asynchronously on `hip_stream` (a
+ * hipStream_t, NULL for the null stream).
  * All pointers are device pointers unless stated otherwise; the caller owns
  * every buffer.  Each returns LP_OK or
  * LP_EINVAL (bad sizes; checked before any launch) or LP_EHIP (launch error);
@@ -335,11 +336,14 @@ int lp_op_kv4_read(int32_t dtype, const void *cache, int64_t n_blocks, const int
 /* Decode attention over a 4-bit cache: row m of q, out [M][Hq][hd] reads
  * positions 0 .. row_pos[m] of slot row_slot[m].  Contexts longer than max_ctx
  * are clamped to it; 64 * max_blocks >= max_ctx.  A row that reads nothing
- * (position -1, no such slot, all its blocks missing) gets zeros.  Any group Hq
- * / Hkv; head_dim 64 or 128.  max_ctx and M Hq are at most 2^30, and a call that
- * would launch 2^23 workgroups or more is refused as well.
- * ws: at least lp_op_kv4_decode_attention_ws_bytes of the same sizes (0 for
- * sizes out of these limits). */
+ * (position -1, no such slot, all its blocks missing), or whose every score is
+ * minus infinity, gets zeros.  Any group Hq / Hkv; head_dim 64 or 128.  max_ctx
+ * and M Hq are at most 2^30.  A call that would launch 2^23 workgroups or more is
+ * refused as well: none is with M Hq below 2^22 and max_ctx up to 2^20, all are
+ * from M Hq = 2^25 on.
+ * ws: at least lp_op_kv4_decode_attention_ws_bytes of the same sizes, which is 0
+ * for sizes out of the limits above and ascends in M and max_ctx: the workspace
+ * of a batch's limits serves its smaller steps. */
 size_t lp_op_kv4_decode_attention_ws_bytes(int32_t M, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                            int32_t max_ctx);
 int lp_op_kv4_decode_attention(int32_t dtype, const void *q, void *out, const void *cache, int64_t n_blocks,

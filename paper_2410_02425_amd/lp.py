@@ -627,11 +627,15 @@ def op_block_tables(seq_slot, cached, lengths, prefix_blocks, prefix_len, free_b
            taken, rslot, rpos, entry, max_rows))
 
 
-def _append_args(qkv, rope_cos, rope_sin, row_pos, row_entry, q, hkv):
-    """What both appends hand over alike: the GPU, the arguments before q, heads and head_dim."""
+def op_qkv_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, kc, vc):
+    """Rotates q and k of the fp32 projection qkv [rows, (Hq + 2 Hkv) hd] (rows
+    may be strided), rounds q to q [rows, Hq, hd] and stores k and v in the
+    cache at row_entry (lp_op_qkv_append)."""
     import torch
     dt, dev = _dt3(q), _gpu(q)
     rows, hq, hd = q.shape
+    n_blocks, hkv = _cache_shape(kc, vc, hd)
+    acts = _pointers(dev, q.dtype, "q kc vc", q, kc, vc)
     cos, sin = _pointers(dev, torch.float32, "rope_cos rope_sin", rope_cos, rope_sin)
     pos, = _pointers(dev, torch.int32, "row_pos", row_pos)
     entry, = _pointers(dev, torch.int64, "row_entry", row_entry)
@@ -641,18 +645,9 @@ def _append_args(qkv, rope_cos, rope_sin, row_pos, row_entry, q, hkv):
     _need(row_pos.numel() == row_entry.numel() == rows, "row_pos and row_entry [rows]")
     _need(rope_cos.shape == rope_sin.shape and rope_cos.dim() == 2 and rope_cos.shape[1] == hd // 2,
           "rope_cos, rope_sin [positions, hd / 2]")
-    return dev, (dt, qkv.data_ptr(), qkv.stride(0) if rows > 1 else width, cos, sin, rope_cos.shape[0], pos, entry,
-                 rows), (hq, hkv, hd)
-
-
-def op_qkv_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, kc, vc):
-    """Rotates q and k of the fp32 projection qkv [rows, (Hq + 2 Hkv) hd] (rows
-    may be strided), rounds q to q [rows, Hq, hd] and stores k and v in the
-    cache at row_entry (lp_op_qkv_append)."""
-    n_blocks, hkv = _cache_shape(kc, vc, q.shape[2])
-    dev, args, heads = _append_args(qkv, rope_cos, rope_sin, row_pos, row_entry, q, hkv)
-    acts = _pointers(dev, q.dtype, "q kc vc", q, kc, vc)
-    _call(lib().lp_op_qkv_append, dev, (*args, *acts, n_blocks, *heads))
+    _call(lib().lp_op_qkv_append, dev,
+          (dt, qkv.data_ptr(), qkv.stride(0) if rows > 1 else width, cos, sin, rope_cos.shape[0], pos, entry, rows,
+           *acts, n_blocks, hq, hkv, hd))
 
 
 def prefix_decode_attention_ws_bytes(M, n_heads, n_kv_heads, head_dim, prefix_len, max_ctx):
@@ -724,11 +719,23 @@ def op_kv4_append(qkv, rope_cos, rope_sin, row_pos, row_entry, q, cache):
     """op_qkv_append into a cache held in 4 bits (lp_op_kv4_append): uint8
     cache [n_blocks, Hkv, 72 hd]."""
     import torch
-    n_blocks, hkv = _kv4_shape(cache, q.shape[2])
-    dev, args, heads = _append_args(qkv, rope_cos, rope_sin, row_pos, row_entry, q, hkv)
+    dt, dev = _dt3(q), _gpu(q)
+    rows, hq, hd = q.shape
+    n_blocks, hkv = _kv4_shape(cache, hd)
     qp, = _pointers(dev, q.dtype, "q", q)
     cp, = _pointers(dev, torch.uint8, "cache", cache)
-    _call(lib().lp_op_kv4_append, dev, (*args, qp, cp, n_blocks, *heads))
+    cos, sin = _pointers(dev, torch.float32, "rope_cos rope_sin", rope_cos, rope_sin)
+    pos, = _pointers(dev, torch.int32, "row_pos", row_pos)
+    entry, = _pointers(dev, torch.int64, "row_entry", row_entry)
+    width = (hq + 2 * hkv) * hd
+    _need(qkv.dtype is torch.float32 and qkv.get_device() == dev and qkv.shape == (rows, width)
+          and (rows == 0 or qkv.stride(1) == 1), "qkv: float32 [rows, (Hq + 2 Hkv) hd], columns contiguous")
+    _need(row_pos.numel() == row_entry.numel() == rows, "row_pos and row_entry [rows]")
+    _need(rope_cos.shape == rope_sin.shape and rope_cos.dim() == 2 and rope_cos.shape[1] == hd // 2,
+          "rope_cos, rope_sin [positions, hd / 2]")
+    _call(lib().lp_op_kv4_append, dev,
+          (dt, qkv.data_ptr(), qkv.stride(0) if rows > 1 else width, cos, sin, rope_cos.shape[0], pos, entry, rows, qp,
+           cp, n_blocks, hq, hkv, hd))
 
 
 def op_kv4_read(cache, src_entry, dst_entry, kc, vc):

@@ -874,6 +874,31 @@ def test_one_row_of_more_than_64_parts(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_the_largest_batches_that_always_fit(dtype):
+    """Rows times heads just under 2^22, of which some rows are looked at."""
+    rng = np.random.default_rng(22)
+    M, Hq, Hkv, hd, ctx = 65530, 64, 8, 64, [101, 228, 300]
+    assert M * Hq < 1 << 22 <= (M + 8) * Hq
+    b = Batch(rng, dtype, Hkv, hd, ctx)
+    q = torch.randn(M, Hq, hd, generator=torch.Generator(DEV).manual_seed(1), device=DEV).to(TYPES[dtype])
+    out, cache, table = torch.empty_like(q), b.cache(), i32(b.table)
+    j = np.arange(M) % 3
+    slot, pos = i32(b.slot[j]), i32(np.array(ctx)[j] - 1)
+    some = [0, 1, 2, 4095, 32768, 60001, M - 2, M - 1]
+    for f, size, index in ((lp.op_kv4_decode_attention, lp.kv4_decode_attention_ws_bytes, (slot, pos)),
+                           (lp.op_kv4_prefill_attention, lp.kv4_prefill_attention_ws_bytes,
+                            (i32(np.arange(M + 1)), slot, pos, 1))):
+        out.fill_(7)
+        ws = torch.empty(size(M, Hq, Hkv, hd, 300), dtype=torch.uint8, device=DEV)
+        f(q, out, cache, table, *index, 300, ws)
+        qs, have = q[some].double().cpu().numpy(), out[some].double().cpu().numpy()
+        for i, m in enumerate(some):
+            ref, tol = b.reference(qs[i:i + 1], j[m], [ctx[j[m]] - 1])
+            assert np.all(np.abs(have[i:i + 1] - ref) <= tol), m
+
+
+@gpu
 def test_caches_past_4_gib():
     """Blocks whose byte offsets pass 32 bits: what a small cache gives, to the bit."""
     rng = np.random.default_rng(21)
@@ -1162,7 +1187,7 @@ def test_binding_refuses_tensors_that_do_not_fit():
         lp.op_kv4_prefill_attention(h(2, 4, 64), h(2, 4, 64), c(3, 2, 4608), n(2, 3), n(2), n(1), n(1), 2, 70, c(64))
     with pytest.raises(ValueError, match="GPU"):
         lp.op_kv4_read(c(3, 2, 4608), e, e, h(3, 2, 64, 64), h(3, 2, 64, 64))
-    with pytest.raises(ValueError, match="cache"):
+    with pytest.raises(ValueError, match="GPU"):
         lp.op_kv4_append(torch.zeros(2, 512), torch.zeros(9, 32), torch.zeros(9, 32), n(2), e, h(2, 4, 64), c(3, 2, 4600))
 
 
