@@ -260,7 +260,10 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(Kv4Read a, T *__restrict_
     if (__all(run) && ((s0 | d0) & 63) == 0 && s0 < (uint64_t)src_end && d0 < (uint64_t)dst_end) {
       const uint8_t *src = src_of(s0);
       const int row = t / 4, i = t % 4;
-      const int q = t % 16, w = t / 16, there = w < WORDS ? n - 4 * q : 0;
+      const int q = t % 16, w = t / 16;
+      int there = w < WORDS ? n - 4 * q : 0;
+      // four positions that go on in the next workgroup's places are stored here, like any quartet
+      if (there > 0 && there < 4 && kv4_quartet(a, r0 + 4 * q)) there = 4;
       words_t kc;
       scales_t ks;
       u32x4_tt x;

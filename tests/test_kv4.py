@@ -977,6 +977,33 @@ def test_read_of_many_contexts(dtype):
     assert np.array_equal(kc.double().cpu().numpy(), wk) and np.array_equal(vc.double().cpu().numpy(), wv)
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("over", [1, 2, 3, 30, 62])
+@pytest.mark.parametrize("more", [0, 90])
+def test_read_of_a_last_block_that_starts_anywhere(dtype, over, more):
+    """The last whole block of a list starts `over` places past a multiple of 64 of
+    the list, and nothing after it begins a block."""
+    rng = np.random.default_rng(over)
+    Hkv, hd, n_blocks = 40, 64, 30
+    cache = noise(rng, n_blocks, Hkv, hd)
+    for lo in (32 * hd, 68 * hd):
+        s = scales(np.abs(rng.standard_normal((n_blocks, Hkv, 2 * hd))))
+        cache[:, :, lo:lo + 4 * hd] = s.astype(np.float16).view(np.uint8)
+    dst = np.concatenate([np.arange(12 * 64), 12 * 64 + 1 + np.arange(over), 13 * 64 + np.arange(64),
+                          16 * 64 + rng.permutation([x for x in range(8 * 64) if x % 64])[:more]])
+    src = rng.permutation(n_blocks)[dst // 64] * 64 + dst % 64
+    n_dst = 24
+    kc = torch.full((n_dst, Hkv, 64, hd), 7.0, dtype=TYPES[dtype], device=DEV)
+    vc = torch.full((n_dst, Hkv, hd, 64), 7.0, dtype=TYPES[dtype], device=DEV)
+    lp.op_kv4_read(torch.from_numpy(cache).to(DEV), i64(src), i64(dst), kc, vc)
+    torch.cuda.synchronize()
+    wk, wv = np.full(kc.shape, 7.0), np.full(vc.shape, 7.0)
+    for s, d in zip(src, dst):
+        wk[d // 64, :, d % 64], wv[d // 64, :, :, d % 64] = get(cache[s // 64], s % 64)
+    assert np.array_equal(kc.double().cpu().numpy(), wk) and np.array_equal(vc.double().cpu().numpy(), wv)
+
+
 # ------------------------------------------------------------------ graphs and streams
 
 @gpu
