@@ -605,7 +605,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
       }
       big = half_swap_max(big);
-      const int ex = big > 0.f ? __builtin_amdgcn_frexp_expf(big) : 0;
+      const int ex = big > 0.f ? min(__builtin_amdgcn_frexp_expf(big), 127) : 0;  // 2^128 is no number
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll

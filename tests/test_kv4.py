@@ -730,6 +730,32 @@ def test_bf16_queries_of_any_size():
             assert np.all(np.abs(got[r:r + 1, h:h + 1] - ref) <= bound("bf16", qr, K, V, ref, mag)), (r, h)
 
 
+@gpu
+@pytest.mark.parametrize("heads", [FEW, MANY])
+def test_bf16_queries_near_the_largest_number(heads):
+    """q at 2^127 along one dim, where K is equal at all places but one: even weights, or that place alone."""
+    rng = np.random.default_rng(13)
+    Hq, Hkv = heads
+    hd, n = 128, 150
+    b = Batch(rng, "bf16", Hkv, hd, [n])
+    K = np.full((n, Hkv, hd), 6 * 2.0 ** -11)
+    K[:, :, 0] = 2.0 ** -11
+    K[40, :, 0] = 1.5 * 2.0 ** -11
+    k, v = quantise(K), quantise(b.V[0])
+    assert np.array_equal(held(*k), K)
+    for p in range(n):
+        b.store(b.slot[0], p, [x[p] for x in k], [x[p] for x in v])
+    q = np.zeros((n, Hq, hd))
+    q[:, :, 0] = 2.0 ** 127
+    got = run_prefill(b, q, [(0, 0, n)], Hq)
+    V = np.repeat(held(*v), Hq // Hkv, axis=1)
+    for r in (0, 20, 39, 40, 41, 149):
+        ref = V[:r + 1].mean(0) if r < 40 else V[40]
+        # weights and the result rounded to 11 and 8 bits, sums of 41 terms in 24
+        mag = np.abs(V[:r + 1]).mean(0) if r < 40 else np.abs(ref)
+        assert np.all(np.abs(got[r] - ref) <= (2.0 ** -11 + 2.0 ** -19) * mag + 2.0 ** -8 * np.abs(ref) * 1.01), r
+
+
 # ------------------------------------------------------------------ attention: shapes of batches
 
 @gpu
