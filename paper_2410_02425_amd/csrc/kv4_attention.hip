@@ -27,6 +27,7 @@ struct Kv4Args {
 };
 // A part's m is the largest score before the scale 1/sqrt(hd), its weights are
 // 2^((score - m) c2).
+constexpr int KV4_UP = 15;  // fp16 weights of the rows' kernel go up to 2^15
 template <int HD>
 constexpr float KV4_C2 = (HD == 64 ? 0.125f : 0.08838834764831845f) * 1.44269504088896341f;
 
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 #pragma unroll
   for (int x = 0; x < 2 * J; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   float mx = -INFINITY, sum = 0.f;  // of row r16; sum: this lane's keys alone
-  int ex = -24;                     // 16-bit types: 2^ex is above V's largest scale so far, at first the least of all
+  int ex = -24 - KV4_UP;  // 16-bit types: 2^(ex + KV4_UP) is above V's largest scale so far, at first the least of all
   // this lane's places in K's and V's halves, the rest of an address being constant
   int kat = (8 * (r16 >> 2) + (r16 & 3)) * (HD / 2) + (J == 4 ? quad : quad >> 1) * 16;
   kat = (kat ^ ((r16 >> 2) & (KP - 1)) * 16) + (J == 4 ? 0 : (quad & 1) * 8);
@@ -238,8 +239,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
     m = fmaxf(mx, quads_max(m));
     int e = ex;
     if constexpr (!WIDE) {
-      // weights times scales stay within fp16's range for values of any size: the
-      // weights are taken by 2^ex, above the largest of the scales so far (of keys that a row of the tile sees)
+      // Weights times scales are taken by 2^-ex: below 2^15 for values of any size,
+      // and normal numbers of fp16 down to 2^-29 of the largest scale so far (of keys
+      // that a row of the tile sees), so that large values elsewhere cost no bits.
       if (go)
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(ND + FULL) : "memory");  // V's scales are there
       else
@@ -256,7 +258,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
         big = fmaxf(big, (float)__builtin_bit_cast(_Float16, (uint16_t)(raw[x] >> 16)));
       }
       big = wave_max(big);
-      e = __builtin_amdgcn_readfirstlane(big > 0.f ? __builtin_amdgcn_frexp_expf(fminf(big, 65504.f)) : ex);
+      e = __builtin_amdgcn_readfirstlane(big > 0.f ? __builtin_amdgcn_frexp_expf(fminf(big, 65504.f)) - KV4_UP : ex);
       e = max(e, ex);
     }
     if (e > ex || __any(m > mx && ctx > 0)) {

@@ -710,6 +710,44 @@ def test_values_of_any_size(dtype, hd, heads, vscale):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,hd", [("f16", 128), ("bf16", 64), ("f32", 128)])
+@pytest.mark.parametrize("heads", [FEW, MANY])
+def test_large_values_beside_small_ones(dtype, hd, heads):
+    """V's groups of sizes up to 2^12 apart, one of them 2^12 times larger still in one place.
+    Bounds are of each group's own largest value, and 2^-39 of the largest of all a key (half
+    the least step of fp16 where the largest scale is held as 2^14)."""
+    rng = np.random.default_rng(hd + 5)
+    Hq, Hkv = heads
+    ctx = [200, 77]
+    b = Batch(rng, dtype, Hkv, hd, ctx)
+    size = np.exp2(-rng.integers(0, 13, (1, Hkv, hd // 32)).astype(float))
+    size[:, :, 1] = 1.0
+    for j, c in enumerate(ctx):
+        large = np.ones((c, 1, hd // 32))
+        large[20, :, 1] = 2.0 ** 12
+        v = quantise(rng.standard_normal((c, Hkv, hd)) * np.repeat(size * large, 32, axis=2))
+        b.V[j] = held(*v)
+        k = quantise(b.K[j])
+        b.K[j] = held(*k)
+        for p in range(c):
+            b.store(b.slot[j], p, [x[p] for x in k], [x[p] for x in v])
+    q = values(rng, (250, Hq, hd), dtype)
+    got = run_prefill(b, q, [(0, 0, 200), (1, 27, 50)], Hq)
+    dec = run_decode(b, q[:2], [(0, 199), (1, 76)], Hq)
+    for have, pairs in ((got, [(r, 0, r) for r in range(200)] + [(200 + r, 1, 27 + r) for r in range(50)]),
+                        (dec, [(0, 0, 199), (1, 1, 76)])):
+        for r, j, p in pairs[::7] + pairs[-1:]:
+            K, V, qr = b.K[j][:p + 1], b.V[j][:p + 1], q[r:r + 1]
+            ref, mag = (T.attention(qr, K, v, [p], np.arange(p + 1), Hkv) for v in (V, np.abs(V)))
+            for h in range(Hkv):
+                for d in range(0, hd, 32):
+                    at = (slice(None), slice(h * Hq // Hkv, (h + 1) * Hq // Hkv), slice(d, d + 32))
+                    tol = bound(dtype, qr, K, V[:, h:h + 1, d:d + 32], ref[at], mag[at])
+                    tol = tol + (p + 1) * 2.0 ** -39 * np.abs(V).max() - 2.0 ** -25 * (dtype == "bf16")
+                    assert np.all(np.abs(have[r:r + 1][at] - ref[at]) <= tol), (j, p, h, d)
+
+
+@gpu
 def test_bf16_queries_of_any_size():
     """Rows of q of very different sizes, and dims of very different sizes in a row, in tiles."""
     rng = np.random.default_rng(12)
