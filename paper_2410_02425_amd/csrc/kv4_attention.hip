@@ -417,6 +417,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 // the format (NaN: the group held an infinity or NaN), the values are 0 as well, and the
 // rows that see the place get NaN in the group's dims afterwards.
 constexpr float KV4_LAZY = 8.f;
+constexpr float KV4_TILE_UP = 7.f;  // weights are taken by 2^7: fp16's normal numbers are then those from 2^-21 to 2^8
 constexpr float KV4_LARGE = 64.f;  // base-2 score up to which the rounded mc is within 2^-19: weights within 1.3e-6
 template <typename T, int HD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void kv4_tile_kernel(
@@ -694,7 +695,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[t][r] *= corr;
-        mc = nm == -INFINITY ? 0.f : nm * c2;  // a row that has seen no key yet
+        mc = nm == -INFINITY ? 0.f : fmaf(nm, c2, -KV4_TILE_UP);  // a row that has seen no key yet
         large = __any(fabsf(mc) > KV4_LARGE);
       }
       // s c2 - mc in one FMA is off 0 at the maximum by what mc's rounding left
@@ -706,7 +707,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[t][r] -= m0;
-        mo = 0.f;
+        mo = -KV4_TILE_UP;
       }
       v8 pb[4];
 #pragma unroll
