@@ -45,7 +45,8 @@ __device__ __forceinline__ typename Mfma<T>::v8 codes8(uint32_t w) {
 // one's), each rounded once to fp16.
 __device__ __forceinline__ uint32_t mul_pair(float x, float y, uint32_t sv) {
   uint32_t d;
-  asm("v_fma_mixlo_f16 %0, %1, %3, 0 op_sel_hi:[0,1,0]\n\tv_fma_mixhi_f16 %0, %2, %3, 0 op_sel:[0,1,0] op_sel_hi:[0,1,0]"
+  asm("v_fma_mixlo_f16 %0, %1, %3, 0 op_sel_hi:[0,1,0]\n\t"
+      "v_fma_mixhi_f16 %0, %2, %3, 0 op_sel:[0,1,0] op_sel_hi:[0,1,0]"
       : "=&v"(d)
       : "v"(x), "v"(y), "v"(sv));
   return d;
@@ -67,9 +68,17 @@ __device__ __forceinline__ float quads_sum(float v) {
 // are worked on, its V half while the scores are.  S^T = K Q^T: a lane holds one
 // row's scores of 8 consecutive keys of each 32, which is the operand of O^T +=
 // V^T P^T as it lies; V's pairs of keys are made from its words of one key by
-// exchanging halves of bytes.
-template <typename T, int HD, int NW>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 ? 3 : 4))) void kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
+// exchanging halves of bytes.  ROOMY, for launches of at most two waves a SIMD, has
+// registers for more loads and products at once (8B heads, one row of 613 tokens 8.5
+// us on the GPU with 123 registers, 8.25 with 176; four waves a SIMD need 128).
+// What bounds it: many rows, the memory (64 rows of 2,300, 170 MB, 49 us; 70B 64 of
+// 8,000, 592 MB, 141 us, 4.2 TB/s of 4.7 that a copy reaches) with the rows' different
+// ends, the join of their parts (5 and 7 us of these) and vector instructions
+// behind it (53% of a SIMD's cycles); a row alone, its chain of loads (slot, ids,
+// codes: 2.1 us) and one or two blocks of a wave (2 us each).
+template <typename T, int HD, int NW, bool ROOMY>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(ROOMY ? 2 : sizeof(T) == 4 ? 3 : 4))) void
+kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef Kv4<HD> F;
   constexpr bool WIDE = sizeof(T) == 4;
   typedef std::conditional_t<WIDE, bf16_t, T> QT;      // operands of the scores
@@ -168,11 +177,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 #pragma unroll
   for (int x = 0; x < 2 * J; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   float mx = -INFINITY, sum = 0.f;  // of row r16; sum: this lane's keys alone
-  int ex = -24 - KV4_UP;  // 16-bit types: 2^(ex + KV4_UP) is above V's largest scale so far, at first the least of all
+  int ex = -24 - KV4_UP;  // 16-bit types: V's largest scale so far is below 2^(ex + KV4_UP), at first the least of all
   // this lane's places in K's and V's halves, the rest of an address being constant
   int kat = (8 * (r16 >> 2) + (r16 & 3)) * (HD / 2) + (J == 4 ? quad : quad >> 1) * 16;
   kat = (kat ^ ((r16 >> 2) & (KP - 1)) * 16) + (J == 4 ? 0 : (quad & 1) * 8);
-  int skat = F::k_scale(8 * quad, 0), vat = F::v_word(8 * quad, J == 4 ? r16 : r16 >> 1), svat = F::v_scale(8 * quad, 0);
+  int skat = F::k_scale(8 * quad, 0), vat = F::v_word(8 * quad, J == 4 ? r16 : r16 >> 1);
+  int svat = F::v_scale(8 * quad, 0);
   asm volatile("" : "+v"(kat), "+v"(skat), "+v"(vat), "+v"(svat));
   int i = 0;
   bool go = more();
@@ -218,7 +228,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[t][e] = fmaf((float)sk[e * J + j], acc[e], s[t][e]);
       }
-      asm volatile("" : "+v"(s[t][0]), "+v"(s[t][1]), "+v"(s[t][2]), "+v"(s[t][3]));  // products end here
+      if constexpr (!ROOMY)
+        asm volatile("" : "+v"(s[t][0]), "+v"(s[t][1]), "+v"(s[t][2]), "+v"(s[t][3]));  // products end here
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K has been read
     if (go) copy(i, true);
@@ -340,7 +351,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
           o[2 * j] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c0), p[k], o[2 * j]);
           o[2 * j + 1] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c1), p[k], o[2 * j + 1]);
         }
-        __builtin_amdgcn_sched_barrier(0);  // a group's loads and operands at a time: 128 registers
+        if constexpr (!ROOMY)
+          __builtin_amdgcn_sched_barrier(0);  // a group's loads and operands at a time: 128 registers
       };
       group(std::integral_constant<int, 0>());
       group(std::integral_constant<int, 1>());
@@ -378,9 +390,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(sizeof(
     if (!__builtin_amdgcn_readlane((int)live, r)) continue;
     const int token = __builtin_amdgcn_readlane(w.token, r), h = __builtin_amdgcn_readlane(w.head, r);
     float M = -INFINITY, L = 0.f, v[HD / 64];
+#pragma unroll
     for (int k = 0; k < NW; ++k) M = fmaxf(M, wm[k * 16 + r]);
 #pragma unroll
     for (int d = 0; d < HD / 64; ++d) v[d] = 0.f;
+#pragma unroll
     for (int k = 0; k < NW; ++k) {
       const float m = wm[k * 16 + r], f = m == M ? 1.f : __builtin_amdgcn_exp2f((m - M) * c2);
       L += f * wl[k * 16 + r];
@@ -898,10 +912,17 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   const unsigned grid = (unsigned)wgs;
   if constexpr (sizeof(T) == 2)
     if (tile) kv4_tile_kernel<T, HD><<<grid, 256, 0, s>>>(q, out, a);
+  const auto rows = [&](auto nw, auto roomy) {
+    constexpr int NW = decltype(nw)::value;
+    kv4_rows_kernel<T, HD, NW, decltype(roomy)::value><<<grid, NW * 64, 0, s>>>(q, out, a);
+  };
+  typedef std::integral_constant<int, 8> eight;
+  typedef std::integral_constant<int, 4> four;
+  const bool roomy = wgs * split.waves <= 2048;  // at most two waves a SIMD
   if (!tile && split.waves == 8)
-    kv4_rows_kernel<T, HD, 8><<<grid, 512, 0, s>>>(q, out, a);
+    roomy ? rows(eight(), std::true_type()) : rows(eight(), std::false_type());
   else if (!tile)
-    kv4_rows_kernel<T, HD, 4><<<grid, 256, 0, s>>>(q, out, a);
+    roomy ? rows(four(), std::true_type()) : rows(four(), std::false_type());
   if (a.splits > 1) launch_attention_join<T>(out, b, a.splits, a.sblk, a.po, a.pml, s);
   return true;
 }
