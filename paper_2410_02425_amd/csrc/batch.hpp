@@ -37,12 +37,14 @@ __device__ __forceinline__ void seq_rows(const PrefixBatch &b, int j, int &start
   n = min(max(b.seq_start[j + 1], start), b.rows) - start;
 }
 
-// Keys that row i of sequence j sees.
-__device__ __forceinline__ int row_ctx(const PrefixBatch &b, int j, int i) {
-  const int slot = b.seq_slot[j], p0 = b.seq_pos[j];
+// Keys that row i of sequence j sees, of a sequence in `slot` from position p0 on.
+__device__ __forceinline__ int row_ctx(const PrefixBatch &b, int slot, int p0, int i) {
   if (slot < 0 || slot >= b.n_slots) return 0;
   const int64_t ctx = (int64_t)p0 + i + 1;
   return p0 < 0 ? 0 : (int)min(ctx, (int64_t)b.max_ctx);
+}
+__device__ __forceinline__ int row_ctx(const PrefixBatch &b, int j, int i) {
+  return row_ctx(b, b.seq_slot[j], b.seq_pos[j], i);
 }
 
 // Rows are packed: a sequence's tokens, each with the G query heads of a KV head.
@@ -63,18 +65,28 @@ __device__ __forceinline__ PrefixRow packed_row(const A &a, int start, int r0, i
 
 // Own tile u of RT packed rows: sequence by sequence, each with as many tiles as
 // its rows need.  Each wave finds it on its own: an inclusive sum over 64
-// sequences at a time, the first whose sum exceeds u.  False past the last.
+// sequences at a time, the first whose sum exceeds u.  False past the last.  The
+// sequence's rows, slot and position come from the same lanes, requested together.
+struct TileSeq {
+  int start, n, slot, p0;
+};
 template <int RT, typename A>
-__device__ __forceinline__ bool own_tile(const A &a, int u, int &j, int &r0) {
+__device__ __forceinline__ bool own_tile(const A &a, int u, int &j, int &r0, TileSeq &s) {
   const int lane = threadIdx.x & 63;
   if (!a.b.seq_start) {  // one row a sequence
-    j = div_by(u, a.by_per);
+    j = __builtin_amdgcn_readfirstlane(div_by(u, a.by_per));  // its loads stay scalar
     r0 = (u - j * (int)a.by_per.d) * RT;
-    return j < a.b.n_seq;
+    if (j >= a.b.n_seq) return false;
+    s = TileSeq{j, 1, a.b.seq_slot[j], a.b.seq_pos[j]};
+    return true;
   }
   for (int base = 0; base < a.b.n_seq; base += 64) {
-    int start, n = 0;
-    if (base + lane < a.b.n_seq) seq_rows(a.b, base + lane, start, n);
+    int start = 0, n = 0, slot = -1, p0 = -1;
+    if (base + lane < a.b.n_seq) {
+      seq_rows(a.b, base + lane, start, n);
+      slot = a.b.seq_slot[base + lane];
+      p0 = a.b.seq_pos[base + lane];
+    }
     const int tiles = (int)(((int64_t)min(n, a.b.max_new) * a.G + RT - 1) / RT);
     const int incl = (int)wave_scan((uint64_t)tiles);
     const int total = __builtin_amdgcn_readlane(incl, 63);
@@ -82,11 +94,18 @@ __device__ __forceinline__ bool own_tile(const A &a, int u, int &j, int &r0) {
       const int k = __popcll(__ballot(incl <= u));  // sequences wholly before the tile
       j = base + k;
       r0 = (__shfl(incl, k, 64) - 1 - u) * RT;  // from the last, whose rows see most
+      s = TileSeq{__shfl(start, k, 64), __shfl(n, k, 64), __shfl(slot, k, 64), __shfl(p0, k, 64)};
       return true;
     }
     u -= total;
   }
   return false;
+}
+
+template <int RT, typename A>
+__device__ __forceinline__ bool own_tile(const A &a, int u, int &j, int &r0) {
+  TileSeq s;
+  return own_tile<RT>(a, u, j, r0, s);
 }
 
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }

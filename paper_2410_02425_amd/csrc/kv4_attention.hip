@@ -97,19 +97,18 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   const int i0 = div_by(blockIdx.x, a.by_hkv), g = blockIdx.x - i0 * Hkv;
   const int part = div_by(i0, a.by_units);  // all rows' first splits, then their second ones
   int j_, r0;
-  if (!own_tile<16>(a, i0 - part * a.units, j_, r0)) return;
-  const int seq = __builtin_amdgcn_readfirstlane(j_);
+  TileSeq ts;
+  if (!own_tile<16>(a, i0 - part * a.units, j_, r0, ts)) return;
   r0 = __builtin_amdgcn_readfirstlane(r0);
-  int start, n;
-  seq_rows(a.b, seq, start, n);
-  const int slot = a.b.seq_slot[seq];
-  const int top = row_ctx(a.b, seq, min(div_by(r0 + 15, a.by_g), n - 1));  // the last row sees most
+  const int start = __builtin_amdgcn_readfirstlane(ts.start), n = __builtin_amdgcn_readfirstlane(ts.n);
+  const int slot = __builtin_amdgcn_readfirstlane(ts.slot), p0 = __builtin_amdgcn_readfirstlane(ts.p0);
+  const int top = row_ctx(a.b, slot, p0, min(div_by(r0 + 15, a.by_g), n - 1));  // the last row sees most
   const int e0 = part * a.sblk, e1 = min(e0 + a.sblk, (top + KV_BLOCK - 1) / KV_BLOCK);
   const bool direct = a.splits == 1;
   if (!direct && !a.b.seq_start && e0 >= e1) return;  // decode's join reads no such part
   auto row_live = [&](const PrefixRow &w) __attribute__((always_inline)) { return w.t < n && w.t < a.b.max_new; };
   const PrefixRow row = packed_row(a, start, r0, r16, g);
-  const int ctx = row_live(row) ? row_ctx(a.b, seq, row.t) : 0;
+  const int ctx = row_live(row) ? row_ctx(a.b, slot, p0, row.t) : 0;
   // keys that every row of the tile sees; rows that see nothing get zeros at the end
   const int ctx_lo = (int)wave_min_u32(ctx ? (uint32_t)ctx : (uint32_t)INT_MAX);
   // Lane i: block id of entry win + i, -1 for none; left: those of them that are
@@ -458,17 +457,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int i0 = div_by(blockIdx.x, a.by_hkv), g = blockIdx.x - i0 * Hkv;
   const int part = div_by(i0, a.by_units);
   int j_, r0;
-  if (!own_tile<RT>(a, i0 - part * a.units, j_, r0)) return;
-  const int seq = __builtin_amdgcn_readfirstlane(j_);
+  TileSeq ts;
+  if (!own_tile<RT>(a, i0 - part * a.units, j_, r0, ts)) return;
   r0 = __builtin_amdgcn_readfirstlane(r0);
-  int start, n;
-  seq_rows(a.b, seq, start, n);
-  const int slot = a.b.seq_slot[seq];
-  const int top = row_ctx(a.b, seq, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
+  const int start = __builtin_amdgcn_readfirstlane(ts.start), n = __builtin_amdgcn_readfirstlane(ts.n);
+  const int slot = __builtin_amdgcn_readfirstlane(ts.slot), p0 = __builtin_amdgcn_readfirstlane(ts.p0);
+  const int top = row_ctx(a.b, slot, p0, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
   const int e0 = part * a.sblk, e1 = min(e0 + a.sblk, (top + KV_BLOCK - 1) / KV_BLOCK);
   const PrefixRow w = packed_row(a, start, r0, wave * 32 + l32, g);
   const bool live = w.t < n && w.t < a.b.max_new;
-  const int wctx = live ? row_ctx(a.b, seq, w.t) : 0;
+  const int wctx = live ? row_ctx(a.b, slot, p0, w.t) : 0;
   // rows that do not exist or see nothing (zeros at the end, whatever is summed for them) ask for no mask
   const int ctx = wctx ? wctx : INT_MAX;
   const int ctx_lo = (int)wave_min_u32((uint32_t)ctx);
@@ -662,6 +660,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int base = e * KV_BLOCK, stage = (e - e0) & 1;
     char *ks = lds + stage * STAGE, *vs = ks + PB;
     const int next = find(e + 2);
+    const int odd = odd_at[stage];  // asked for long before its use
     if (staged >= 0 && base < ctx_top) {  // else no block, or wholly past this wave's rows
       floatx16_t s[2];
 #pragma unroll
@@ -753,7 +752,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         fill_v(stage ^ 1, k);
       }
       load_v(next);
-      if (odd_at[stage] == e + 1) {
+      if (odd == e + 1) {
         const char *sc = head_of(staged);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
