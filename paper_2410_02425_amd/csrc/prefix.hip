@@ -816,9 +816,10 @@ __global__ __launch_bounds__(512) void prefix_row_kernel(const T *__restrict__ q
 // Joins the parts of a (token, head), a wave each, or with more than 16 parts
 // four: its lanes hold the weights of 64 parts first, then the dims of U parts
 // at a time; of four waves each takes 16 of the 64, and they add up in LDS (one
-// row of 32 heads, 66 parts: the call 26.2 -> 22.3 us).  Bound by memory: 633
-// rows of 32 heads, three parts each, 9.2 us, 4.0 TB/s.
-template <typename T, int HD, int U, int W>
+// row of 32 heads, 66 parts: the call 26.2 -> 22.3 us).  Bound by memory: MANY, for
+// rows enough to hide the weights' loads, then asks for the o of parts with keys
+// alone (633 rows of 32 heads, two of three parts each, 9.2 us, else 11.0).
+template <typename T, int HD, int U, int W, bool MANY>
 __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, PrefixArgs a) {
   static_assert(W == 1 || (W == 4 && U == 16), "a fourth of 64 parts in one step");
   constexpr int DPL = HD / 64;
@@ -849,16 +850,22 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, P
     const float f = x.x == -INFINITY ? 0.f : x.x == mn ? 1.f : __builtin_amdgcn_exp2f((x.x - mn) * c2);
     L = L * f0 + wave_sum(f * x.y);
     M = mn;
+    if (MANY && !filled) continue;
+    const int first = MANY ? __builtin_ctzll(filled) : 0;
 #pragma unroll
     for (int d = 0; d < DPL; ++d) o[d] *= f0;
     for (int p = W == 1 ? 0 : wave * U; p < n; p += W * U) {
       // all requested before any is used, and before it is known which parts have
-      // keys (half a microsecond a call); past the last part: 0 of that part again
+      // keys (half a microsecond a call of few rows); past the last part: 0 of that part
+      // again
       float v[U][DPL];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        int from = min(p + u, n - 1);
+        if (MANY && !(filled >> from & 1)) from = first;
 #pragma unroll
-        for (int d = 0; d < DPL; ++d) v[u][d] = po[(int64_t)(p0 + min(p + u, n - 1)) * HD + d];
+        for (int d = 0; d < DPL; ++d) v[u][d] = po[(int64_t)(p0 + from) * HD + d];
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const float fu = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), p + u));
@@ -1037,15 +1044,22 @@ size_t prefix_attention_ws_bytes(bool decode, int rows, int n_heads, int n_kv_he
 static int64_t join_wgs(const PrefixBatch &b, int parts) {
   return parts <= 16 ? ((int64_t)b.rows * b.n_heads + 3) / 4 : (int64_t)b.rows * b.n_heads;
 }
+constexpr int JOIN_MANY = 4096;
 template <typename T, int HD>
 static void launch_join(T *out, const PrefixArgs &a, hipStream_t s) {
   const unsigned wgs = (unsigned)join_wgs(a.b, a.parts);
+  const bool many = (int64_t)a.b.rows * a.b.n_heads >= JOIN_MANY;
   if (a.parts <= 4)
-    prefix_join_kernel<T, HD, 4, 1><<<wgs, 256, 0, s>>>(out, a);
+    many ? prefix_join_kernel<T, HD, 4, 1, true><<<wgs, 256, 0, s>>>(out, a)
+         : prefix_join_kernel<T, HD, 4, 1, false><<<wgs, 256, 0, s>>>(out, a);
+  else if (a.parts <= 8)
+    many ? prefix_join_kernel<T, HD, 8, 1, true><<<wgs, 256, 0, s>>>(out, a)
+         : prefix_join_kernel<T, HD, 8, 1, false><<<wgs, 256, 0, s>>>(out, a);
   else if (a.parts <= 16)
-    prefix_join_kernel<T, HD, 16, 1><<<wgs, 256, 0, s>>>(out, a);
+    many ? prefix_join_kernel<T, HD, 16, 1, true><<<wgs, 256, 0, s>>>(out, a)
+         : prefix_join_kernel<T, HD, 16, 1, false><<<wgs, 256, 0, s>>>(out, a);
   else
-    prefix_join_kernel<T, HD, 16, 4><<<wgs, 256, 0, s>>>(out, a);
+    prefix_join_kernel<T, HD, 16, 4, false><<<wgs, 256, 0, s>>>(out, a);
 }
 
 template <typename T, int HD>
