@@ -548,7 +548,7 @@ def _call(fn, dev, args):
         stream = C_._cuda_getCurrentRawStream(dev)
     else:
         stream = torch.cuda.current_stream(dev).cuda_stream
-    if dev == torch.cuda.current_device():
+    if dev == C_._cuda_getDevice():
         rc = fn(*args, stream)
     else:
         with torch.cuda.device(dev):
@@ -585,15 +585,17 @@ def _pointers(dev, dtype, names, *tensors):
     return out
 
 
+_DT3 = {}  # torch's types that the operators take, as the library's; filled at the first call
+
+
 def _dt3(t):
-    import torch
-    d = t.dtype
-    if d is torch.float16:
-        return LP_F16
-    if d is torch.bfloat16:
-        return LP_BF16
-    _need(d is torch.float32, f"float32, bfloat16 or float16 tensors, got {d}")
-    return LP_F32
+    d = _DT3.get(t.dtype)
+    if d is None:
+        import torch
+        _DT3.update({torch.float32: LP_F32, torch.float16: LP_F16, torch.bfloat16: LP_BF16})
+        d = _DT3.get(t.dtype)
+        _need(d is not None, f"float32, bfloat16 or float16 tensors, got {t.dtype}")
+    return d
 
 
 def _cache_shape(kc, vc, hd):
@@ -767,16 +769,21 @@ def _kv4_args(q, out, cache, block_table, ws, index, names):
     index tensors' pointers, heads and head_dim, the workspace's pointer and bytes."""
     import torch
     dt, dev = _dt3(q), _gpu(q)
-    hq, hd = q.shape[1:]
+    _, hq, hd = q.shape
     n_blocks, hkv = _kv4_shape(cache, hd)
-    acts = _pointers(dev, q.dtype, "q out", q, out)
+    qp, op = _pointers(dev, q.dtype, "q out", q, out)
     cp, = _pointers(dev, torch.uint8, "cache", cache)
-    table, *idx = _pointers(dev, torch.int32, names, block_table, *index)
+    idx = _pointers(dev, torch.int32, names, *index, block_table)
     n_slots, max_blocks = block_table.shape
-    _need(out.shape == q.shape, "out: shape of q")
-    _need(ws is None or (ws.get_device() == dev and ws.is_contiguous()), "ws: contiguous, on the GPU of q")
-    space = (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
-    return dev, (dt, *acts, cp, n_blocks, table, n_slots, max_blocks), idx, (hq, hkv, hd), space
+    if out.shape != q.shape:
+        raise ValueError("out: shape of q")
+    if ws is None:
+        space = (None, 0)
+    elif ws.get_device() == dev and ws.is_contiguous():
+        space = (ws.data_ptr(), ws.nbytes)
+    else:
+        raise ValueError("ws: contiguous, on the GPU of q")
+    return dev, (dt, qp, op, cp, n_blocks, idx.pop(), n_slots, max_blocks), idx, (hq, hkv, hd), space
 
 
 def op_kv4_decode_attention(q, out, cache, block_table, row_slot, row_pos, max_ctx, ws):
@@ -786,7 +793,7 @@ def op_kv4_decode_attention(q, out, cache, block_table, row_slot, row_pos, max_c
     kv4_decode_attention_ws_bytes."""
     M = q.shape[0]
     dev, cache_args, idx, heads, space = _kv4_args(q, out, cache, block_table, ws, (row_slot, row_pos),
-                                                   "block_table row_slot row_pos")
+                                                   "row_slot row_pos block_table")
     _need(row_slot.numel() == row_pos.numel() == M, "row_slot, row_pos [M]")
     _call(lib().lp_op_kv4_decode_attention, dev, (*cache_args, *idx, M, *heads, max_ctx, *space))
 
@@ -798,6 +805,6 @@ def op_kv4_prefill_attention(q, out, cache, block_table, seq_start, seq_slot, se
     others as for decode, ws of kv4_prefill_attention_ws_bytes."""
     rows, n = q.shape[0], seq_slot.numel()
     dev, cache_args, idx, heads, space = _kv4_args(q, out, cache, block_table, ws, (seq_start, seq_slot, seq_pos),
-                                                   "block_table seq_start seq_slot seq_pos")
+                                                   "seq_start seq_slot seq_pos block_table")
     _need(seq_start.numel() == n + 1 and seq_pos.numel() == n, "seq_start [n + 1], seq_slot and seq_pos [n]")
     _call(lib().lp_op_kv4_prefill_attention, dev, (*cache_args, *idx, n, rows, max_new, *heads, max_ctx, *space))
