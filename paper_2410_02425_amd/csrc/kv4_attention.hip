@@ -70,13 +70,14 @@ __device__ __forceinline__ float quads_sum(float v) {
 // V^T P^T as it lies; V's pairs of keys are made from its words of one key by
 // exchanging halves of bytes.  ROOMY, for launches of at most two waves a SIMD, has
 // registers for more loads and products at once (8B heads, one row of 613 tokens 8.5
-// us on the GPU with 123 registers, 8.25 with 176; four waves a SIMD need 128).
+// us on the GPU with 123 registers, 8.25 with 176; four waves a SIMD need 128).  A
+// workgroup has the result's dims of one of DP parts.
 // What bounds it: many rows, the memory (64 rows of 2,300, 170 MB, 49 us; 70B 64 of
 // 8,000, 592 MB, 141 us, 4.2 TB/s of 4.7 that a copy reaches) with the rows' different
 // ends, the join of their parts (5 and 7 us of these) and vector instructions
 // behind it (53% of a SIMD's cycles); a row alone, its chain of loads (slot, ids,
-// codes: 2.1 us) and one or two blocks of a wave (2 us each).
-template <typename T, int HD, int NW, bool ROOMY>
+// codes: 2.1 us) and one or two blocks of a wave (2 us each, half of it the values).
+template <typename T, int HD, int NW, bool ROOMY, int DP>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(ROOMY ? 2 : sizeof(T) == 4 ? 3 : 4))) void
 kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef Kv4<HD> F;
@@ -86,6 +87,7 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef typename Mfma<QT>::v8 qv8;
   typedef typename Mfma<PT>::v8 pv8;
   constexpr int J = F::J, NP = WIDE ? 3 : 1;
+  constexpr int JP = J / DP, HP = HD / DP;  // groups and dims of the result that this workgroup has
   constexpr float c2 = KV4_C2<HD>;
   constexpr int PART = 36 * HD, FULL = 32 * HD / 1024, TAIL = 4 * HD / 16;  // a half's bytes, copies, lanes of the last
   constexpr int ND = FULL + 1;
@@ -94,7 +96,8 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   const int Hkv = a.b.kv.n_kv_heads, Hq = a.b.n_heads;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int r16 = lane & 15, quad = lane >> 4;
-  const int i0 = div_by(blockIdx.x, a.by_hkv), g = blockIdx.x - i0 * Hkv;
+  const int dp = blockIdx.x % DP, bid = blockIdx.x / DP;
+  const int i0 = div_by(bid, a.by_hkv), g = bid - i0 * Hkv;
   const int part = div_by(i0, a.by_units);  // all rows' first splits, then their second ones
   int j_, r0;
   TileSeq ts;
@@ -172,9 +175,9 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
     }
   }
   // o[2 j + x][i]: dim 32 j + 8 quad + 2 i + x of row r16, times 2^-ex
-  floatx4_t o[2 * J];
+  floatx4_t o[2 * JP];
 #pragma unroll
-  for (int x = 0; x < 2 * J; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+  for (int x = 0; x < 2 * JP; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   float mx = -INFINITY, sum = 0.f;  // of row r16; sum: this lane's keys alone
   int ex = -24 - KV4_UP;  // 16-bit types: V's largest scale so far is below 2^(ex + KV4_UP), at first the least of all
   // this lane's places in K's and V's halves, the rest of an address being constant
@@ -277,7 +280,7 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
       ex = e;
       sum *= corr;
 #pragma unroll
-      for (int x = 0; x < 2 * J; ++x)
+      for (int x = 0; x < 2 * JP; ++x)
 #pragma unroll
         for (int y = 0; y < 4; ++y) o[x][y] *= corr;
     }
@@ -310,7 +313,7 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
         hi[y] = ((x[2 * y] >> 4) & 0x0F0F0F0Fu) | (x[2 * y + 1] & 0xF0F0F0F0u);
       }
       auto group = [&](auto j_c) __attribute__((always_inline)) {
-        constexpr int j = decltype(j_c)::value;
+        constexpr int j = decltype(j_c)::value, l = j % JP;
         u32x4_tt raw = *(const u32x4_tt *)(ks + svat + 64 * h + 128 * j);
         if (partly) {
           // scales at places that the row does not see may be anything, and 0 * NaN is not 0
@@ -347,17 +350,17 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
                              kv4_pair16<PT, j>(hi[3])};
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
-          o[2 * j] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c0), p[k], o[2 * j]);
-          o[2 * j + 1] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c1), p[k], o[2 * j + 1]);
+          o[2 * l] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c0), p[k], o[2 * l]);
+          o[2 * l + 1] = Mfma<PT>::m16(__builtin_bit_cast(pv8, c1), p[k], o[2 * l + 1]);
         }
         if constexpr (!ROOMY)
           __builtin_amdgcn_sched_barrier(0);  // a group's loads and operands at a time: 128 registers
       };
-      group(std::integral_constant<int, 0>());
-      group(std::integral_constant<int, 1>());
+      if (dp == 0) group(std::integral_constant<int, 0>());
+      if (dp == 1 / JP) group(std::integral_constant<int, 1>());
       if constexpr (J == 4) {
-        group(std::integral_constant<int, 2>());
-        group(std::integral_constant<int, 3>());
+        if (dp == 2 / JP) group(std::integral_constant<int, 2>());
+        if (dp == 3 / JP) group(std::integral_constant<int, 3>());
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V has been read
@@ -371,12 +374,12 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   if (quad == 0) wm[wave * 16 + r16] = mx, wl[wave * 16 + r16] = sum;
   if (r16 < nrows) {
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int j = 0; j < JP; ++j)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         const float4 v = make_float4(o[2 * j][2 * y] * back, o[2 * j + 1][2 * y] * back, o[2 * j][2 * y + 1] * back,
                                      o[2 * j + 1][2 * y + 1] * back);
-        *(float4 *)(ks + (r16 * HD + 32 * j + 8 * quad + 4 * y) * 4) = v;
+        *(float4 *)(ks + (r16 * HP + 32 * j + 8 * quad + 4 * y) * 4) = v;
       }
   }
   __syncthreads();
@@ -384,33 +387,35 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   asm volatile("" : "+v"(l16));  // found again here, not held in registers over the walk
   const PrefixRow w = packed_row(a, start, r0, l16, g);
   const bool live = row_live(w);
+  constexpr int VN = (HP + 63) / 64;
   // a wave a row: its lanes over the dims
   for (int r = wave; r < nrows; r += NW) {
     if (!__builtin_amdgcn_readlane((int)live, r)) continue;
     const int token = __builtin_amdgcn_readlane(w.token, r), h = __builtin_amdgcn_readlane(w.head, r);
-    float M = -INFINITY, L = 0.f, v[HD / 64];
+    float M = -INFINITY, L = 0.f, v[VN];
 #pragma unroll
     for (int k = 0; k < NW; ++k) M = fmaxf(M, wm[k * 16 + r]);
 #pragma unroll
-    for (int d = 0; d < HD / 64; ++d) v[d] = 0.f;
+    for (int d = 0; d < VN; ++d) v[d] = 0.f;
 #pragma unroll
     for (int k = 0; k < NW; ++k) {
       const float m = wm[k * 16 + r], f = m == M ? 1.f : __builtin_amdgcn_exp2f((m - M) * c2);
       L += f * wl[k * 16 + r];
 #pragma unroll
-      for (int d = 0; d < HD / 64; ++d) v[d] += f * ((const float *)(lds + k * F::BYTES))[r * HD + d * 64 + lane];
+      for (int d = 0; d < VN; ++d) v[d] += f * ((const float *)(lds + k * F::BYTES))[r * HP + d * 64 + lane];
     }
     const bool none = __builtin_amdgcn_readlane(ctx, r) == 0;
     const int64_t row = (int64_t)token * Hq + h, rec = row * a.splits + part;
 #pragma unroll
-    for (int d = 0; d < HD / 64; ++d) {
+    for (int d = 0; d < VN; ++d) {
       if (none) v[d] = 0.f;
-      if (direct)
-        out[row * HD + d * 64 + lane] = round_to<T>(L == 0.f ? 0.f : v[d] / L);
-      else if (e0 < e1)
-        a.po[rec * HD + d * 64 + lane] = v[d];
+      if (direct && (HP >= 64 || lane < HP))
+        out[row * HD + dp * HP + d * 64 + lane] = round_to<T>(L == 0.f ? 0.f : v[d] / L);
+      else if (!direct && e0 < e1 && (HP >= 64 || lane < HP))
+        a.po[rec * HD + dp * HP + d * 64 + lane] = v[d];
     }
-    if (!direct && lane == 0) *(float2 *)(a.pml + rec * 2) = none ? make_float2(-INFINITY, 0.f) : make_float2(M, L);
+    if (!direct && dp == 0 && lane == 0)
+      *(float2 *)(a.pml + rec * 2) = none ? make_float2(-INFINITY, 0.f) : make_float2(M, L);
   }
 }
 
@@ -880,6 +885,17 @@ size_t kv4_attention_ws_bytes(bool decode, int rows, int n_heads, int head_dim, 
          sizeof(float);
 }
 
+// Parts of the result's dims, a workgroup each, by the blocks of all items: scores
+// are computed again on other CUs, the values' share of a wave's time shrinks.  (us
+// with one part, two, a group of 32 dims each: 8B heads, one row of 613 tokens, 80
+// blocks, 8.3 7.5 7.0, eight, 640, 8.4 7.9 9.8, one of 2,000 in items of four, 256, 8.9 -
+// 8.4, of 4,000, 504, 8.9 9.5; 7B one of 613, 320, 7.8 7.0 7.8, three, 1,056, 8.0 9.3; 70B
+// one of 3,000 in items, 376, 9.9 9.3; 8B in fp32, whose values cost three times as much,
+// one of 613 12.2 10.4 9.1, four in items, 512, 10.2 9.8.)
+static int kv4_dim_parts(int64_t blocks, bool split16, int groups) {
+  return blocks <= 288 ? groups : blocks <= (split16 ? 400 : 720) ? 2 : 1;
+}
+
 template <typename T, int HD>
 static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, hipStream_t s) {
   Kv4Args a{};
@@ -917,17 +933,25 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   const unsigned grid = (unsigned)wgs;
   if constexpr (sizeof(T) == 2)
     if (tile) kv4_tile_kernel<T, HD><<<grid, 256, 0, s>>>(q, out, a);
-  const auto rows = [&](auto nw, auto roomy) {
-    constexpr int NW = decltype(nw)::value;
-    kv4_rows_kernel<T, HD, NW, decltype(roomy)::value><<<grid, NW * 64, 0, s>>>(q, out, a);
+  const auto rows = [&](auto nw, auto roomy, auto parts) {
+    constexpr int NW = decltype(nw)::value, DP = decltype(parts)::value;
+    kv4_rows_kernel<T, HD, NW, decltype(roomy)::value, DP><<<grid * DP, NW * 64, 0, s>>>(q, out, a);
   };
-  typedef std::integral_constant<int, 8> eight;
-  typedef std::integral_constant<int, 4> four;
-  const bool roomy = wgs * split.waves <= 2048;  // at most two waves a SIMD
+  const auto plan = [&](auto nw) {
+    const int parts = kv4_dim_parts(wgs * a.sblk, a.splits > 1 && sizeof(T) == 2, HD / 32);
+    if (wgs * split.waves > 2048)  // more than two waves a SIMD
+      rows(nw, std::false_type(), std::integral_constant<int, 1>());
+    else if (parts == 1)
+      rows(nw, std::true_type(), std::integral_constant<int, 1>());
+    else if (parts == 2)
+      rows(nw, std::true_type(), std::integral_constant<int, 2>());
+    else
+      rows(nw, std::true_type(), std::integral_constant<int, HD / 32>());
+  };
   if (!tile && split.waves == 8)
-    roomy ? rows(eight(), std::true_type()) : rows(eight(), std::false_type());
+    plan(std::integral_constant<int, 8>());
   else if (!tile)
-    roomy ? rows(four(), std::true_type()) : rows(four(), std::false_type());
+    plan(std::integral_constant<int, 4>());
   if (a.splits > 1) launch_attention_join<T>(out, b, a.splits, a.sblk, a.po, a.pml, s);
   return true;
 }

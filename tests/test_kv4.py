@@ -278,7 +278,8 @@ def test_append_rotates(dtype, Hq, Hkv, hd, runs, extra):
 
 @gpu
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
-@pytest.mark.parametrize("Hkv,hd,rows", [(8, 128, 1), (2, 64, 5), (3, 128, 64), (1, 64, 200), (5, 128, 333), (40, 64, 130)])
+@pytest.mark.parametrize("Hkv,hd,rows", [(8, 128, 1), (2, 64, 5), (3, 128, 64), (1, 64, 200), (5, 128, 333),
+                                         (40, 64, 130)])
 @pytest.mark.parametrize("ordered", [True, False])
 def test_read(dtype, Hkv, hd, rows, ordered):
     """Every value comes back exactly; rows without an entry on either side, and
@@ -794,6 +795,23 @@ def test_bf16_queries_near_the_largest_number(heads):
         assert np.all(np.abs(got[r] - ref) <= (2.0 ** -11 + 2.0 ** -19) * mag + 2.0 ** -8 * np.abs(ref) * 1.01), r
 
 
+@gpu
+@pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("f16", 32, 8, 128), ("bf16", 8, 8, 64), ("f32", 16, 8, 128),
+                                             ("f32", 8, 8, 64)])
+@pytest.mark.parametrize("rows,ctx", [(1, 200), (3, 700), (5, 600), (8, 600), (12, 700), (1, 1500), (2, 1500),
+                                      (4, 1500)])
+def test_decode_of_few_blocks_and_many(dtype, Hq, Hkv, hd, rows, ctx):
+    """Batches from 32 blocks and heads to over 1,000, of one item a row and of several."""
+    rng = np.random.default_rng(rows + ctx)
+    b = Batch(rng, dtype, Hkv, hd, [ctx - 13 * j for j in range(rows)])
+    q = values(rng, (rows, Hq, hd), dtype)
+    pairs = [(j, ctx - 13 * j - 1) for j in range(rows)]
+    got = run_decode(b, q, pairs, Hq)
+    for r, (j, p) in enumerate(pairs):
+        ref, tol = b.reference(q[r:r + 1], j, [p])
+        assert np.all(np.abs(got[r:r + 1] - ref) <= tol), (j, p)
+
+
 # ------------------------------------------------------------------ attention: shapes of batches
 
 @gpu
@@ -1279,7 +1297,8 @@ def test_binding_refuses_tensors_that_do_not_fit():
     with pytest.raises(ValueError, match="GPU"):
         lp.op_kv4_read(c(3, 2, 4608), e, e, h(3, 2, 64, 64), h(3, 2, 64, 64))
     with pytest.raises(ValueError, match="GPU"):
-        lp.op_kv4_append(torch.zeros(2, 512), torch.zeros(9, 32), torch.zeros(9, 32), n(2), e, h(2, 4, 64), c(3, 2, 4600))
+        lp.op_kv4_append(torch.zeros(2, 512), torch.zeros(9, 32), torch.zeros(9, 32), n(2), e, h(2, 4, 64),
+                         c(3, 2, 4600))
 
 
 @gpu
@@ -1292,7 +1311,8 @@ def test_binding_refuses_shapes_on_the_gpu():
                 max_ctx=70, ws=c(1 << 20))
     lp.op_kv4_decode_attention(**good)
     for bad in (dict(q=h(2, 4, 128)[:, :, ::2]), dict(out=h(3, 4, 64)), dict(cache=c(3, 2, 4600)), dict(row_slot=n(3)),
-                dict(row_pos=n(2).long()), dict(cache=h(3, 2, 4608)), dict(block_table=n(3, 2).T), dict(row_slot=n(2).cpu()),
+                dict(row_pos=n(2).long()), dict(cache=h(3, 2, 4608)), dict(block_table=n(3, 2).T),
+                dict(row_slot=n(2).cpu()),
                 dict(cache=c(3, 2, 9216)), dict(q=h(2, 4, 80), out=h(2, 4, 80))):
         with pytest.raises(ValueError):
             lp.op_kv4_decode_attention(**{**good, **bad})
