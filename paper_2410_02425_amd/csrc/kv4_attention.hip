@@ -827,12 +827,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // and KV head, a "pair", is one item of all blocks where there are pairs enough
 // or few blocks, for which a second launch costs more than it brings; eight
 // waves share it while that fills the GPU once.  Else items of a few blocks, about
-// 1,024 of them, at most 24 blocks each, so that long rows end with the others.
+// 1,365 of them for the longest rows' lengths, at most 24 blocks each, so that long
+// rows end with the others.
 // (Graphs of calls; an item's blocks with four waves, "all" with eight.  8B heads:
 // one row of 300 tokens 4 8.4 us, all 7.4; four of 613, longest 16 blocks, 4 8.8, all
 // 10.6; one of 2,000 4 9.2, 8 10.5, 16 14.7; one of 8,000 4 10.1, 8 12.0; 16 of 1,000 4
 // 16.3, 8 15.2, all 17.3; 20 of 300, 160 pairs, 12 13.2, all 10.8; 24 of 800, 192, 16
-// 17.7, all 15.6; 64 of 1,000, 512, 16 28.8, all 28.0; 64 of 2,300 16 54.2, 24 49.8, 32
+// 17.7, all 15.6; 32 of 2,300, 256, 17 34.3, 23 39.9; 16 of 2,300 8 22.1, 10 24.3; 48
+// of 1,500, 384, 18 35.8, 24 33.3; 64 of 1,000, 512, 16 28.8, all 28.0; 64 of 2,300 16 54.2, 24 49.8, 32
 // 52.4, 48 54.5; 70B 64 of 8,000 16 152.7, 24 141.4, 32 141.6, 48 146.4; 13B 64 of
 // 1,200, 2,560 pairs, 8 95.8, 16 91.5, all with four waves 87.2, with eight 91.3.)
 struct Kv4Split {
@@ -840,7 +842,7 @@ struct Kv4Split {
 };
 static Kv4Split kv4_rows_split(int64_t pairs, int blocks) {
   if (blocks <= 12 || (blocks <= 40 && pairs >= 7 * blocks) || pairs >= 2048) return {blocks, pairs <= 512 ? 8 : 4};
-  const int even = (int)std::min<int64_t>((blocks * std::min<int64_t>(pairs, 1024) + 1023) / 1024, 24);
+  const int even = (int)std::min<int64_t>((blocks * std::min<int64_t>(pairs, 1024) * 3 + 4095) / 4096, 24);
   return {std::min(blocks, std::max(even, pairs < 64 ? 4 : 8)), 4};
 }
 
@@ -873,7 +875,7 @@ static int kv4_tile_split(int64_t items, int blocks, int64_t rows_heads) {
 // so that a workspace for a batch's limits serves its smaller steps.  Plans stay
 // within it by themselves but for batches with far more rows than their sequences
 // can have: 16-row items split only below 2,048 pairs, 32,768 rows and heads, into
-// parts of 24 blocks, or smaller ones (of four at least) up to about 1,024 items;
+// parts of 24 blocks, or smaller ones (of four at least) up to about 1,365 items;
 // tiles up to 1,024 items of 128 rows.
 static int64_t kv4_partials(bool decode, int64_t rows_heads, int blocks) {
   const int64_t quarter = rows_heads * ((blocks + 3) / 4);
