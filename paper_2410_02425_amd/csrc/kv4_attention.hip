@@ -434,11 +434,11 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
 // Values at places that no row of the tile sees are 0.  Where V's scale is not of
 // the format (NaN: the group held an infinity or NaN), the values are 0 as well, and the
 // rows that see the place get NaN in the group's dims afterwards.
-// Bound by the matrix cores and the vector instructions beside them (nine a MFMA):
-// three prompts of 2,100 after 2,000 of 70B heads, 637 GFLOP, 712 us at 2.2 GHz, 790
-// at 2.0, matrix cores busy 40% of the cycles, vector units 55%.  (Values turned
-// before the matrix instructions instead of between them 817 us for 735; eight
-// waves on 256 rows 820, 64 rows a wave 1,068.)
+// Bound by the card's power: three prompts of 2,100 after 2,000 of 70B heads, 637
+// GFLOP, 1.50 M cycles, 707 us at 2.1 GHz, 790 at 1.9; matrix cores are busy 41% of the
+// cycles, vector units 56% (nine instructions a MFMA).  (Values turned before the
+// matrix instructions instead of between them 817 us for 735; eight waves on 256 rows
+// 820, with a half of them a phase behind 811; 64 rows a wave 1,068.)
 // A reference within 2^8 of the maximum (735 us; following it exactly 773).
 constexpr float KV4_LAZY = 8.f;
 constexpr float KV4_TILE_UP = 7.f;  // weights are taken by 2^7: fp16's normal numbers are then those from 2^-21 to 2^8
