@@ -22,9 +22,24 @@ struct Kv4Args {
   int G;                // query heads of a KV head
   int units;            // row tiles
   int splits, sblk;     // splits of a tile's blocks, blocks of a split
-  Divisor by_g, by_hkv, by_units, by_per;
+  Divisor by_g, by_hkv, by_units, by_per, by_sblk;
   float *po, *pml;      // partial o [rows][n_heads][splits][hd], (m, l) [rows][n_heads][splits][2]
 };
+// Blocks of a part: a context's are shared out evenly, by STEP, among as many parts as
+// sblk asks for, so that items end together (8B heads, 48 rows of 1,500 tokens 31.9 us for
+// 35.4, 64 of 2,300 48.5 for 49.5, 64 of 1,500 39.1 for 38.2).
+template <int STEP>
+__device__ __forceinline__ void part_blocks(const Kv4Args &a, int part, int top, int &e0, int &e1) {
+  const int blocks = (top + KV_BLOCK - 1) / KV_BLOCK;
+  int each = blocks;
+  if (a.splits > 1 && blocks > a.sblk) {
+    const unsigned parts = div_by(blocks + a.sblk - 1, a.by_sblk);
+    each = (int)((blocks + parts - 1) / parts);
+    each = min((each + STEP - 1) / STEP * STEP, a.sblk);
+  }
+  e0 = part * each;
+  e1 = min(e0 + each, blocks);
+}
 // A part's m is the largest score before the scale 1/sqrt(hd), its weights are
 // 2^((score - m) c2).
 constexpr int KV4_UP = 15;  // fp16 weights of the rows' kernel go up to 2^15
@@ -106,7 +121,8 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   const int start = __builtin_amdgcn_readfirstlane(ts.start), n = __builtin_amdgcn_readfirstlane(ts.n);
   const int slot = __builtin_amdgcn_readfirstlane(ts.slot), p0 = __builtin_amdgcn_readfirstlane(ts.p0);
   const int top = row_ctx(a.b, slot, p0, min(div_by(r0 + 15, a.by_g), n - 1));  // the last row sees most
-  const int e0 = part * a.sblk, e1 = min(e0 + a.sblk, (top + KV_BLOCK - 1) / KV_BLOCK);
+  int e0, e1;
+  part_blocks<NW>(a, part, top, e0, e1);
   const bool direct = a.splits == 1;
   if (!direct && !a.b.seq_start && e0 >= e1) return;  // decode's join reads no such part
   auto row_live = [&](const PrefixRow &w) __attribute__((always_inline)) { return w.t < n && w.t < a.b.max_new; };
@@ -468,7 +484,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   const int start = __builtin_amdgcn_readfirstlane(ts.start), n = __builtin_amdgcn_readfirstlane(ts.n);
   const int slot = __builtin_amdgcn_readfirstlane(ts.slot), p0 = __builtin_amdgcn_readfirstlane(ts.p0);
   const int top = row_ctx(a.b, slot, p0, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
-  const int e0 = part * a.sblk, e1 = min(e0 + a.sblk, (top + KV_BLOCK - 1) / KV_BLOCK);
+  int e0, e1;
+  part_blocks<1>(a, part, top, e0, e1);
   const PrefixRow w = packed_row(a, start, r0, wave * 32 + l32, g);
   const bool live = w.t < n && w.t < a.b.max_new;
   const int wctx = live ? row_ctx(a.b, slot, p0, w.t) : 0;
@@ -833,10 +850,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // one row of 300 tokens 4 8.4 us, all 7.4; four of 613, longest 16 blocks, 4 8.8, all
 // 10.6; one of 2,000 4 9.2, 8 10.5, 16 14.7; one of 8,000 4 10.1, 8 12.0; 16 of 1,000 4
 // 16.3, 8 15.2, all 17.3; 20 of 300, 160 pairs, 12 13.2, all 10.8; 24 of 800, 192, 16
-// 17.7, all 15.6; 32 of 2,300, 256, 17 34.3, 23 39.9; 16 of 2,300 8 22.1, 10 24.3; 48
-// of 1,500, 384, 18 35.8, 24 33.3; 64 of 1,000, 512, 16 28.8, all 28.0; 64 of 2,300 16 54.2, 24 49.8, 32
-// 52.4, 48 54.5; 70B 64 of 8,000 16 152.7, 24 141.4, 32 141.6, 48 146.4; 13B 64 of
-// 1,200, 2,560 pairs, 8 95.8, 16 91.5, all with four waves 87.2, with eight 91.3.)
+// 17.7, all 15.6; 32 of 2,300, 256, 17 34.3, 23 39.9; 16 of 2,300 8 22.1, 10 24.3; 64
+// of 1,000, 512, 16 28.8, all 28.0; 64 of 2,300 16 54.2, 24 49.8, 32 52.4, 48 54.5; 70B
+// 64 of 8,000 16 152.7, 24 141.4, 32 141.6, 48 146.4; 13B 64 of 1,200, 2,560 pairs, 8
+// 95.8, 16 91.5, all with four waves 87.2, with eight 91.3.)
 struct Kv4Split {
   int blocks, waves;
 };
@@ -929,6 +946,7 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   a.by_g = divisor(a.G);
   a.by_hkv = divisor(Hkv);
   a.by_units = divisor(a.units);
+  a.by_sblk = divisor(a.sblk);
   a.by_per = divisor(ceil_div(a.G, 16));
   const int64_t wgs = pairs * a.splits;
   if (std::max(wgs, attention_join_wgs(b, a.splits)) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads
