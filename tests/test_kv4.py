@@ -631,6 +631,37 @@ def test_nan_groups_reach_the_rows_that_see_them(dtype, hd, heads):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,heads,seq", [
+    ("f16", (32, 8), (1500, 1)), ("bf16", (32, 8), (1500, 30)), ("f32", (4, 4), (1500, 9)), ("bf16", (64, 8), (2016, 100)),
+    ("f16", (64, 8), (2016, 100)), ("f16", (32, 8), (90, 3)), ("bf16", (64, 8), (0, 120))])
+def test_nan_scores_make_nan_rows(dtype, heads, seq):
+    """A row of q that holds NaN, and a key that does and is alone in its block, the last."""
+    rng = np.random.default_rng(77)
+    Hq, Hkv = heads
+    hd, cached, new = 128, *seq
+    n = cached + new
+    n += (1 - n) % 64               # the last key begins a block
+    cached = n - new
+    b = Batch(rng, dtype, Hkv, hd, [n])
+    q = values(rng, (new, Hq, hd), dtype)
+    if new > 1:
+        q[0] = np.nan
+        got = run_prefill(b, q, [(0, cached, new)], Hq)
+        assert np.isnan(got[0]).all() and np.isfinite(got[1:]).all()
+    dec = run_decode(b, np.full((1, Hq, hd), np.nan), [(0, n - 1)], Hq)
+    assert np.isnan(dec).all()
+    q[0] = 1.0
+    k = rng.standard_normal((Hkv, hd))
+    k[:, 40] = np.nan
+    b.store(b.slot[0], n - 1, quantise(k), quantise(rng.standard_normal((Hkv, hd))))
+    dec = run_decode(b, q[:1], [(0, n - 1)], Hq)
+    assert np.isnan(dec).all()
+    if new > 1:
+        got = run_prefill(b, q, [(0, cached, new)], Hq)
+        assert np.isnan(got[-1]).all() and np.isfinite(got[:-1]).all()
+
+
+@gpu
 @pytest.mark.parametrize("dtype,lo,hi", [("f16", 4, 30), ("bf16", 4, 90), ("f32", 4, 90)])
 @pytest.mark.parametrize("many", [False, True])
 def test_scores_of_any_size(dtype, lo, hi, many):
