@@ -863,23 +863,28 @@ static Kv4Split kv4_rows_split(int64_t pairs, int blocks) {
   return {std::min(blocks, std::max(even, pairs < 64 ? 4 : 8)), 4};
 }
 
-// Prompts' tiles of 128 rows: blocks of a split, for `items` tiles and KV heads.
-// In us: a block takes 1.45 alone on a CU, 2.45 with a second tile beside it, a
-// tile 4 more, and the join 3 and 1.6e-4 a row, head and part (more past four parts).
-// Contexts are taken to be 0.6 of the longest.  Fitted to (new + cached tokens, graphs
-// of calls): 8B 16 x 40 + 1,500 all blocks 76.5, 24 63.7, 16 56.7, 12 70.2; 4 x 100 +
-// 3,000 all 93, 24 52.7, 16 50.6, 8 56; 8 x 200 + 1,000 all 64.7, 24 78; 1 x 2,000 all
-// 58.6, 16 79; 70B 1 x 100 + 2,000 all 52.5, 16 35.4, 8 27.9, 4 28.4; 7B 1 x 547 all
-// 18.8, 6 26.2; 13B 4 x 100 + 1,000 all 50.8, 16 48.5, 12 42.7, 8 46.6.
-static int kv4_tile_split(int64_t items, int blocks, int64_t rows_heads) {
+// Prompts' tiles of 128 rows: blocks of a split, for about `items` tiles and KV heads
+// of `live` sequences.  In us: a block takes 1.45 alone on a CU, 2.25 with a second tile
+// beside it, which a launch of up to 480 tiles keeps to; more come as others end and
+// take 1.1 each.  A tile takes 3.7 more, the join 2.6 and 1.7e-4 a row, head and part.
+// Contexts of several sequences are taken to be 0.8 of the longest.  Fitted to (new +
+// cached tokens, graphs of calls, blocks of a split): 8B 16 x 40 + 1,500 all 78.0, 25 65.5,
+// 17 51.6, 13 57.1; 4 x 100 + 3,000 all 92.6, 21 56.5, 13 45.5, 11 54.2; 8 x 200 + 1,000
+// all 63.7, 15 73.8; 8 x 60 + 2,000 all 81.8, 14 46.2, 11 54.3; 32 x 30 + 800 all 53.0,
+// 14 48.3, 9 49.1; 2 x 300 + 4,000 all 123, 28 78.9, 21 88.8; 1 x 2,000 all 57.5, 16 74.5;
+// 70B 1 x 100 + 2,000 all 50.8, 17 36.7, 9 27.0, 7 26.5; 7B 1 x 547 + 2,000 all 63.1, 20
+// 54.9, 14 45.2, 10 54.5; 6 x 80 + 1,500 all 53.5, 11 44.9, 9 49.2; 13B 4 x 100 + 1,000
+// all 50.9, 16 48.1, 11 40.1, 8 46.9.
+static int kv4_tile_split(double items, int live, int blocks, int64_t rows_heads) {
+  const double all = items * blocks * (live == 1 ? 1 : 0.8) * 1.1 / 256;  // at 1.1 a block
   int best = blocks;
   double least = 0;
   for (int s = 1; s <= ceil_div(blocks, 4) && (s == 1 || items * s <= 1024); ++s) {
     const int n = ceil_div(blocks, s);
     if (ceil_div(blocks, n) != s) continue;
-    const double work = items * (double)blocks * 0.6 * 2.45 / 512;
-    const double t = 4 + std::max(n * 1.45, work + n * 0.75) +
-                     (s == 1 ? 0 : 3 + rows_heads * s * 1.6e-4 + (s > 4 ? 5 : 0));
+    const double tiles = items * s;
+    const double walk = tiles <= 256 ? n * 1.45 : tiles <= 480 ? n * 2.25 : std::max(n * 2.25, all + n * 0.7);
+    const double t = 3.7 * std::max(1.0, tiles / 512) + walk + (s == 1 ? 0 : 2.6 + rows_heads * s * 1.7e-4);
     if (s == 1 || t < least) {
       least = t;
       best = n;
@@ -935,7 +940,8 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   const bool tile = sizeof(T) == 2 && !decode && ((int64_t)units(16) * Hkv > 256 || blocks <= 2);
   a.units = units(tile ? 128 : 16);
   const int64_t pairs = (int64_t)a.units * Hkv;
-  const Kv4Split split = tile ? Kv4Split{kv4_tile_split(pairs, blocks, (int64_t)b.rows * b.n_heads), 4}
+  const double items = std::min<double>(pairs, ((double)b.rows * a.G / 128 + live / 2.0) * Hkv);  // last tiles half full
+  const Kv4Split split = tile ? Kv4Split{kv4_tile_split(items, live, blocks, (int64_t)b.rows * b.n_heads), 4}
                               : kv4_rows_split(pairs, blocks);
   const int64_t most = std::max<int64_t>(1, kv4_partials(decode, (int64_t)b.rows * b.n_heads, blocks) /
                                                 ((int64_t)b.rows * b.n_heads));

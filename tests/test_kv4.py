@@ -632,8 +632,9 @@ def test_nan_groups_reach_the_rows_that_see_them(dtype, hd, heads):
 
 @gpu
 @pytest.mark.parametrize("dtype,heads,seq", [
-    ("f16", (32, 8), (1500, 1)), ("bf16", (32, 8), (1500, 30)), ("f32", (4, 4), (1500, 9)), ("bf16", (64, 8), (2016, 100)),
-    ("f16", (64, 8), (2016, 100)), ("f16", (32, 8), (90, 3)), ("bf16", (64, 8), (0, 120))])
+    ("f16", (32, 8), (1500, 1)), ("bf16", (32, 8), (1500, 30)), ("f32", (4, 4), (1500, 9)),
+    ("bf16", (64, 8), (2016, 100)), ("f16", (64, 8), (2016, 100)), ("f16", (32, 8), (90, 3)),
+    ("bf16", (64, 8), (0, 120))])
 def test_nan_scores_make_nan_rows(dtype, heads, seq):
     """A row of q that holds NaN, and a key that does and is alone in its block, the last."""
     rng = np.random.default_rng(77)
