@@ -940,7 +940,8 @@ static bool launch_kv4_hd(const T *q, T *out, const PrefixBatch &b, float *ws, h
   const bool tile = sizeof(T) == 2 && !decode && ((int64_t)units(16) * Hkv > 256 || blocks <= 2);
   a.units = units(tile ? 128 : 16);
   const int64_t pairs = (int64_t)a.units * Hkv;
-  const double items = std::min<double>(pairs, ((double)b.rows * a.G / 128 + live / 2.0) * Hkv);  // last tiles half full
+  // sequences' last tiles taken to be half full
+  const double items = std::min<double>(pairs, ((double)b.rows * a.G / 128 + live / 2.0) * Hkv);
   const Kv4Split split = tile ? Kv4Split{kv4_tile_split(items, live, blocks, (int64_t)b.rows * b.n_heads), 4}
                               : kv4_rows_split(pairs, blocks);
   const int64_t most = std::max<int64_t>(1, kv4_partials(decode, (int64_t)b.rows * b.n_heads, blocks) /
