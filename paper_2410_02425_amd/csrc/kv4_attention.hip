@@ -48,6 +48,7 @@ constexpr float KV4_C2 = (HD == 64 ? 0.125f : 0.08838834764831845f) * 1.44269504
 
 typedef unsigned int u32x2_tt __attribute__((ext_vector_type(2)));
 typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 
 // Eight codes (a word, the low half first) as an MFMA operand.
 template <typename T>
@@ -57,14 +58,13 @@ __device__ __forceinline__ typename Mfma<T>::v8 codes8(uint32_t w) {
 }
 
 // Two products of fp32 weights and fp16 scales (x the low half of sv's, y the high
-// one's), each rounded once to fp16.
+// one's), each rounded once to fp16.  With 0 added a product is a fused step, which
+// this GPU has with these types in one instruction; the compiler picks it, and so
+// keeps the wait states before the MFMA that reads it.
 __device__ __forceinline__ uint32_t mul_pair(float x, float y, uint32_t sv) {
-  uint32_t d;
-  asm("v_fma_mixlo_f16 %0, %1, %3, 0 op_sel_hi:[0,1,0]\n\t"
-      "v_fma_mixhi_f16 %0, %2, %3, 0 op_sel:[0,1,0] op_sel_hi:[0,1,0]"
-      : "=&v"(d)
-      : "v"(x), "v"(y), "v"(sv));
-  return d;
+  const half2_t s = __builtin_bit_cast(half2_t, sv);
+  const half2_t d = {(_Float16)fmaf(x, (float)s[0], 0.f), (_Float16)fmaf(y, (float)s[1], 0.f)};
+  return __builtin_bit_cast(uint32_t, d);
 }
 
 // Maximum / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
@@ -464,7 +464,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef Kv4<HD> F;
   typedef f16x8_t v8;
-  typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
   constexpr int RT = 128;
   constexpr int J = F::J, KS = HD / 16, NT = HD / 32;
   constexpr int CK = HD / 8;           // 16-byte pieces of a K row

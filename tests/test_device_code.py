@@ -54,3 +54,41 @@ def test_loads_into_lds_keep_their_wait_states(name, tmp_path):
             assert not (op.startswith("v_") and sgprs(dst) & base), (i, waits, code[j], code[i])
             waits += int(args, 0) + 1 if op == "s_nop" else 1
             j -= 1
+
+
+def vgprs(operand):
+    """The vector registers that an operand names."""
+    m = re.fullmatch(r"v(\d+)|v\[(\d+):(\d+)\]", operand.strip())
+    if not m:
+        return set()
+    lo = int(m.group(1) or m.group(2))
+    return set(range(lo, int(m.group(3) or lo) + 1))
+
+
+@pytest.mark.parametrize("name", ["gemm", "attention", "prefix", "kv4_attention"])
+def test_operands_of_matrix_instructions_keep_their_wait_states(name, tmp_path):
+    """Two wait states stand between a vector instruction's write of a register and
+    an MFMA that reads it, one between a transcendental's and a vector instruction
+    that reads it.  The compiler keeps both for instructions of its own, but not
+    for those in asm blocks."""
+    code = [ins.partition(" ") for ins in gfx950_listing(name, tmp_path)]
+    trans = re.compile(r"v_(exp|log|rcp|rsq|sqrt|sin|cos)_")
+    mfmas = 0
+    for i, (op, _, args) in enumerate(code):
+        if not op.startswith("v_") or i == 0:
+            continue
+        read = set().union(*(vgprs(x) for x in re.findall(r"v\[\d+:\d+\]|v\d+", args.split(",", 1)[-1])))
+        before, _, written = code[i - 1]
+        if trans.match(before) and not trans.match(op):
+            assert not vgprs(written.split(",")[0]) & read, (i, code[i - 1], code[i])
+        if not op.startswith("v_mfma"):
+            continue
+        mfmas += 1
+        waits, j = 0, i - 1
+        while waits < 2 and j >= 0:
+            before, _, written = code[j]
+            if before.startswith("v_") and not before.startswith("v_mfma"):
+                assert not vgprs(written.split(",")[0]) & read, (i, waits, code[j], code[i])
+            waits += int(written, 0) + 1 if before == "s_nop" else 1
+            j -= 1
+    assert mfmas > 50
