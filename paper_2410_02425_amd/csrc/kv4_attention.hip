@@ -118,14 +118,15 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   TileSeq ts;
   if (!own_tile<16>(a, i0 - part * a.units, j_, r0, ts)) return;
   r0 = __builtin_amdgcn_readfirstlane(r0);
-  const int start = __builtin_amdgcn_readfirstlane(ts.start), n = __builtin_amdgcn_readfirstlane(ts.n);
+  const int start = __builtin_amdgcn_readfirstlane(ts.start);
+  const int n = __builtin_amdgcn_readfirstlane(min(ts.n, a.b.max_new));  // rows with a result: none reads past theirs
   const int slot = __builtin_amdgcn_readfirstlane(ts.slot), p0 = __builtin_amdgcn_readfirstlane(ts.p0);
   const int top = row_ctx(a.b, slot, p0, min(div_by(r0 + 15, a.by_g), n - 1));  // the last row sees most
   int e0, e1;
   part_blocks<NW>(a, part, top, e0, e1);
   const bool direct = a.splits == 1;
   if (!direct && !a.b.seq_start && e0 >= e1) return;  // decode's join reads no such part
-  auto row_live = [&](const PrefixRow &w) __attribute__((always_inline)) { return w.t < n && w.t < a.b.max_new; };
+  auto row_live = [&](const PrefixRow &w) __attribute__((always_inline)) { return w.t < n; };
   const PrefixRow row = packed_row(a, start, r0, r16, g);
   const int ctx = row_live(row) ? row_ctx(a.b, slot, p0, row.t) : 0;
   // keys that every row of the tile sees; rows that see nothing get zeros at the end
@@ -480,13 +481,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   TileSeq ts;
   if (!own_tile<RT>(a, i0 - part * a.units, j_, r0, ts)) return;
   r0 = __builtin_amdgcn_readfirstlane(r0);
-  const int start = __builtin_amdgcn_readfirstlane(ts.start), n = __builtin_amdgcn_readfirstlane(ts.n);
+  const int start = __builtin_amdgcn_readfirstlane(ts.start);
+  const int n = __builtin_amdgcn_readfirstlane(min(ts.n, a.b.max_new));  // rows with a result: none reads past theirs
   const int slot = __builtin_amdgcn_readfirstlane(ts.slot), p0 = __builtin_amdgcn_readfirstlane(ts.p0);
   const int top = row_ctx(a.b, slot, p0, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
   int e0, e1;
   part_blocks<1>(a, part, top, e0, e1);
   const PrefixRow w = packed_row(a, start, r0, wave * 32 + l32, g);
-  const bool live = w.t < n && w.t < a.b.max_new;
+  const bool live = w.t < n;
   const int wctx = live ? row_ctx(a.b, slot, p0, w.t) : 0;
   // rows that do not exist or see nothing (zeros at the end, whatever is summed for them) ask for no mask
   const int ctx = wctx ? wctx : INT_MAX;

@@ -939,6 +939,25 @@ def test_rows_past_max_new_and_outside_the_rows(dtype, heads):
 
 
 @gpu
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("heads", [FEW, (4, 4), MANY])
+@pytest.mark.parametrize("after", [2, 22])
+def test_places_past_max_new_cost_no_bits(hd, heads, after):
+    """Positions that only rows from max_new on would see hold the largest values, the
+    others some 2^-18: results are as near as ever, so near as weights of 11 bits make them."""
+    rng = np.random.default_rng(18)
+    (Hq, Hkv), first, new = heads, 150, 18
+    b = Batch(rng, "bf16", Hkv, hd, [first + new], vscale=2.0 ** -18)
+    for p in range(first + new, first + new + after):
+        b.store(b.slot[0], p, *(quantise(rng.standard_normal((Hkv, hd)) * x) for x in (1.0, 3e4)))
+    q = values(rng, (new + after, Hq, hd), "bf16")
+    got = run_prefill(b, q, [(0, first, new + after)], Hq, max_new=new)
+    ref, tol = b.reference(q[:new], 0, np.arange(first, first + new))
+    tol = tol - 2.0 ** -25      # bf16 has no least step there
+    assert np.all(np.abs(got[:new] - ref) <= tol), (np.abs(got[:new] - ref) / tol).max()
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 def test_many_rows_that_no_sequence_has(dtype):
     """A batch of 3,000 rows of which sequences have three: its plan stays inside its workspace."""
