@@ -337,10 +337,11 @@ int lp_op_kv4_read(int32_t dtype, const void *cache, int64_t n_blocks, const int
  * positions 0 .. row_pos[m] of slot row_slot[m].  Contexts longer than max_ctx
  * are clamped to it; 64 * max_blocks >= max_ctx.  A row that reads nothing
  * (position -1, no such slot, all its blocks missing), or whose every score is
- * minus infinity, gets zeros.  Any group Hq / Hkv; head_dim 64 or 128.  max_ctx
- * and M Hq are at most 2^30.  A call that would launch 2^23 workgroups or more is
- * refused as well: none is with M Hq below 2^22 and max_ctx up to 2^20, all are
- * from M Hq = 2^25 on.
+ * minus infinity, gets zeros.  Scores q k, before the scale 1 / sqrt(hd), are
+ * fp32 numbers: q of any size may be given as long as they are below 2^128.  Any
+ * group Hq / Hkv; head_dim 64 or 128.  max_ctx and M Hq are at most 2^30.  A
+ * call that would launch 2^23 workgroups or more is refused as well: none is
+ * with M Hq below 2^22 and max_ctx up to 2^20, all are from M Hq = 2^25 on.
  * ws: at least lp_op_kv4_decode_attention_ws_bytes of the same sizes, which is 0
  * for sizes out of the limits above and ascends in M and max_ctx: the workspace
  * of a batch's limits serves its smaller steps. */

@@ -103,7 +103,7 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   typedef typename Mfma<PT>::v8 pv8;
   constexpr int J = F::J, NP = WIDE ? 3 : 1;
   constexpr int JP = J / DP, HP = HD / DP;  // groups and dims of the result that this workgroup has
-  constexpr float c2 = KV4_C2<HD>;
+  float c2 = KV4_C2<HD>;
   constexpr int PART = 36 * HD, FULL = 32 * HD / 1024, TAIL = 4 * HD / 16;  // a half's bytes, copies, lanes of the last
   constexpr int ND = FULL + 1;
   __shared__ __attribute__((aligned(1024))) char lds[NW * F::BYTES];
@@ -171,23 +171,58 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   };
 
   qv8 qa[NP][J];  // Q^T as the B operand: this lane's row, dims 32 j + 8 quad ..
+  int up = 0;     // scores are taken by 2^-up of their row
   {
+    typedef uint32_t words_t __attribute__((ext_vector_type(2 * sizeof(T))));
     const T *qr = q + ((int64_t)(row_live(row) ? row.token : start) * Hq + row.head) * HD + quad * 8;
+    words_t x[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) x[j] = *(const words_t *)(qr + 32 * j);
+    if constexpr (!std::is_same_v<T, f16_t>) {
+      // Products with codes are summed before the group's scale makes them small: a row of q
+      // from 2^97 on is taken by a power of two to below it, and a sum over hd dims of codes up
+      // to 6 and scales up to 10,752 then stays below 2^121.
+      uint32_t big = 0;  // the largest exponent, that of the largest number for an infinity or NaN
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int e = 0; e < 2 * (int)sizeof(T); ++e) {
+          big = max(big, x[j][e] & 0x7F800000u);
+          if constexpr (!WIDE) big = max(big, x[j][e] << 16 & 0x7F800000u);
+        }
+      const float top_q = quads_max(__uint_as_float(min(big, 0x7F000000u)));
+      up = max((int)(__float_as_uint(top_q) >> 23) - 127 - 96, 0);
+      if (__any(up > 0)) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int e = 0; e < 2 * (int)sizeof(T); ++e) {
+            const float hi = __builtin_amdgcn_ldexpf(__uint_as_float(WIDE ? x[j][e] : x[j][e] & 0xFFFF0000u), -up);
+            if constexpr (WIDE) {
+              x[j][e] = __float_as_uint(hi);
+            } else {
+              const float lo = __builtin_amdgcn_ldexpf(__uint_as_float(x[j][e] << 16), -up);
+              x[j][e] = (uint32_t)round_to<bf16_t>(hi) << 16 | round_to<bf16_t>(lo);
+            }
+          }
+        c2 = __builtin_amdgcn_ldexpf(c2, up);
+      }
+    }
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       if constexpr (!WIDE) {
-        qa[0][j] = load8<T>(qr + 32 * j);
+        qa[0][j] = __builtin_bit_cast(qv8, x[j]);
       } else {
-        const float4 x = *(const float4 *)(qr + 32 * j), y = *(const float4 *)(qr + 32 * j + 4);
-        float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int p = 0; p < 3; ++p)
+        for (int e = 0; e < 8; ++e) {
+          float v = __uint_as_float(x[j][e]);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const __bf16 part_ = (__bf16)v[e];
+          for (int p = 0; p < 3; ++p) {
+            const __bf16 part_ = (__bf16)v;
             qa[p][j][e] = part_;
-            v[e] -= (float)part_;
+            v -= (float)part_;
           }
+        }
       }
     }
   }
@@ -410,13 +445,14 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
     if (!__builtin_amdgcn_readlane((int)live, r)) continue;
     const int token = __builtin_amdgcn_readlane(w.token, r), h = __builtin_amdgcn_readlane(w.head, r);
     float M = -INFINITY, L = 0.f, v[VN];
+    const float row_c2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(c2), r));
 #pragma unroll
     for (int k = 0; k < NW; ++k) M = fmaxf(M, wm[k * 16 + r]);
 #pragma unroll
     for (int d = 0; d < VN; ++d) v[d] = 0.f;
 #pragma unroll
     for (int k = 0; k < NW; ++k) {
-      const float m = wm[k * 16 + r], f = m == M ? 1.f : __builtin_amdgcn_exp2f((m - M) * c2);
+      const float m = wm[k * 16 + r], f = m == M ? 1.f : __builtin_amdgcn_exp2f((m - M) * row_c2);
       L += f * wl[k * 16 + r];
 #pragma unroll
       for (int d = 0; d < VN; ++d) v[d] += f * ((const float *)(lds + k * F::BYTES))[r * HP + d * 64 + lane];
@@ -432,7 +468,9 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
         a.po[rec * HD + dp * HP + d * 64 + lane] = v[d];
     }
     if (!direct && dp == 0 && lane == 0)
-      *(float2 *)(a.pml + rec * 2) = none ? make_float2(-INFINITY, 0.f) : make_float2(M, L);
+      *(float2 *)(a.pml + rec * 2) =
+          none ? make_float2(-INFINITY, 0.f)
+               : make_float2(__builtin_amdgcn_ldexpf(M, __builtin_amdgcn_readlane(up, r)), L);
   }
 }
 

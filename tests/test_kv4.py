@@ -827,6 +827,48 @@ def test_bf16_queries_near_the_largest_number(heads):
         assert np.all(np.abs(got[r] - ref) <= (2.0 ** -11 + 2.0 ** -19) * mag + 2.0 ** -8 * np.abs(ref) * 1.01), r
 
 
+def one_dim_batch(rng, dtype, Hkv, n, base, at_40):
+    """A sequence whose K differs along dim 0 alone: `base` codes' worth there, at place 40 `at_40`."""
+    b = Batch(rng, dtype, Hkv, 128, [n])
+    K = np.full((n, Hkv, 128), 6 * 2.0 ** -11)
+    K[:, :, 0] = base * 2.0 ** -11
+    K[40, :, 0] = at_40 * 2.0 ** -11
+    k, v = quantise(K), quantise(b.V[0])
+    assert np.array_equal(held(*k), K)
+    for p in range(n):
+        b.store(b.slot[0], p, [x[p] for x in k], [x[p] for x in v])
+    b.K[0], b.V[0] = K, held(*v)
+    return b
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", [FEW, MANY])
+@pytest.mark.parametrize("n", [150, 1500])
+@pytest.mark.parametrize("size", [2.0 ** 100, 2.0 ** 125, 2.0 ** 127 * 1.5, (2 - 2.0 ** -12) * 2.0 ** 127, -2.0 ** 127])
+def test_queries_whose_products_with_codes_pass_fp32(dtype, heads, n, size):
+    """q near the largest number along one dim, where K has codes up to 6: even weights as
+    long as all places have the same, then that place alone which has the most."""
+    rng = np.random.default_rng(14)
+    Hq, Hkv = heads
+    size = float(np.clip(size, None, (2 - 2.0 ** -7) * 2.0 ** 127)) if dtype == "bf16" else size
+    least = size < 0                # then the least is the largest score
+    b = one_dim_batch(rng, dtype, Hkv, n, 6 if least else 4, 4 if least else 6)
+    q = np.zeros((n, Hq, 128))
+    q[:, :, 0] = size
+    q[:, :, 1] = 1.0                # of no account beside it
+    got = run_prefill(b, q[:100], [(0, 0, 100)], Hq)
+    dec = run_decode(b, q[:3], [(0, 39), (0, 40), (0, n - 1)], Hq)
+    V = np.repeat(b.V[0], Hq // Hkv, axis=1)
+    for have, p in [(got[r], r) for r in (0, 20, 39, 40, 41, 99)] + list(zip(dec, (39, 40, n - 1))):
+        ref = V[:p + 1].mean(0) if p < 40 else V[40]
+        mag = np.abs(V[:p + 1]).mean(0) if p < 40 else np.abs(ref)
+        # weights and the result rounded to 11 and 8 bits, or neither; sums of 40 terms in 24
+        half = 2.0 ** -24 * np.abs(ref) if dtype == "f32" else 2.0 ** -11 * mag + 2.0 ** -8 * np.abs(ref) * 1.01
+        tol = 2.0 ** -18 * mag + half
+        assert np.all(np.abs(have - ref) <= tol), p
+
+
 @gpu
 @pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("f16", 32, 8, 128), ("bf16", 8, 8, 64), ("f32", 16, 8, 128),
                                              ("f32", 8, 8, 64)])
