@@ -172,6 +172,7 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
 
   qv8 qa[NP][J];  // Q^T as the B operand: this lane's row, dims 32 j + 8 quad ..
   int up = 0;     // scores are taken by 2^-up of their row
+  bool odd = false;  // infinities or NaN among q
   {
     typedef uint32_t words_t __attribute__((ext_vector_type(2 * sizeof(T))));
     const T *qr = q + ((int64_t)(row_live(row) ? row.token : start) * Hq + row.head) * HD + quad * 8;
@@ -190,6 +191,7 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
           big = max(big, x[j][e] & 0x7F800000u);
           if constexpr (!WIDE) big = max(big, x[j][e] << 16 & 0x7F800000u);
         }
+      odd = big >= 0x7F800000u;
       const float top_q = quads_max(__uint_as_float(min(big, 0x7F000000u)));
       up = max((int)(__float_as_uint(top_q) >> 23) - 127 - 96, 0);
       if (__any(up > 0)) {
@@ -225,6 +227,14 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
         }
       }
     }
+    if constexpr (WIDE)
+      if (__any(odd)) {  // an infinity is its first part alone: what it leaves is NaN
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if ((x[j][e] & 0x7FFFFFFFu) == 0x7F800000u) qa[1][j][e] = qa[2][j][e] = (__bf16)0.f;
+      }
   }
   // o[2 j + x][i]: dim 32 j + 8 quad + 2 i + x of row r16, times 2^-ex
   floatx4_t o[2 * JP];

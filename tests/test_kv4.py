@@ -870,6 +870,28 @@ def test_queries_whose_products_with_codes_pass_fp32(dtype, heads, n, size):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("heads", [FEW, MANY])
+@pytest.mark.parametrize("n", [150, 1500])
+def test_rows_of_scores_of_minus_infinity_are_zeros(dtype, heads, n):
+    """An infinity in a row of q, of the sign that K does not have there: every score is
+    minus infinity and the result 0; of K's sign it is NaN; the rows beside are as ever."""
+    rng = np.random.default_rng(15)
+    Hq, Hkv = heads
+    b = one_dim_batch(rng, dtype, Hkv, n, 4, 6)
+    q = values(rng, (100, Hq, 128), dtype)
+    clean = run_prefill(b, q, [(0, n - 100, 100)], Hq)
+    q[[3, 50], :, 0] = -np.inf
+    q[70, :, 0] = np.inf
+    got = run_prefill(b, q, [(0, n - 100, 100)], Hq)
+    dec = run_decode(b, q[[3, 70]], [(0, n - 1)] * 2, Hq)
+    assert np.all(got[[3, 50]] == 0) and np.all(dec[0] == 0)
+    assert np.isnan(got[70]).all() and np.isnan(dec[1]).all()
+    rest = np.setdiff1d(np.arange(100), [3, 50, 70])
+    assert np.array_equal(got[rest], clean[rest])
+
+
+@gpu
 @pytest.mark.parametrize("dtype,Hq,Hkv,hd", [("f16", 32, 8, 128), ("bf16", 8, 8, 64), ("f32", 16, 8, 128),
                                              ("f32", 8, 8, 64)])
 @pytest.mark.parametrize("rows,ctx", [(1, 200), (3, 700), (5, 600), (8, 600), (12, 700), (1, 1500), (2, 1500),
