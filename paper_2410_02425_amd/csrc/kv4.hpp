@@ -45,10 +45,11 @@ struct Kv4 {
 // A group's scale from the bits of its largest magnitude: the least number of 6
 // significant bits and steps of 2^-23 that is not below a sixth of it; NaN for
 // an infinity or NaN.  The division is the correctly rounded one, which reaches
-// a number of 6 bits only where the quotient is one.
+// a number of 6 bits only where the quotient is one; where it is 0 but the magnitude
+// is not, 2^-149 stands for it, whose scale is the same.
 __device__ __forceinline__ float kv4_scale(uint32_t amax) {
   if (amax >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-  const float t = __uint_as_float(amax) / 6.0f;
+  const float t = __uint_as_float(max(__float_as_uint(__uint_as_float(amax) / 6.0f), min(amax, 1u)));
   const float s = t < 0x1p-18f ? ceilf(t * 0x1p23f) * 0x1p-23f
                                : __uint_as_float((__float_as_uint(t) + 0x3FFFFu) & ~0x3FFFFu);
   return fminf(s, 10752.f);

@@ -214,6 +214,31 @@ def test_append_of_unrotated_rows_is_exact(dtype, Hq, Hkv, hd, runs, extra):
     assert np.array_equal(q[inside], wq[inside], equal_nan=True) and np.all(q[~inside] == 7)
 
 
+@gpu
+@pytest.mark.parametrize("hd", [64, 128])
+def test_append_of_the_least_magnitudes(hd):
+    """Groups whose largest magnitude is 0 to 9 times the least of fp32, 2^-149: all but 0 have the
+    least scale, 2^-23, also where a sixth of the magnitude is nothing in fp32."""
+    rng = np.random.default_rng(149)
+    Hq, Hkv, rows = 2, 2, 70
+    x = rng.integers(-2, 3, (rows, Hq + 2 * Hkv, hd // 32, 32)) * 2.0 ** -149
+    top = rng.integers(0, 10, x.shape[:3])
+    x[top == 0] = 0
+    x[..., 3] = top * 2.0 ** -149 * rng.choice([-1, 1], top.shape)
+    x[0, ..., 3] = [[1 * 2.0 ** -149]] * x.shape[1]
+    x[1, ..., 3] = [[3 * 2.0 ** -149]] * x.shape[1]
+    x[0, ..., 4:], x[1, ..., 4:], x[:2, ..., :3] = 0, 0, 0
+    x = x.astype(np.float32).reshape(rows, -1)
+    cos, sin = np.ones((4, hd // 2), np.float32), np.zeros((4, hd // 2), np.float32)
+    before, entry = noise(rng, 3, Hkv, hd), rng.permutation(3 * 64)[:rows]
+    _, cache = run_append("f32", x, x.shape[1], cos, sin, [1] * rows, entry, Hq, hd, before)
+    want, h = before.copy(), x.astype(np.float64).reshape(rows, -1, hd)
+    for r, e in enumerate(entry):
+        put(want[e // 64], e % 64, quantise(h[r, Hq:Hq + Hkv]), quantise(h[r, Hq + Hkv:]))
+    assert quantise(h[0])[1].min() == quantise(h[1])[1].min() == 2.0 ** -23
+    assert np.array_equal(canonical(cache), canonical(want))
+
+
 def canonical(cache):
     """Cache bytes with every NaN scale the same, and codes of NaN groups, and signs of zero codes, cleared."""
     n, Hkv, size = cache.shape
