@@ -328,7 +328,7 @@ int lp_op_kv4_append(int32_t dtype, const float *qkv, int64_t ld, const float *r
  * [n_dst_blocks][Hkv][64][hd], v_cache [n_dst_blocks][Hkv][hd][64]): K and V of
  * src_entry[i] go to dst_entry[i], i < rows, exactly.  Rows with either entry
  * outside its cache are left out.  No two rows may have the same dst_entry.
- * rows Hkv at most 2^26. */
+ * rows Hkv at most 2^26, ceil(rows / 64) Hkv below 2^24. */
 int lp_op_kv4_read(int32_t dtype, const void *cache, int64_t n_blocks, const int64_t *src_entry,
                    const int64_t *dst_entry, int32_t rows, void *k_cache, void *v_cache, int64_t n_dst_blocks,
                    int32_t n_kv_heads, int32_t head_dim, void *hip_stream);

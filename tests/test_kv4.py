@@ -1368,6 +1368,13 @@ def test_read_refusals():
         assert call(**{k: A + 8}) == EINVAL, k
 
 
+@pytest.mark.parametrize("rows,Hkv", [(1, 1 << 24), (1, 1 << 26), (3, 1 << 24)])
+def test_reads_past_one_launch_are_refused(rows, Hkv):
+    """Rows times heads within their limit, but more workgroups than a launch has."""
+    assert lp.lib().lp_op_kv4_read(F16, A, 5, A, A, rows, A, A, 6, Hkv, 128, None) == EINVAL
+    assert "kv4 read: sizes" in lp.lib().lp_last_error(None).decode()
+
+
 @pytest.mark.parametrize("decode", [True, False])
 def test_attention_refusals(decode):
     L = lp.lib()
