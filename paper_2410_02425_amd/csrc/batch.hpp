@@ -66,7 +66,8 @@ __device__ __forceinline__ PrefixRow packed_row(const A &a, int start, int r0, i
 // Own tile u of RT packed rows: sequence by sequence, each with as many tiles as
 // its rows need.  Each wave finds it on its own: an inclusive sum over 64
 // sequences at a time, the first whose sum exceeds u.  False past the last.  The
-// sequence's rows, slot and position come from the same lanes, requested together.
+// sequence's rows (those with a result, max_new at most), slot and position come from
+// the same lanes, requested together.
 struct TileSeq {
   int start, n, slot, p0;
 };
@@ -84,10 +85,11 @@ __device__ __forceinline__ bool own_tile(const A &a, int u, int &j, int &r0, Til
     int start = 0, n = 0, slot = -1, p0 = -1;
     if (base + lane < a.b.n_seq) {
       seq_rows(a.b, base + lane, start, n);
+      n = min(n, a.b.max_new);
       slot = a.b.seq_slot[base + lane];
       p0 = a.b.seq_pos[base + lane];
     }
-    const int tiles = (int)(((int64_t)min(n, a.b.max_new) * a.G + RT - 1) / RT);
+    const int tiles = (int)(((int64_t)n * a.G + RT - 1) / RT);
     const int incl = (int)wave_scan((uint64_t)tiles);
     const int total = __builtin_amdgcn_readlane(incl, 63);
     if (u < total) {

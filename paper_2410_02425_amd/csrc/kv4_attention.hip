@@ -118,8 +118,7 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
   TileSeq ts;
   if (!own_tile<16>(a, i0 - part * a.units, j_, r0, ts)) return;
   r0 = __builtin_amdgcn_readfirstlane(r0);
-  const int start = __builtin_amdgcn_readfirstlane(ts.start);
-  const int n = __builtin_amdgcn_readfirstlane(min(ts.n, a.b.max_new));  // rows with a result: none reads past theirs
+  const int start = __builtin_amdgcn_readfirstlane(ts.start), n = __builtin_amdgcn_readfirstlane(ts.n);
   const int slot = __builtin_amdgcn_readfirstlane(ts.slot), p0 = __builtin_amdgcn_readfirstlane(ts.p0);
   const int top = row_ctx(a.b, slot, p0, min(div_by(r0 + 15, a.by_g), n - 1));  // the last row sees most
   int e0, e1;
@@ -170,71 +169,13 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
     }
   };
 
-  qv8 qa[NP][J];  // Q^T as the B operand: this lane's row, dims 32 j + 8 quad ..
-  int up = 0;     // scores are taken by 2^-up of their row
-  bool odd = false;  // infinities or NaN among q
+  // q: this lane's row, dims 32 j + 8 quad ..; looked at once the first copies are out
+  typedef uint32_t words_t __attribute__((ext_vector_type(2 * sizeof(T))));
+  words_t qx[J];
   {
-    typedef uint32_t words_t __attribute__((ext_vector_type(2 * sizeof(T))));
     const T *qr = q + ((int64_t)(row_live(row) ? row.token : start) * Hq + row.head) * HD + quad * 8;
-    words_t x[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) x[j] = *(const words_t *)(qr + 32 * j);
-    if constexpr (!std::is_same_v<T, f16_t>) {
-      // Products with codes are summed before the group's scale makes them small: a row of q
-      // from 2^97 on is taken by a power of two to below it, and a sum over hd dims of codes up
-      // to 6 and scales up to 10,752 then stays below 2^121.
-      uint32_t big = 0;  // the largest exponent, that of the largest number for an infinity or NaN
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int e = 0; e < 2 * (int)sizeof(T); ++e) {
-          big = max(big, x[j][e] & 0x7F800000u);
-          if constexpr (!WIDE) big = max(big, x[j][e] << 16 & 0x7F800000u);
-        }
-      odd = big >= 0x7F800000u;
-      const float top_q = quads_max(__uint_as_float(min(big, 0x7F000000u)));
-      up = max((int)(__float_as_uint(top_q) >> 23) - 127 - 96, 0);
-      if (__any(up > 0)) {
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-          for (int e = 0; e < 2 * (int)sizeof(T); ++e) {
-            const float hi = __builtin_amdgcn_ldexpf(__uint_as_float(WIDE ? x[j][e] : x[j][e] & 0xFFFF0000u), -up);
-            if constexpr (WIDE) {
-              x[j][e] = __float_as_uint(hi);
-            } else {
-              const float lo = __builtin_amdgcn_ldexpf(__uint_as_float(x[j][e] << 16), -up);
-              x[j][e] = (uint32_t)round_to<bf16_t>(hi) << 16 | round_to<bf16_t>(lo);
-            }
-          }
-        c2 = __builtin_amdgcn_ldexpf(c2, up);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      if constexpr (!WIDE) {
-        qa[0][j] = __builtin_bit_cast(qv8, x[j]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float v = __uint_as_float(x[j][e]);
-#pragma unroll
-          for (int p = 0; p < 3; ++p) {
-            const __bf16 part_ = (__bf16)v;
-            qa[p][j][e] = part_;
-            v -= (float)part_;
-          }
-        }
-      }
-    }
-    if constexpr (WIDE)
-      if (__any(odd)) {  // an infinity is its first part alone: what it leaves is NaN
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if ((x[j][e] & 0x7FFFFFFFu) == 0x7F800000u) qa[1][j][e] = qa[2][j][e] = (__bf16)0.f;
-      }
+    for (int j = 0; j < J; ++j) qx[j] = *(const words_t *)(qr + 32 * j);
   }
   // o[2 j + x][i]: dim 32 j + 8 quad + 2 i + x of row r16, times 2^-ex
   floatx4_t o[2 * JP];
@@ -255,6 +196,69 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
     copy(i, true);
     copy(i, false);
   }
+  qv8 qa[NP][J];  // Q^T as the B operand: this lane's row
+  int up = 0;     // scores are taken by 2^-up of their row
+  bool large = false;  // wave-uniform: values from 2^97 on, infinities or NaN among q
+  if constexpr (!std::is_same_v<T, f16_t>) {
+    // Products with codes are summed before the group's scale makes them small: a row of q
+    // from 2^97 on is taken by a power of two to below it, and a sum over hd dims of codes up
+    // to 6 and scales up to 10,752 then stays below 2^121.  (8B heads in bf16, one row of
+    // 613 tokens 7.0 us, without the look at q 6.9.)
+    typedef std::conditional_t<WIDE, uint32_t, uint16_t> bits_t;
+    typedef bits_t lanes_t __attribute__((ext_vector_type(4 / sizeof(T))));
+    constexpr uint32_t EXPS = WIDE ? 0x7F800000u : 0x7F807F80u;
+    lanes_t most = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int e = 0; e < 2 * (int)sizeof(T); ++e)
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(lanes_t, qx[j][e] & EXPS));
+    uint32_t big = most[0];  // the largest exponent
+    if constexpr (!WIDE) big = (uint32_t)max(most[0], most[1]) << 16;
+    large = __any(big >= (127u + 97) << 23);
+    if (__builtin_expect(large, 0)) {
+      // that of the largest number stands for infinities and NaN
+      up = max((int)(__float_as_uint(quads_max(__uint_as_float(min(big, 254u << 23)))) >> 23) - 127 - 96, 0);
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int e = 0; e < 2 * (int)sizeof(T); ++e) {
+          const float hi = __builtin_amdgcn_ldexpf(__uint_as_float(WIDE ? qx[j][e] : qx[j][e] & 0xFFFF0000u), -up);
+          if constexpr (WIDE) {
+            qx[j][e] = __float_as_uint(hi);
+          } else {
+            const float lo = __builtin_amdgcn_ldexpf(__uint_as_float(qx[j][e] << 16), -up);
+            qx[j][e] = (uint32_t)round_to<bf16_t>(hi) << 16 | round_to<bf16_t>(lo);
+          }
+        }
+      c2 = __builtin_amdgcn_ldexpf(c2, up);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    if constexpr (!WIDE) {
+      qa[0][j] = __builtin_bit_cast(qv8, qx[j]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float v = __uint_as_float(qx[j][e]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          const __bf16 part_ = (__bf16)v;
+          qa[p][j][e] = part_;
+          v -= (float)part_;
+        }
+      }
+    }
+  }
+  if constexpr (WIDE)
+    if (__builtin_expect(large, 0)) {  // an infinity is its first part alone: what it leaves is NaN
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if ((qx[j][e] & 0x7FFFFFFFu) == 0x7F800000u) qa[1][j][e] = qa[2][j][e] = (__bf16)0.f;
+    }
   while (go) {
     const int base = (win + i) * KV_BLOCK;
     left &= left - 1;
@@ -529,8 +533,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   TileSeq ts;
   if (!own_tile<RT>(a, i0 - part * a.units, j_, r0, ts)) return;
   r0 = __builtin_amdgcn_readfirstlane(r0);
-  const int start = __builtin_amdgcn_readfirstlane(ts.start);
-  const int n = __builtin_amdgcn_readfirstlane(min(ts.n, a.b.max_new));  // rows with a result: none reads past theirs
+  const int start = __builtin_amdgcn_readfirstlane(ts.start), n = __builtin_amdgcn_readfirstlane(ts.n);
   const int slot = __builtin_amdgcn_readfirstlane(ts.slot), p0 = __builtin_amdgcn_readfirstlane(ts.p0);
   const int top = row_ctx(a.b, slot, p0, min(div_by(r0 + RT - 1, a.by_g), n - 1));  // the last row sees most
   int e0, e1;
