@@ -311,7 +311,13 @@ int lp_op_prefix_prefill_attention(int32_t dtype, const void *q, void *out, cons
  *                                byte J r + j of a position's hd / 2 bytes: dims
  *                                32 j + 2 r and the next (r < 16)
  *   V scales  [J][64] fp16
- * Any bytes are a cache: places that no row may read need not be cleared. */
+ * Any bytes are a cache: places that no row may read need not be cleared; those
+ * that rows read hold what lp_op_kv4_append wrote, or scales and codes of the kind.
+ *
+ * Attention of 16-bit types rounds each weight once, to fp16.  bf16 rows of q of
+ * longer prompts are taken to fp16 by their largest element: elements below 2^-14
+ * of it are then off by up to 2^-25 of it, which only keys far larger in their dims
+ * than in the largest's would show. */
 
 /* Bytes of a cache; 0 for sizes that no call takes. */
 size_t lp_op_kv4_cache_bytes(int64_t n_blocks, int32_t n_kv_heads, int32_t head_dim);

@@ -87,10 +87,10 @@ __device__ __forceinline__ float quads_sum(float v) {
 // registers for more loads and products at once (8B heads, one row of 613 tokens 8.5
 // us on the GPU with 123 registers, 8.25 with 176; four waves a SIMD need 128).  A
 // workgroup has the result's dims of one of DP parts.
-// What bounds it: many rows, the memory (64 rows of 2,300, 170 MB, 49 us; 70B 64 of
+// What bounds it: many rows, the memory (64 rows of 2,300, 170 MB, 48 us; 70B 64 of
 // 8,000, 592 MB, 141 us, 4.2 TB/s of 4.7 that a copy reaches) with the rows' different
 // ends, the join of their parts (5 and 7 us of these) and vector instructions
-// behind it (53% of a SIMD's cycles); a row alone, its chain of loads (slot, ids,
+// behind it (45% and 54% of a SIMD's cycles); a row alone, its chain of loads (slot, ids,
 // codes: 2.1 us) and one or two blocks of a wave (2 us each, half of it the values).
 template <typename T, int HD, int NW, bool ROOMY, int DP>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(ROOMY ? 2 : sizeof(T) == 4 ? 3 : 4))) void
@@ -499,7 +499,8 @@ kv4_rows_kernel(const T *__restrict__ q, T *__restrict__ out, Kv4Args a) {
 //   are consecutive keys, the operand of O^T += V^T P^T.
 // bf16: a row of q is taken by its largest exponent, which the scores' factor
 // brings back; its fp16 is then exact but for values below 2^-14 of the largest,
-// whose rounding (2^-25 of the largest) is that of the fp32 sums.
+// whose rounding (2^-25 of the largest) is that of the fp32 sums (of rows whose large
+// elements meet large keys: the rows' kernel keeps such values whole).
 // Values at places that no row of the tile sees are 0.  Where V's scale is not of
 // the format (NaN: the group held an infinity or NaN), the values are 0 as well, and the
 // rows that see the place get NaN in the group's dims afterwards.

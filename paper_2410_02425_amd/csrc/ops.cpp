@@ -371,8 +371,9 @@ extern "C" int lp_op_kv4_read(int32_t dtype, const void *cache, int64_t n_blocks
                               int64_t n_dst_blocks, int32_t n_kv_heads, int32_t head_dim, void *stream) {
   OPCHK(n_kv_heads > 0 && (head_dim == 64 || head_dim == 128), "kv4 read: heads, head_dim 64 or 128");
   OPCHK(dtype == LP_BF16 || dtype == LP_F16 || dtype == LP_F32, "kv4 read: dtype");
+  // a launch has fewer than 2^32 threads, 256 to a workgroup
   OPCHK(rows >= 0 && n_blocks > 0 && n_dst_blocks > 0 && (int64_t)rows * n_kv_heads <= 1 << 26 &&
-            ((int64_t)rows + 63) / 64 * n_kv_heads < 1 << 24,  // a launch has fewer than 2^32 threads, 256 to a workgroup
+            ((int64_t)rows + 63) / 64 * n_kv_heads < 1 << 24,
         "kv4 read: sizes");
   if (rows == 0) return LP_OK;  // no rows: nothing is read or written
   OPCHK(cache && src_entry && dst_entry && k_cache && v_cache, "kv4 read: pointers");

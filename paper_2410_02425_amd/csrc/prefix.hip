@@ -818,7 +818,9 @@ __global__ __launch_bounds__(512) void prefix_row_kernel(const T *__restrict__ q
 // at a time; of four waves each takes 16 of the 64, and they add up in LDS (one
 // row of 32 heads, 66 parts: the call 26.2 -> 22.3 us).  Bound by memory: MANY, for
 // rows enough to hide the weights' loads, then asks for the o of parts with keys
-// alone (633 rows of 32 heads, two of three parts each, 9.2 us, else 11.0).
+// alone (634 rows of 32 heads, one to three of three parts with keys, 8.65 us, else 9.1;
+// where nearly all have keys the two are alike: 633 rows, up to four parts, 9.4 and 9.2,
+// 547, 9.3 and 9.3, 64 rows of 64 heads, more than eight, 7.75 and 7.7).
 template <typename T, int HD, int U, int W, bool MANY>
 __global__ __launch_bounds__(256) void prefix_join_kernel(T *__restrict__ out, PrefixArgs a) {
   static_assert(W == 1 || (W == 4 && U == 16), "a fourth of 64 parts in one step");
@@ -1090,7 +1092,8 @@ static bool launch_prefix_hd(const T *q, T *out, const PrefixBatch &b, float *ws
   a.by_shared = divisor(a.shared_rows);
   a.by_per = divisor(ceil_div(a.G, rto));
   const int64_t items = ((int64_t)(a.tiles + a.shared_rows) * a.splits + (int64_t)a.units * a.osplits) * Hkv;
-  if (std::max(items, join_wgs(b, a.parts)) >= 1 << 23) return false;  // a launch has fewer than 2^32 threads, 512 to a workgroup
+  // a launch has fewer than 2^32 threads, 512 to a workgroup
+  if (std::max(items, join_wgs(b, a.parts)) >= 1 << 23) return false;
   auto grid = [](int64_t n) { return dim3((unsigned)n); };
   if (a.whole) {
     prefix_row_kernel<T, HD><<<grid((int64_t)a.otiles * Hkv), WHOLE_WAVES<T, HD> * 64, 0, s>>>(q, out, a);
